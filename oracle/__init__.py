@@ -6,4 +6,4 @@ __graft_entry__.smoke() and bench.py's cpu_baseline leg may import this
 package; the product (paper_2511_12056_amd) never does.
 """
 from .attention import attention_head, attention, widen_bf16, merge_partials  # noqa: F401
-from . import pipesp_layout, planner, pack  # noqa: F401,E402
+from . import pipesp_layout, planner, pack, train  # noqa: F401,E402

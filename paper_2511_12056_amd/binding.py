@@ -18,6 +18,13 @@ PDA_NOALLOC_MAX_SLOTS = 576
 PDA_MAX_KEY_RANGES = 16
 PDA_MAX_LOCAL_HEADS = 64
 PDA_SINK_HEAD_MAJOR, PDA_SINK_TOKEN_ARRIVAL, PDA_SINK_TOKEN_FINAL = 0, 1, 2
+PDA_F32, PDA_BF16 = 0, 1
+PDA_LAYER_NORM_MAX = 8192
+
+
+class AttnBwdStrides(C.Structure):
+    """pda_attn_bwd_strides: batch and head strides in elements."""
+    _fields_ = [(n + "_" + a, C.c_int64) for n in ("dout", "q", "kv", "out", "lse", "dq", "dkv") for a in ("batch", "head")]
 
 
 class PdaError(RuntimeError):
@@ -77,6 +84,20 @@ def _load() -> C.CDLL:
     lib.pda_probe_mfma_rate.restype = i32
     lib.pda_probe_loop_rate.argtypes = [vp, i64, i64, i32, C.POINTER(f32), C.POINTER(f32), vp]
     lib.pda_probe_loop_rate.restype = i32
+    lib.pda_attn_bwd.argtypes = [vp] * 5 + [i32, fp, vp, vp, vp, i32, i32, i64, i64, i32, f32, i64, vp, i64, vp]
+    lib.pda_attn_bwd.restype = i32
+    lib.pda_attn_bwd_strided.argtypes = [vp] * 5 + [i32, fp, vp, vp, vp, i32, i32, i64, i64, i32, C.POINTER(AttnBwdStrides), f32, i64, vp, i64, vp]
+    lib.pda_attn_bwd_strided.restype = i32
+    lib.pda_attn_bwd_workspace.argtypes = [i32, i32, i64, i64, i32, i64, i32, C.POINTER(i64)]
+    lib.pda_attn_bwd_workspace.restype = i32
+    lib.pda_layer_norm_fwd.argtypes = [vp, i32, fp, fp, vp, i32, fp, fp, i64, i64, i32, f32, vp]
+    lib.pda_layer_norm_fwd.restype = i32
+    lib.pda_layer_norm_bwd.argtypes = [vp, i32, vp, i32, fp, fp, fp, vp, fp, fp, i64, i64, i32, vp, i64, vp]
+    lib.pda_layer_norm_bwd.restype = i32
+    lib.pda_layer_norm_bwd_workspace.argtypes = [i64, i64, i32, i32, C.POINTER(i64)]
+    lib.pda_layer_norm_bwd_workspace.restype = i32
+    lib.pda_pack_heads_bwd.argtypes = [vp, fp, fp, i32, i64, i32, i32, i32, f32, vp]
+    lib.pda_pack_heads_bwd.restype = i32
     lib.pda_last_error.argtypes = []
     lib.pda_last_error.restype = C.c_char_p
     lib.pda_version.argtypes = []
@@ -358,6 +379,192 @@ def pack_heads(x, y, unit_rms: bool, premul: float = 1.0, stream=None):
     _expect(y, torch.bfloat16, (B, H, S, d), "y")
     _check(lib.pda_pack_heads(_ptr(x), _ptr(y), B, S, H, d, 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
     return y
+
+
+# ---- training: gradients, layer norm (include/pipedit_train.h) ----------------------------------------------
+
+def _type_code(t, name):
+    import torch
+    if t.dtype is torch.float32:
+        return PDA_F32
+    if t.dtype is torch.bfloat16:
+        return PDA_BF16
+    raise ValueError(f"{name}: expected fp32 or bf16, got {t.dtype}")
+
+
+def _workspace(nbytes: int, workspace, stream):
+    """The given workspace, checked, or a new one from torch's allocator, on the stream of the call that is to use it."""
+    import torch
+    if workspace is None:
+        if nbytes == 0:
+            return None
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda:
+        raise ValueError("workspace: expected a contiguous cuda uint8 tensor")
+    return workspace
+
+
+def attn_bwd_workspace_bytes(B: int, H: int, Sq: int, Skv: int, d: int, kv_valid_len: Optional[int] = None, n_cu: int = 0) -> int:
+    """pda_attn_bwd_workspace; n_cu = 0 asks the current device."""
+    n = C.c_int64(0)
+    _check(lib.pda_attn_bwd_workspace(int(B), int(H), int(Sq), int(Skv), int(d), int(Skv if kv_valid_len is None else kv_valid_len),
+                                      int(n_cu), C.byref(n)))
+    return n.value
+
+
+def attn_bwd_workspace(B: int, H: int, Sq: int, Skv: int, d: int, kv_valid_len: Optional[int] = None):
+    """A workspace for attn_bwd calls of these sizes on the current device, for programs that keep it."""
+    import torch
+    return torch.empty(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, kv_valid_len), dtype=torch.uint8, device="cuda")
+
+
+def attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid_len: Optional[int] = None, workspace=None, stream=None):
+    """pda_attn_bwd: dout, q [B,H,Sq,d], k, v [B,H,Skv,d] bf16, out fp32 or bf16 and lse of the forward call -> dq, dk, dv bf16.
+
+    workspace: a uint8 tensor of attn_bwd_workspace_bytes (attn_bwd_workspace makes one); None takes one from torch's allocator.
+    """
+    import torch
+    B, H, Sq, d = q.shape
+    Skv = k.shape[2]
+    bf16 = torch.bfloat16
+    _expect(q, bf16, (B, H, Sq, d), "q")
+    _expect(k, bf16, (B, H, Skv, d), "k")
+    _expect(v, bf16, (B, H, Skv, d), "v")
+    _expect(dout, bf16, (B, H, Sq, d), "dout")
+    out_type = _type_code(out, "out")
+    _expect(out, out.dtype, (B, H, Sq, d), "out")
+    _expect(lse, torch.float32, (B, H, Sq), "lse")
+    _expect(dq, bf16, (B, H, Sq, d), "dq")
+    _expect(dk, bf16, (B, H, Skv, d), "dk")
+    _expect(dv, bf16, (B, H, Skv, d), "dv")
+    n_v = Skv if kv_valid_len is None else int(kv_valid_len)
+    if workspace is None:
+        workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
+    else:
+        _workspace(0, workspace, stream)
+    _check(lib.pda_attn_bwd(_ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(out), out_type, _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
+                            B, H, Sq, Skv, d, float(scale), n_v, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                            _stream_handle(stream)))
+    return dq, dk, dv
+
+
+def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid_len: Optional[int] = None, workspace=None, stream=None):
+    """pda_attn_bwd_strided: as attn_bwd, on [B,H,S,d] VIEWS (e.g. x[:, :, a:b]) with compact rows; no copies."""
+    import torch
+    B, H, Sq, d = q.shape
+    Skv = k.shape[2]
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (dout, "dout"), (dq, "dq"), (dk, "dk"), (dv, "dv")):
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"{name}: expected bf16")
+    out_type = _type_code(out, "out")
+    if lse.dtype != torch.float32:
+        raise ValueError("lse: expected fp32")
+    if any(tuple(t.shape) != (B, H, Sq, d) for t in (dout, out, dq)) or any(tuple(t.shape) != (B, H, Skv, d) for t in (k, v, dk, dv)) \
+            or tuple(lse.shape) != (B, H, Sq):
+        raise ValueError("shape mismatch")
+    st = [_view_strides(t, 2, name) for t, name in ((dout, "dout"), (q, "q"), (k, "k"), (out, "out"))]
+    st += [_view_strides(lse, 1, "lse"), _view_strides(dq, 2, "dq"), _view_strides(dk, 2, "dk")]
+    if _view_strides(v, 2, "v") != st[2] or _view_strides(dv, 2, "dv") != st[6]:
+        raise ValueError("k and v must share their strides, and dk and dv theirs")
+    n_v = Skv if kv_valid_len is None else int(kv_valid_len)
+    if workspace is None:
+        workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
+    else:
+        _workspace(0, workspace, stream)
+    _check(lib.pda_attn_bwd_strided(_ptr(dout), _ptr(q), _ptr(k), _ptr(v), _ptr(out), out_type, _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv),
+                                    B, H, Sq, Skv, d, C.byref(AttnBwdStrides(*(x for s in st for x in s))), float(scale), n_v,
+                                    _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream)))
+    return dq, dk, dv
+
+
+def _norm_rows(x, name):
+    if x.dim() < 1 or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name}: expected a contiguous cuda tensor of at least one axis")
+    D = x.shape[-1]
+    return (x.numel() // D if D else 0), D
+
+
+def _norm_groups(D, *params):
+    """Groups of [D] or [groups, D] fp32 parameters (None: not wanted), which must agree."""
+    import torch
+    groups = None
+    for t, name in params:
+        if t is None:
+            continue
+        if t.dtype is not torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != D or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: expected contiguous cuda fp32 [{D}] or [groups, {D}], got {t.dtype} {tuple(t.shape)}")
+        n = t.shape[0] if t.dim() == 2 else 1
+        if groups not in (None, n):
+            raise ValueError(f"{name}: {n} groups, another parameter has {groups}")
+        groups = n
+    return 1 if groups is None else groups
+
+
+def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, stream=None):
+    """pda_layer_norm_fwd: x [..., D] -> y [..., D] (fp32 or bf16 each), mean and rstd [rows] fp32 for the backward call.
+
+    weight, bias: [D], or [groups, D] with one row for every rows/groups consecutive rows of x, or None.
+    """
+    import torch
+    rows, D = _norm_rows(x, "x")
+    _expect(y, y.dtype, x.shape, "y")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
+    _check(lib.pda_layer_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(bias), _ptr(y), _type_code(y, "y"), _ptr(mean), _ptr(rstd),
+                                  rows, _norm_groups(D, (weight, "weight"), (bias, "bias")), D, float(eps), _stream_handle(stream)))
+    return y, mean, rstd
+
+
+def layer_norm_bwd_workspace_bytes(rows: int, D: int, groups: int = 1, n_cu: int = 0) -> int:
+    """pda_layer_norm_bwd_workspace; n_cu = 0 asks the current device."""
+    n = C.c_int64(0)
+    _check(lib.pda_layer_norm_bwd_workspace(int(rows), int(groups), int(D), int(n_cu), C.byref(n)))
+    return n.value
+
+
+def layer_norm_bwd_workspace(rows: int, D: int, groups: int = 1):
+    """A workspace for layer_norm_bwd calls of these sizes on the current device, for programs that keep it."""
+    import torch
+    return torch.empty(layer_norm_bwd_workspace_bytes(rows, D, groups), dtype=torch.uint8, device="cuda")
+
+
+def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace=None, stream=None):
+    """pda_layer_norm_bwd: dy like y, x, weight, mean, rstd of the forward call -> dx like x, dweight and dbias [D] or [groups, D].
+
+    dx, dweight and dbias may be None; weight is None where the forward call had none.
+    """
+    import torch
+    rows, D = _norm_rows(x, "x")
+    _expect(dy, dy.dtype, x.shape, "dy")
+    if dx is not None:
+        _expect(dx, x.dtype, x.shape, "dx")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
+    groups = _norm_groups(D, (weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
+    if workspace is None:
+        need = layer_norm_bwd_workspace_bytes(rows, D, groups) if dweight is not None or dbias is not None else 0
+        workspace = _workspace(need, None, stream)
+    else:
+        _workspace(0, workspace, stream)
+    _check(lib.pda_layer_norm_bwd(_ptr(dy), _type_code(dy, "dy"), _ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(mean), _ptr(rstd),
+                                  _ptr(dx), _ptr(dweight), _ptr(dbias), rows, groups, D,
+                                  _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream)))
+    return dx, dweight, dbias
+
+
+def pack_heads_bwd(dy, x, dx, unit_rms: bool, premul: float = 1.0, stream=None):
+    """pda_pack_heads_bwd: dy [B,H,S,d] bf16, the pack's x [B,S,H,d] fp32 (None without unit_rms) -> dx [B,S,H,d] fp32."""
+    import torch
+    B, H, S, d = dy.shape
+    _expect(dy, torch.bfloat16, (B, H, S, d), "dy")
+    if x is not None:
+        _expect(x, torch.float32, (B, S, H, d), "x")
+    _expect(dx, torch.float32, (B, S, H, d), "dx")
+    _check(lib.pda_pack_heads_bwd(_ptr(dy), _ptr(x), _ptr(dx), B, S, H, d, 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
+    return dx
 
 
 def plan_n_decode(t_denoise: float, t_decode: float, N: int) -> int:

@@ -11,6 +11,7 @@
 #include <vector>
 #include "../../include/pipedit_attn.h"
 #include "attn_internal.h"
+#include "train_internal.h"
 
 namespace {
 
@@ -99,6 +100,14 @@ hipError_t launch_strided(const void* q, const void* k, const void* v, float* ou
 }  // namespace
 
 namespace pda {
+
+int report(int code, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
 
 hipError_t device_cu_count(int* n_cu) {
     static std::atomic<int> cu[KernelSetup::MAX_DEV] = {};

@@ -7,11 +7,14 @@
 //     head-contiguous order (k_orig = k), i.e. with the post-processing folded into the copy.
 //   * pack_heads_kernel: token-major fp32 projections -> head-major bf16, optionally dividing
 //     every d-vector by its root mean square.
+//   * pack_heads_bwd_kernel: its gradient, head-major bf16 -> token-major fp32.
 // Every thread moves 16 bytes of fp32; a d-vector (64 or 128 floats) is one 256/512-byte segment,
 // so both sides of each copy are made of full cache lines.
 #include <hip/hip_runtime.h>
 #include "attn_internal.h"
 #include "attn_device.h"
+#include "train_device.h"
+#include "train_internal.h"
 
 namespace pda {
 
@@ -148,6 +151,61 @@ hipError_t launch_pack(const float* x, void* y, int B, int64_t S, int H, int d, 
         hipLaunchKernelGGL(pack_heads_kernel<16>, dim3(H, g.y, g.z), dim3(256), 0, st, xs, yd, S, H, n_blk, B, unit_rms, premul);
     }
     return hipGetLastError();
+}
+
+// Gradient of the pack.  The work split of pack_heads_kernel: LPV lanes a d-vector, VPB consecutive tokens of a head in a
+// workgroup; reads of dy advance sequentially in every head, and the H workgroups of a token block write one contiguous piece of dx.
+template <int LPV, bool RMS>
+__global__ __launch_bounds__(256) void pack_heads_bwd_kernel(const uint2* __restrict__ dy, const float4* x, float4* dx,
+                                                             int64_t S, int H, int64_t n_blk /* ceil(S/VPB) */, int B, float premul) {
+    constexpr int VPB = 256 / LPV;
+    const int lane = threadIdx.x % LPV;
+    const int hh = blockIdx.x;
+    const int64_t bb = grid_row();                            // b * n_blk + block
+    if (bb >= n_blk * B) return;
+    int64_t b = 0, blk = bb;
+    if (B > 1) { b = bb / n_blk; blk = bb - b * n_blk; }     // wave-uniform, taken only with several batches
+    const int64_t s = blk * VPB + threadIdx.x / LPV;
+    const bool live = s < S;
+    float4 g = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int64_t at = ((b * S + s) * H + hh) * LPV + lane;
+    if (live) {
+        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(dy + ((b * H + hh) * S + s) * LPV + lane));
+        g = make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
+    }
+    if constexpr (RMS) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (live) a = nt_load4(x + at);
+        const float ss = lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w);
+        const float dot = lane_sum<LPV>(a.x * g.x + a.y * g.y + a.z * g.z + a.w * g.w);
+        // dx = premul r (dy - x <x, dy> / <x, x>)
+        const float r = ss > 0.f ? premul / sqrtf(ss * (1.0f / (4 * LPV))) : 0.f;
+        const float f = ss > 0.f ? -dot / ss : 0.f;
+        g.x = r * __builtin_fmaf(a.x, f, g.x);
+        g.y = r * __builtin_fmaf(a.y, f, g.y);
+        g.z = r * __builtin_fmaf(a.z, f, g.z);
+        g.w = r * __builtin_fmaf(a.w, f, g.w);
+    } else {
+        g.x *= premul; g.y *= premul; g.z *= premul; g.w *= premul;
+    }
+    if (live) nt_store4(dx + at, g);
+}
+
+template <int LPV>
+static hipError_t launch_pack_bwd_d(const void* dy, const float* x, float* dx, int B, int64_t S, int H, int unit_rms, float premul, hipStream_t st) {
+    const uint2* g = reinterpret_cast<const uint2*>(dy);
+    const float4* xs = reinterpret_cast<const float4*>(x);
+    float4* to = reinterpret_cast<float4*>(dx);
+    const int64_t n_blk = (S + 256 / LPV - 1) / (256 / LPV);
+    const RowGrid r = row_grid(n_blk * B);
+    const dim3 grid(H, r.y, r.z);
+    if (unit_rms) hipLaunchKernelGGL((pack_heads_bwd_kernel<LPV, true>), grid, dim3(256), 0, st, g, xs, to, S, H, n_blk, B, premul);
+    else hipLaunchKernelGGL((pack_heads_bwd_kernel<LPV, false>), grid, dim3(256), 0, st, g, xs, to, S, H, n_blk, B, premul);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack_bwd(const void* dy, const float* x, float* dx, int B, int64_t S, int H, int d, int unit_rms, float premul, hipStream_t st) {
+    return d == 128 ? launch_pack_bwd_d<32>(dy, x, dx, B, S, H, unit_rms, premul, st) : launch_pack_bwd_d<16>(dy, x, dx, B, S, H, unit_rms, premul, st);
 }
 
 }  // namespace pda

@@ -1,0 +1,242 @@
+// C ABI of the training operators: argument validation and launches.
+#include <hip/hip_runtime.h>
+#include <cmath>
+#include "../../include/pipedit_train.h"
+#include "attn_internal.h"
+#include "train_internal.h"
+
+namespace {
+
+using pda::report;
+
+int hip_error(hipError_t e, const char* what) { return report(PDA_ERR_HIP, "%s: %s", what, hipGetErrorString(e)); }
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+bool bad_type(int t) { return t != PDA_F32 && t != PDA_BF16; }
+
+// Do the ranges [a, a + na) and [b, b + nb) share a byte?
+bool overlap(const void* a, double na, const void* b, double nb) {
+    const double x = (double)reinterpret_cast<uintptr_t>(a), y = (double)reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+int check_bwd_sizes(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_valid_len) {
+    if (B < 0 || H < 0 || Sq < 0 || Skv < 0) return report(PDA_ERR_INVALID_ARG, "negative size (B=%d H=%d Sq=%lld Skv=%lld)", B, H, (long long)Sq, (long long)Skv);
+    if (d != 64 && d != 128) return report(PDA_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", d);
+    if (kv_valid_len < 0 || kv_valid_len > Skv) return report(PDA_ERR_INVALID_ARG, "kv_valid_len=%lld outside [0, Skv=%lld]", (long long)kv_valid_len, (long long)Skv);
+    if (Sq >= (int64_t)1 << 31 || Skv >= (int64_t)1 << 31) return report(PDA_ERR_UNSUPPORTED, "sequence length beyond 2^31");
+    if ((double)B * H * (double)(Sq > Skv ? Sq : Skv) * d >= 1099511627776.0) return report(PDA_ERR_UNSUPPORTED, "B*H*S*d overflows 2^40 elements");
+    if ((int64_t)B * H > 65535) return report(PDA_ERR_UNSUPPORTED, "B*H > 65535");
+    return PDA_OK;
+}
+
+int attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type, const float* lse,
+             void* dq, void* dk, void* dv, int B, int H, int64_t Sq, int64_t Skv, int d, const pda_attn_bwd_strides& s, bool compact,
+             float scale, int64_t n_v, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_bwd_sizes(B, H, Sq, Skv, d, n_v);
+    if (rc != PDA_OK) return rc;
+    if (!(scale >= 0.0f) || !std::isfinite(scale)) return report(PDA_ERR_INVALID_ARG, "scale must be finite and >= 0");
+    if (bad_type(out_type)) return report(PDA_ERR_INVALID_ARG, "unknown out_type=%d", out_type);
+    if (B == 0 || H == 0 || (Sq == 0 && Skv == 0)) return PDA_OK;
+    if (Sq > 0 && (!dout || !q || !out || !lse || !dq)) return report(PDA_ERR_INVALID_ARG, "null dout/q/out/lse/dq");
+    if (Sq > 0 && n_v > 0 && (!k || !v)) return report(PDA_ERR_INVALID_ARG, "null k/v");
+    if (Skv > 0 && (!dk || !dv)) return report(PDA_ERR_INVALID_ARG, "null dk/dv");
+    for (const void* p : {dout, q, k, v, out, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
+        if (!aligned(p, 16)) return report(PDA_ERR_UNSUPPORTED, "dout/q/k/v/out/dq/dk/dv must be 16-byte aligned");
+    if (!aligned(lse, 4)) return report(PDA_ERR_UNSUPPORTED, "lse must be 4-byte aligned");
+    const double rows_q = (double)B * H * (double)Sq, rows_k = (double)B * H * (double)Skv;
+    const struct { const void* p; double bytes; const char* name; } in[6] = {
+        {dout, rows_q * d * 2, "dout"}, {q, rows_q * d * 2, "q"}, {out, rows_q * d * (out_type == PDA_BF16 ? 2 : 4), "out"}, {lse, rows_q * 4, "lse"},
+        {k, rows_k * d * 2, "k"}, {v, rows_k * d * 2, "v"}};
+    const struct { const void* p; double bytes; const char* name; } res[3] = {{dq, rows_q * d * 2, "dq"}, {dk, rows_k * d * 2, "dk"}, {dv, rows_k * d * 2, "dv"}};
+    for (int i = 0; i < 3; ++i) {         // views may interleave: only their first elements are compared
+        const double n = compact ? res[i].bytes : (res[i].bytes > 0 ? 1 : 0);
+        for (const auto& x : in)
+            if (x.p && overlap(res[i].p, n, x.p, compact ? x.bytes : 1)) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", res[i].name, x.name);
+        for (int j = 0; j < i; ++j)
+            if (overlap(res[i].p, n, res[j].p, compact ? res[j].bytes : (res[j].bytes > 0 ? 1 : 0))) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", res[i].name, res[j].name);
+    }
+    int64_t need = 0;
+    if ((rc = pda_attn_bwd_workspace(B, H, Sq, Skv, d, n_v, 0, &need)) != PDA_OK) return rc;
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", workspace ? (long long)workspace_bytes : 0LL, (long long)need);
+    if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
+    pda::AttnBwdParams p{};
+    p.dout = static_cast<const __bf16*>(dout);
+    p.q = static_cast<const __bf16*>(q);
+    p.k = static_cast<const __bf16*>(k);
+    p.v = static_cast<const __bf16*>(v);
+    p.out = out;
+    p.lse = lse;
+    p.dq = static_cast<__bf16*>(dq);
+    p.dk = static_cast<__bf16*>(dk);
+    p.dv = static_cast<__bf16*>(dv);
+    p.Sq = Sq; p.Skv = Skv; p.n_v = n_v;
+    p.stat_rows = pda::bwd_stat_rows(Sq);
+    p.nlse2 = static_cast<float*>(workspace);
+    p.ndelta = p.nlse2 + (int64_t)B * H * p.stat_rows;
+    p.do_bs = s.dout_batch; p.do_hs = s.dout_head;
+    p.q_bs = s.q_batch; p.q_hs = s.q_head;
+    p.kv_bs = s.kv_batch; p.kv_hs = s.kv_head;
+    p.o_bs = s.out_batch; p.o_hs = s.out_head;
+    p.l_bs = s.lse_batch; p.l_hs = s.lse_head;
+    p.dq_bs = s.dq_batch; p.dq_hs = s.dq_head;
+    p.dkv_bs = s.dkv_batch; p.dkv_hs = s.dkv_head;
+    p.B = B; p.H = H;
+    p.out_bf16 = out_type == PDA_BF16 ? 1 : 0;
+    p.scale = scale;
+    p.scale_log2e = (float)((double)scale * 1.4426950408889634);     // exactly 1 for scale = (float)ln 2
+    const hipError_t e = pda::launch_attn_bwd(p, d, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)PDA_OK : hip_error(e, "attention gradient launch");
+}
+
+int check_layer_norm(int x_type, int y_type, int64_t rows, int64_t groups, int D) {
+    if (bad_type(x_type) || bad_type(y_type)) return report(PDA_ERR_INVALID_ARG, "unknown type (x_type=%d y_type=%d)", x_type, y_type);
+    if (rows < 0 || groups < 1) return report(PDA_ERR_INVALID_ARG, "rows=%lld groups=%lld (need >= 0, >= 1)", (long long)rows, (long long)groups);
+    if (rows % groups != 0) return report(PDA_ERR_INVALID_ARG, "rows=%lld is not a multiple of groups=%lld", (long long)rows, (long long)groups);
+    if (D < 1) return report(PDA_ERR_INVALID_ARG, "D=%d (need >= 1)", D);
+    if (D > PDA_LAYER_NORM_MAX) return report(PDA_ERR_UNSUPPORTED, "D=%d exceeds PDA_LAYER_NORM_MAX=%d", D, PDA_LAYER_NORM_MAX);
+    if (groups > 65535) return report(PDA_ERR_UNSUPPORTED, "groups=%lld beyond 65535", (long long)groups);
+    if (rows >= (int64_t)1 << 31 || (double)rows * D >= 1099511627776.0) return report(PDA_ERR_UNSUPPORTED, "rows beyond 2^31 or rows*D beyond 2^40 elements");
+    return PDA_OK;
+}
+
+double row_bytes(int64_t rows, int D, int type) { return (double)rows * D * (type == PDA_BF16 ? 2 : 4); }
+
+// An output may be an input itself (equal address and type), but not lie across it.
+int check_in_place(const void* out, int out_type, const char* out_name, const void* in, int in_type, const char* in_name, int64_t rows, int D) {
+    if (out == in && out_type == in_type) return PDA_OK;
+    if (overlap(out, row_bytes(rows, D, out_type), in, row_bytes(rows, D, in_type)))
+        return report(PDA_ERR_INVALID_ARG, "%s overlaps %s without being it", out_name, in_name);
+    return PDA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_valid_len, int n_cu, int64_t* bytes) {
+    int rc = check_bwd_sizes(B, H, Sq, Skv, d, kv_valid_len);
+    if (rc != PDA_OK) return rc;
+    if (n_cu < 0) return report(PDA_ERR_INVALID_ARG, "n_cu=%d is negative", n_cu);
+    if (!bytes) return report(PDA_ERR_INVALID_ARG, "null bytes");
+    *bytes = pda::bwd_workspace_bytes((int64_t)B * H, Sq);
+    return PDA_OK;
+}
+
+int pda_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type,
+                 const float* lse, void* dq, void* dk, void* dv,
+                 int B, int H, int64_t Sq, int64_t Skv, int d, float scale, int64_t kv_valid_len,
+                 void* workspace, int64_t workspace_bytes, void* stream) {
+    const int rc = check_bwd_sizes(B, H, Sq, Skv, d, kv_valid_len);       // before they are multiplied
+    if (rc != PDA_OK) return rc;
+    const int64_t qh = Sq * d, kh = Skv * d, qb = H * qh, kb = H * kh;
+    const pda_attn_bwd_strides s{qb, qh, qb, qh, kb, kh, qb, qh, H * Sq, Sq, qb, qh, kb, kh};
+    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, true, scale, kv_valid_len, workspace, workspace_bytes, stream);
+}
+
+int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type,
+                         const float* lse, void* dq, void* dk, void* dv,
+                         int B, int H, int64_t Sq, int64_t Skv, int d, const pda_attn_bwd_strides* strides, float scale,
+                         int64_t kv_valid_len, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_bwd_sizes(B, H, Sq, Skv, d, kv_valid_len);
+    if (rc != PDA_OK) return rc;
+    if (!strides) return report(PDA_ERR_INVALID_ARG, "null strides");
+    if (bad_type(out_type)) return report(PDA_ERR_INVALID_ARG, "unknown out_type=%d", out_type);
+    const pda_attn_bwd_strides& s = *strides;
+    for (int64_t x : {s.dout_batch, s.dout_head, s.q_batch, s.q_head, s.kv_batch, s.kv_head, s.out_batch, s.out_head, s.lse_batch, s.lse_head,
+                      s.dq_batch, s.dq_head, s.dkv_batch, s.dkv_head})
+        if (x < 0 || x >= ((int64_t)1 << 40)) return report(PDA_ERR_INVALID_ARG, "stride %lld outside [0, 2^40)", (long long)x);
+    if ((s.dout_batch | s.dout_head | s.q_batch | s.q_head | s.kv_batch | s.kv_head | s.dq_batch | s.dq_head | s.dkv_batch | s.dkv_head) % 8 != 0)
+        return report(PDA_ERR_UNSUPPORTED, "strides of bf16 tensors must be multiples of 8 elements");
+    if ((s.out_batch | s.out_head) % (out_type == PDA_BF16 ? 8 : 4) != 0) return report(PDA_ERR_UNSUPPORTED, "out strides must be multiples of 16 bytes");
+    const struct { int64_t batch, head, extent; const char* name; } res[2] = {{s.dq_batch, s.dq_head, Sq * d, "dq"}, {s.dkv_batch, s.dkv_head, Skv * d, "dk/dv"}};
+    for (const auto& x : res) {
+        if (H > 1 && x.head < x.extent) return report(PDA_ERR_INVALID_ARG, "heads of %s overlap (head stride too small)", x.name);
+        if (B > 1 && x.batch < (int64_t)(H - 1) * x.head + x.extent) return report(PDA_ERR_INVALID_ARG, "batches of %s overlap (batch stride too small)", x.name);
+    }
+    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, false, scale, kv_valid_len, workspace, workspace_bytes, stream);
+}
+
+int pda_layer_norm_fwd(const void* x, int x_type, const float* weight, const float* bias, void* y, int y_type,
+                       float* mean, float* rstd, int64_t rows, int64_t groups, int D, float eps, void* stream) {
+    int rc = check_layer_norm(x_type, y_type, rows, groups, D);
+    if (rc != PDA_OK) return rc;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return report(PDA_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if (!mean != !rstd) return report(PDA_ERR_INVALID_ARG, "mean and rstd go together");
+    if (rows == 0) return PDA_OK;
+    if (!x || !y) return report(PDA_ERR_INVALID_ARG, "null x/y");
+    if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, 16) || !aligned(bias, 16)) return report(PDA_ERR_UNSUPPORTED, "x/y/weight/bias must be 16-byte aligned");
+    if (!aligned(mean, 4) || !aligned(rstd, 4)) return report(PDA_ERR_UNSUPPORTED, "mean/rstd must be 4-byte aligned");
+    if ((rc = check_in_place(y, y_type, "y", x, x_type, "x", rows, D)) != PDA_OK) return rc;
+    pda::LayerNormParams p{};
+    p.x = x; p.weight = weight; p.bias = bias; p.y = y; p.mean = mean; p.rstd = rstd;
+    p.rows = rows; p.groups = groups; p.group_rows = rows / groups; p.D = D; p.eps = eps;
+    const hipError_t e = pda::launch_layer_norm_fwd(p, x_type == PDA_BF16, y_type == PDA_BF16, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)PDA_OK : hip_error(e, "layer norm launch");
+}
+
+int pda_layer_norm_bwd_workspace(int64_t rows, int64_t groups, int D, int n_cu, int64_t* bytes) {
+    int rc = check_layer_norm(PDA_F32, PDA_F32, rows, groups, D);
+    if (rc != PDA_OK) return rc;
+    if (n_cu < 0) return report(PDA_ERR_INVALID_ARG, "n_cu=%d is negative", n_cu);
+    if (!bytes) return report(PDA_ERR_INVALID_ARG, "null bytes");
+    if (n_cu == 0) {
+        const hipError_t e = pda::device_cu_count(&n_cu);
+        if (e != hipSuccess) return hip_error(e, "device query");
+    }
+    *bytes = pda::ln_workspace_bytes(rows, groups, D, n_cu);
+    return PDA_OK;
+}
+
+int pda_layer_norm_bwd(const void* dy, int y_type, const void* x, int x_type, const float* weight, const float* mean,
+                       const float* rstd, void* dx, float* dweight, float* dbias, int64_t rows, int64_t groups, int D,
+                       void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_layer_norm(x_type, y_type, rows, groups, D);
+    if (rc != PDA_OK) return rc;
+    if (!dx && !dweight && !dbias) return report(PDA_ERR_INVALID_ARG, "null dx, dweight and dbias: nothing to compute");
+    if (!aligned(weight, 16) || !aligned(dweight, 16) || !aligned(dbias, 16)) return report(PDA_ERR_UNSUPPORTED, "weight/dweight/dbias must be 16-byte aligned");
+    if (rows == 0 && !dweight && !dbias) return PDA_OK;
+    pda::LayerNormParams p{};
+    if (rows > 0) {
+        if (!dy || !x || !mean || !rstd) return report(PDA_ERR_INVALID_ARG, "null dy/x/mean/rstd");
+        if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(dx, 16)) return report(PDA_ERR_UNSUPPORTED, "dy/x/dx must be 16-byte aligned");
+        if (!aligned(mean, 4) || !aligned(rstd, 4)) return report(PDA_ERR_UNSUPPORTED, "mean/rstd must be 4-byte aligned");
+        if (dx && (rc = check_in_place(dx, x_type, "dx", x, x_type, "x", rows, D)) != PDA_OK) return rc;
+        if (dx && (rc = check_in_place(dx, x_type, "dx", dy, y_type, "dy", rows, D)) != PDA_OK) return rc;
+        int n_cu = 0;
+        const hipError_t e = pda::device_cu_count(&n_cu);
+        if (e != hipSuccess) return hip_error(e, "device query");
+        const int64_t need = dweight || dbias ? pda::ln_workspace_bytes(rows, groups, D, n_cu) : 0;
+        if (need > 0 && (!workspace || workspace_bytes < need))
+            return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", workspace ? (long long)workspace_bytes : 0LL, (long long)need);
+        if (need > 0 && !aligned(workspace, 16)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 16-byte aligned");
+        p.group_rows = rows / groups;
+        p.chunk_rows = pda::ln_chunk_rows(p.group_rows, groups, n_cu);
+        p.chunks = pda::ln_chunks(p.group_rows, groups, n_cu);
+    }
+    p.x = x; p.dy = dy; p.weight = weight; p.y = dx;
+    p.mean = const_cast<float*>(mean); p.rstd = const_cast<float*>(rstd);
+    p.dweight = dweight; p.dbias = dbias; p.part = static_cast<float*>(workspace);
+    p.rows = rows; p.groups = groups; p.D = D;
+    const hipError_t e = pda::launch_layer_norm_bwd(p, x_type == PDA_BF16, y_type == PDA_BF16, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)PDA_OK : hip_error(e, "layer norm gradient launch");
+}
+
+int pda_pack_heads_bwd(const void* dy, const float* x, float* dx, int B, int64_t S, int H, int d, int unit_rms, float premul, void* stream) {
+    if (B < 0 || H < 0 || S < 0) return report(PDA_ERR_INVALID_ARG, "negative size (B=%d H=%d S=%lld)", B, H, (long long)S);
+    if (d != 64 && d != 128) return report(PDA_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", d);
+    if ((double)B * H * (double)S * d >= 1099511627776.0) return report(PDA_ERR_UNSUPPORTED, "B*H*S*d overflows 2^40 elements");
+    if (B == 0 || H == 0 || S == 0) return PDA_OK;
+    if (!dy || !dx || (unit_rms && !x)) return report(PDA_ERR_INVALID_ARG, "null dy/dx, or x with unit_rms");
+    if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(dx, 16)) return report(PDA_ERR_UNSUPPORTED, "dy, x and dx must be 16-byte aligned");
+    const double n = (double)B * H * (double)S * d;
+    if (overlap(dx, n * 4, dy, n * 2)) return report(PDA_ERR_INVALID_ARG, "dx overlaps dy");
+    if (unit_rms && dx != x && overlap(dx, n * 4, x, n * 4)) return report(PDA_ERR_INVALID_ARG, "dx overlaps x without being it");
+    if (!std::isfinite(premul)) return report(PDA_ERR_INVALID_ARG, "premul must be finite");
+    const hipError_t e = pda::launch_pack_bwd(dy, x, dx, B, S, H, d, unit_rms, premul, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)PDA_OK : hip_error(e, "pack gradient launch");
+}
+
+}  // extern "C"
