@@ -62,165 +62,285 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
             const float x = p.lse[(int64_t)b * p.l_bs + (int64_t)h * p.l_hs + row];
             l = x == -INFINITY ? -INFINITY : -x * kLog2e;
         }
-        p.nlse2[bh * p.stat_rows + row] = l;
-        p.ndelta[bh * p.stat_rows + row] = -sum;
+        float* to = p.stats + (bh * p.stat_rows + row / 32 * 32) * 2 + row % 32;
+        to[0] = l;
+        to[32] = -sum;
     }
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------
 constexpr int kBwdTile = 32;            // streamed rows of a step
-constexpr int kBwdRows = 128;           // resident rows of a workgroup: 32 a wavefront
-constexpr int bwd_smem(int d) { return 2 * 2 * kBwdTile * d * 2; }
+constexpr int kBwdRows = 256;           // resident rows of a workgroup: 64 for each of four pairs of wavefronts
+constexpr int kBwdRing = 4;             // tile buffers per streamed tensor
+constexpr int kBwdExchange = 64 * kBwdTile * 4;          // bytes of the probabilities of a pair and step
+constexpr int bwd_tile_bytes(int d) { return kBwdTile * d * 2; }
+constexpr int bwd_stat_base(int d) { return kBwdRing * 2 * bwd_tile_bytes(d); }
+constexpr int bwd_p_base(int d) { return bwd_stat_base(d) + kBwdRing * 256; }
+constexpr int bwd_smem(int d) { return bwd_p_base(d) + 2 * 4 * kBwdExchange; }
+
+// 4 bytes per lane from global memory straight into LDS (see lds_dma16).
+__device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 vcc, %2\n\tglobal_load_lds_dword %1, vcc"
+                 :
+                 : "s"(lds_addr), "v"(voff), "s"(sbase)
+                 : "memory", "m0", "vcc");
+}
 
 template <int D, bool KEYS>
 __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0) {
-    extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32;
-    constexpr int TILE = kBwdTile * D * 2, CPT = TILE / 1024, RPC = 1024 / (D * 2);
-    const int lane = threadIdx.x & 63, li = lane & 31, lh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2);
+    constexpr int LPI = D == 128 ? 2 : 1;                      // loads of a wavefront per step: a chunk of both tensors, or of one
+    constexpr int PF = 3;                                      // operand fragments read ahead
+    extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))bwd_smem_;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), pair = wave & 3;
+    const int lane = opaque_lane(), li = lane & 31, lh = lane >> 5;
+    const bool second = wave >= 4;
     const int b = bh / p.H, h = bh - b * p.H;
     const __bf16* qp = p.q + (int64_t)b * p.q_bs + (int64_t)h * p.q_hs;
     const __bf16* dop = p.dout + (int64_t)b * p.do_bs + (int64_t)h * p.do_hs;
     const __bf16* kp = p.k + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
     const __bf16* vp = p.v + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
-    const float* nlse2 = p.nlse2 + bh * p.stat_rows;
-    const float* ndelta = p.ndelta + bh * p.stat_rows;
-    const int64_t n_res = KEYS ? p.n_v : p.Sq, n_str = KEYS ? p.Sq : p.n_v;
-    const int64_t row = row0 + wave * 32 + li;                 // this lane's resident row
-    const int nt = row0 < n_res ? (int)((n_str + kBwdTile - 1) / kBwdTile) : 0;
+    const float* stats = p.stats + bh * p.stat_rows * 2;
+    const int64_t n_res = KEYS ? p.n_v : p.Sq;
+    const int n_str = (int)(KEYS ? p.Sq : p.n_v);
+    const int64_t first = row0 + pair * 64;                    // this lane's resident rows: first + li and first + 32 + li
+    const int nt = row0 < n_res ? (n_str + kBwdTile - 1) / kBwdTile : 0;
 
-    f32x16 acc1[NDB], acc2[KEYS ? NDB : 1];                    // dK^T or dQ^T; dV^T
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            acc1[db][r] = 0.f;
-            if constexpr (KEYS) acc2[db][r] = 0.f;
+    // ---- loads of the streamed tiles
+    const __bf16* s1 = KEYS ? qp : kp;
+    const __bf16* s2 = KEYS ? dop : vp;
+    auto issue = [&](int t) __attribute__((always_inline)) {
+        const int slot = t % kBwdRing;
+        const int last = n_str - 1 - t * kBwdTile;
+        const int j = D == 128 ? wave : pair, r = j * RPC + lane / G;
+        const int c = r < last ? r : last;                     // rows behind the last: that row again
+        const unsigned off = c * (D * 2) + (((lane % G) ^ swz_kv<D>(r)) * 16);
+        const unsigned to = lds0 + slot * 2 * TILE + j * 1024;
+        if (D == 128 || !second) lds_dma16(s1 + (int64_t)t * (kBwdTile * D), off, to);
+        if (D == 128 || second) lds_dma16(s2 + (int64_t)t * (kBwdTile * D), off, to + TILE);
+        if (KEYS && wave == 4) lds_dma4(stats + (int64_t)t * (2 * kBwdTile), lane * 4, lds0 + bwd_stat_base(D) + slot * 256);
+    };
+    // the end of step t: what step t + 1 needs is there, what was fetched in this step may be under way
+    auto step_end = [&](int t) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 2 < nt) {
+            if (KEYS && wave == 4) wait_vmcnt<LPI + 1>();
+            else wait_vmcnt<LPI>();
+        } else {
+            wait_vmcnt<0>();
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // ---- operand addresses in slot 0; blocks are XORed in
+    const int t16 = lane & 15, tr_row = 4 * lh + (t16 >> 2), tr_g = 2 * (li >> 4) + ((t16 & 3) >> 1);
+    const unsigned rows_at = lds0 + li * (D * 2) + ((lh ^ swz_kv<D>(li)) * 16);
+    const unsigned tr_lo = lds0 + tr_row * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row)) * 16) + (t16 & 1) * 8;
+    const unsigned tr_hi = lds0 + (tr_row + 8) * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row + 8)) * 16) + (t16 & 1) * 8;
+    auto block = [](unsigned at, auto n) __attribute__((always_inline)) {
+        unsigned r = at;
+        if constexpr (decltype(n)::value != 0) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(r) : "n"(decltype(n)::value), "v"(at));
+        return r;
+    };
+    auto rows_frag = [&](unsigned at, auto kk) __attribute__((always_inline)) {
+        return *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, decltype(kk)::value * 32>{});
+    };
+    auto tr_frag = [&](unsigned lo_at, unsigned hi_at, auto idx) __attribute__((always_inline)) {      // idx = u * NDB + db
+        constexpr int db = decltype(idx)::value % NDB, u = decltype(idx)::value / NDB;
+        LDS_PTR(const unsigned char) x = (LDS_PTR(const unsigned char))(uintptr_t)block(lo_at, std::integral_constant<int, db * 64>{});
+        LDS_PTR(const unsigned char) y = (LDS_PTR(const unsigned char))(uintptr_t)block(hi_at, std::integral_constant<int, db * 64>{});
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(x + u * 16 * (D * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + u * 16 * (D * 2)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const unsigned p_at = lds0 + bwd_p_base(D) + pair * kBwdExchange + lane * 16;
+    auto exchange = [&](int t, int i, int a) __attribute__((always_inline)) {
+        return (LDS_PTR(f32x4))(LDS_PTR(unsigned char))(uintptr_t)(p_at + (t & 1) * (4 * kBwdExchange) + (i * 4 + a) * 1024);
+    };
+    auto stat_at = [&](int t, int which, int a) __attribute__((always_inline)) {
+        return *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(lds0 + bwd_stat_base(D) + (t % kBwdRing) * 256 + which * 128 + 32 * a + 16 * lh);
+    };
+
+    // ---- resident rows
+    bf16x8 res[2][NKK];
+    float res_stat[2] = {0.f, 0.f};
+    f32x16 acc[2][NDB];                                        // first wavefront of a pair: dV^T; second: dK^T or dQ^T
     if (nt > 0) {
-        const __bf16* s1 = KEYS ? qp : kp;
-        const __bf16* s2 = KEYS ? dop : vp;
-        LDS_PTR(unsigned char) smem = (LDS_PTR(unsigned char))bwd_smem_;
-        const unsigned lds0 = (unsigned)(uintptr_t)smem;
-        // chunk j of a tile holds rows j RPC ..; wavefront w fetches chunks w, w + 4 of both tensors
-        auto issue = [&](int t) __attribute__((always_inline)) {
-            const int last = (int)(n_str - 1 - (int64_t)t * kBwdTile < kBwdTile - 1 ? n_str - 1 - (int64_t)t * kBwdTile : kBwdTile - 1);
-            const unsigned to = lds0 + (t & 1) * 2 * TILE;
-#pragma unroll
-            for (int i = 0; i < CPT / 4; ++i) {
-                const int j = wave + 4 * i;
-                const int r = j * RPC + lane / G, c = r < last ? r : last;      // rows behind the last: that row again
-                const unsigned off = c * (D * 2) + (((lane % G) ^ swz_kv<D>(r)) * 16);
-                lds_dma16(s1 + (int64_t)t * (kBwdTile * D), off, to + j * 1024);
-                lds_dma16(s2 + (int64_t)t * (kBwdTile * D), off, to + TILE + j * 1024);
-            }
-        };
         issue(0);
-        bf16x8 r1[NKK], r2[NKK];
-        {
-            const int64_t c = row < n_res ? row : n_res - 1;
-            const __bf16* a1 = (KEYS ? kp : qp) + c * D + lh * 8;
-            const __bf16* a2 = (KEYS ? vp : dop) + c * D + lh * 8;
+        if (nt > 1) issue(1);
+        const __bf16* src = second ? (KEYS ? vp : dop) : (KEYS ? kp : qp);
 #pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) {
-                r1[kk] = *reinterpret_cast<const bf16x8*>(a1 + kk * 16);
-                r2[kk] = *reinterpret_cast<const bf16x8*>(a2 + kk * 16);
-            }
-        }
-        float l_res = 0.f, d_res = 0.f;
-        if constexpr (!KEYS) {
-            l_res = row < n_res ? nlse2[row] : -INFINITY;
-            d_res = row < n_res ? ndelta[row] : 0.f;
+        for (int i = 0; i < 2; ++i) {
+            const int64_t c = first + li + 32 * i < n_res ? first + li + 32 * i : n_res - 1;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) res[i][kk] = *reinterpret_cast<const bf16x8*>(src + c * D + lh * 8 + kk * 16);
+            if constexpr (!KEYS) res_stat[i] = stats[(c / kBwdTile) * (2 * kBwdTile) + (second ? kBwdTile : 0) + c % kBwdTile];
         }
         wait_vmcnt<0>();
         __syncthreads();
-        const int t16 = lane & 15, tr_row = 4 * lh + (t16 >> 2);
-        auto rows_frag = [&](LDS_PTR(const unsigned char) tile, int kk) __attribute__((always_inline)) {
-            return *(LDS_PTR(const bf16x8))(tile + li * (D * 2) + (((2 * kk + lh) ^ swz_kv<D>(li)) * 16));
-        };
-        auto tr_frag = [&](LDS_PTR(const unsigned char) tile, int db, int u) __attribute__((always_inline)) {
-            const int g = db * 4 + 2 * (li >> 4) + ((t16 & 3) >> 1);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(tile + (u * 16 + tr_row) * (D * 2) + ((g ^ swz_kv<D>(tr_row)) * 16) + (t16 & 1) * 8));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(tile + (u * 16 + tr_row + 8) * (D * 2) + ((g ^ swz_kv<D>(tr_row + 8)) * 16) + (t16 & 1) * 8));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        const float c = p.scale_log2e;
-        for (int t = 0; t < nt; ++t) {
-            if (t + 1 < nt) issue(t + 1);
-            LDS_PTR(const unsigned char) t1 = (LDS_PTR(const unsigned char))smem + (t & 1) * 2 * TILE;
-            LDS_PTR(const unsigned char) t2 = t1 + TILE;
-            f32x16 s, dp;
-            f32x4 l[4];
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                f32x4 dl = {d_res, d_res, d_res, d_res};
-                l[a] = f32x4{l_res, l_res, l_res, l_res};
-                if constexpr (KEYS) {
-                    l[a] = *reinterpret_cast<const f32x4*>(nlse2 + t * kBwdTile + 8 * a + 4 * lh);
-                    dl = *reinterpret_cast<const f32x4*>(ndelta + t * kBwdTile + 8 * a + 4 * lh);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { s[4 * a + e] = 0.f; dp[4 * a + e] = dl[e]; }
-            }
-#pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows_frag(t1, kk), r1[kk], s, 0, 0, 0);
-#pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows_frag(t2, kk), r2[kk], dp, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, l[r / 4][r % 4]));
-            if (!KEYS && (int64_t)(t + 1) * kBwdTile > n_str) {
-                const int hidden = (int)(n_str - (int64_t)t * kBwdTile) - 4 * lh;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if ((r >> 2) * 8 + (r & 3) >= hidden) s[r] = 0.f;
-            }
-            u32x4 pk[2], ds[2];
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                pk[r / 8][(r % 8) / 2] = pack_bf16(s[r], s[r + 1]);
-                ds[r / 8][(r % 8) / 2] = pack_bf16(s[r] * dp[r], s[r + 1] * dp[r + 1]);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int db = 0; db < NDB; ++db) {
-                    if constexpr (KEYS) acc2[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_frag(t2, db, u), __builtin_bit_cast(bf16x8, pk[u]), acc2[db], 0, 0, 0);
-                    acc1[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tr_frag(t1, db, u), __builtin_bit_cast(bf16x8, ds[u]), acc1[db], 0, 0, 0);
-                }
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __syncthreads();
-        }
     }
-    // ---- results: 16 bytes a lane (the lane pair's halves of eight columns trade places)
-    const int64_t n_out = KEYS ? p.Skv : p.Sq;
-    auto store = [&](const f32x16* acc, __bf16* base, float factor) __attribute__((always_inline)) {
-        const bool hidden = KEYS && row >= n_res;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
-            for (int a = 0; a < 4; a += 2) {
-                unsigned x[2][2];
+            for (int r = 0; r < 16; ++r) acc[i][db][r] = 0.f;
+    const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    bf16x8 frag[PF + 1];
+    auto step = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+
+    if (!second) {
+        const float c = p.scale_log2e;
+        for (int t = 0; t < nt; ++t) {
+            if (t + 2 < nt) issue(t + 2);
+            const unsigned slot = (t % kBwdRing) * 2 * TILE;
+            f32x16 s[2];
+            {
+                const unsigned at = rows_at + slot;
+                static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = rows_frag(at, j); });
+                static_for<0, NKK>([&](auto j) {
+                    constexpr int n = decltype(j)::value;
+                    if constexpr (n + PF < NKK) frag[(n + PF) % (PF + 1)] = rows_frag(at, std::integral_constant<int, n + PF>{});
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], res[i][n], n == 0 ? zero : s[i], 0, 0, 0);
+                    step();
+                });
+            }
+            const unsigned lo = tr_lo + slot + TILE, hi = tr_hi + slot + TILE;
+            if constexpr (KEYS) static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = tr_frag(lo, hi, j); });
+            u32x4 pk[2][2];
+            const bool tail = !KEYS && (t + 1) * kBwdTile > n_str;
+            const int hidden = n_str - t * kBwdTile - 4 * lh;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                f32x4 l;
+                if constexpr (KEYS) l = stat_at(t, 0, a);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (!KEYS) l = f32x4{res_stat[i], res_stat[i], res_stat[i], res_stat[i]};
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][4 * a + e], c, l[e]));
+                    if (tail)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = 8 * a + e >= hidden ? 0.f : x[e];
+                    *exchange(t, i, a) = x;
+                    if constexpr (KEYS) {
+                        pk[i][a / 2][(a % 2) * 2] = pack_bf16(x[0], x[1]);
+                        pk[i][a / 2][(a % 2) * 2 + 1] = pack_bf16(x[2], x[3]);
+                    }
+                }
+                step();
+            }
+            if constexpr (KEYS) {
+                static_for<0, 2 * NDB>([&](auto j) {
+                    constexpr int n = decltype(j)::value;
+                    if constexpr (n + PF < 2 * NDB) frag[(n + PF) % (PF + 1)] = tr_frag(lo, hi, std::integral_constant<int, n + PF>{});
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        acc[i][n % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], __builtin_bit_cast(bf16x8, pk[i][n / NDB]), acc[i][n % NDB], 0, 0, 0);
+                    step();
+                });
+            }
+            step_end(t);
+        }
+    } else {
+        f32x16 dp[2];
+        // ds of step t - 1 (its p is there), its products, then dp of step t
+        auto sums = [&](int t) __attribute__((always_inline)) {
+            const unsigned slot = (t % kBwdRing) * 2 * TILE;
+            const unsigned lo = tr_lo + slot, hi = tr_hi + slot;
+            u32x4 ds[2][2];
+            static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = tr_frag(lo, hi, j); });
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x4 x = *exchange(t, i, a);
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = x[e] * (KEYS ? dp[i][4 * a + e] : dp[i][4 * a + e] + res_stat[i]);
+                    ds[i][a / 2][(a % 2) * 2] = pack_bf16(y[0], y[1]);
+                    ds[i][a / 2][(a % 2) * 2 + 1] = pack_bf16(y[2], y[3]);
+                }
+            }
+            step();
+            static_for<0, 2 * NDB>([&](auto j) {
+                constexpr int n = decltype(j)::value;
+                if constexpr (n + PF < 2 * NDB) frag[(n + PF) % (PF + 1)] = tr_frag(lo, hi, std::integral_constant<int, n + PF>{});
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
+                    acc[i][n % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], __builtin_bit_cast(bf16x8, ds[i][n / NDB]), acc[i][n % NDB], 0, 0, 0);
+                step();
+            });
+        };
+        auto products = [&](int t) __attribute__((always_inline)) {
+            const unsigned at = rows_at + (t % kBwdRing) * 2 * TILE + TILE;
+            if constexpr (KEYS) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        x[i][e] = hidden ? 0u : pack_bf16(acc[db][4 * (a + i) + 2 * e] * factor, acc[db][4 * (a + i) + 2 * e + 1] * factor);
-                const auto lo = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
-                const auto hi = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
-                if (row < n_out) *reinterpret_cast<u32x4*>(base + row * D + db * 32 + a * 8 + lh * 8) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+                for (int a = 0; a < 4; ++a) {
+                    const f32x4 x = stat_at(t, 1, a);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[0][4 * a + e] = dp[1][4 * a + e] = x[e];
+                }
             }
-    };
-    if constexpr (KEYS) {
-        store(acc1, p.dk + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs, p.scale);
-        store(acc2, p.dv + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs, 1.0f);
-    } else {
-        store(acc1, p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs, p.scale);
+            static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = rows_frag(at, j); });
+            static_for<0, NKK>([&](auto j) {
+                constexpr int n = decltype(j)::value;
+                if constexpr (n + PF < NKK) frag[(n + PF) % (PF + 1)] = rows_frag(at, std::integral_constant<int, n + PF>{});
+#pragma unroll
+                for (int i = 0; i < 2; ++i) dp[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], res[i][n], !KEYS && n == 0 ? zero : dp[i], 0, 0, 0);
+                step();
+            });
+        };
+        for (int t = 0; t < nt; ++t) {
+            if (t + 2 < nt) issue(t + 2);
+            if (t > 0) sums(t - 1);
+            products(t);
+            step_end(t);
+        }
+        if (nt > 0) sums(nt - 1);
+    }
+
+    // ---- results: 16 bytes a lane (the lane pair's halves of eight columns trade places)
+    const int64_t n_out = KEYS ? p.Skv : p.Sq;
+    if (KEYS || second) {
+        const int end_lane = opaque_lane(), col = (end_lane >> 5) * 8;      // formed here, not kept through the steps
+        const float factor = second ? p.scale : 1.0f;
+        __bf16* base = p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
+        if constexpr (KEYS) {
+            base = p.dv + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs;
+            if (second) base += p.dk - p.dv;                   // (a choice of one of two arguments would put both into scratch memory)
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t r = first + (end_lane & 31) + 32 * i;
+            const bool hidden = KEYS && r >= n_res;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int a = 0; a < 4; a += 2) {
+                    unsigned x[2][2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            x[j][e] = hidden ? 0u : pack_bf16(acc[i][db][4 * (a + j) + 2 * e] * factor, acc[i][db][4 * (a + j) + 2 * e + 1] * factor);
+                    const auto l = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+                    const auto u = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+                    if (r < n_out) *reinterpret_cast<u32x4*>(base + r * D + db * 32 + a * 8 + col) = u32x4{l[0], u[0], l[1], u[1]};
+                }
+        }
     }
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 1) void attn_bwd_kernel(const AttnBwdParams p) {
+__global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams p) {
     const int key_blocks = (int)((p.Skv + kBwdRows - 1) / kBwdRows), query_blocks = (int)((p.Sq + kBwdRows - 1) / kBwdRows);
     int i = (int)blockIdx.x;
     const int key_items = key_blocks * p.B * p.H;
@@ -245,7 +365,10 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
     }
     const int64_t items = ((p.Skv + kBwdRows - 1) / kBwdRows + (p.Sq + kBwdRows - 1) / kBwdRows) * BH;
     if (items > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(256), bwd_smem(D), st, p);
+    static KernelSetup setup;
+    const hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), bwd_smem(D), nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(512), bwd_smem(D), st, p);
     return hipGetLastError();
 }
 

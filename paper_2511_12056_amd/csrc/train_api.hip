@@ -74,8 +74,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     p.dv = static_cast<__bf16*>(dv);
     p.Sq = Sq; p.Skv = Skv; p.n_v = n_v;
     p.stat_rows = pda::bwd_stat_rows(Sq);
-    p.nlse2 = static_cast<float*>(workspace);
-    p.ndelta = p.nlse2 + (int64_t)B * H * p.stat_rows;
+    p.stats = static_cast<float*>(workspace);
     p.do_bs = s.dout_batch; p.do_hs = s.dout_head;
     p.q_bs = s.q_batch; p.q_hs = s.q_head;
     p.kv_bs = s.kv_batch; p.kv_hs = s.kv_head;

@@ -24,6 +24,14 @@ __device__ __forceinline__ float lane_sum(float x) {
     return x;
 }
 
+// The lane's index, formed anew where it is used: the compiler cannot trace two of them back to each other, so it keeps nothing
+// derived from it in registers in between.
+__device__ __forceinline__ int opaque_lane() {
+    int lane;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    return lane;
+}
+
 __device__ __forceinline__ float bf16_lo(unsigned x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(unsigned x) { return __uint_as_float(x & 0xffff0000u); }
 
