@@ -20,6 +20,7 @@
 namespace pda {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaitLoads = 0x0f70;      // s_waitcnt vmcnt(0), the other counters not waited for
 
 // Row-dependent XOR on the 16-byte granules of a tile's rows.  The tiles here are read both ways: 16 rows, one
 // granule each (ds_read_b128), and four consecutive rows, four granules each (transposing reads); see swz_k and swz_v for either alone.  The row's two
@@ -71,12 +72,13 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
 // ---- the products ---------------------------------------------------------------------------------------------
 constexpr int kBwdTile = 32;            // streamed rows of a step
 constexpr int kBwdRows = 256;           // resident rows of a workgroup: 64 for each of four pairs of wavefronts
-constexpr int kBwdRing = 4;             // tile buffers per streamed tensor
+constexpr int kBwdRing = 5;             // tile buffers per streamed tensor
+constexpr int kBwdAhead = 3;            // tile t + kBwdAhead is fetched in step t, into the buffer of tile t - 2
 constexpr int kBwdExchange = 64 * kBwdTile * 4;          // bytes of the probabilities of a pair and step
 constexpr int bwd_tile_bytes(int d) { return kBwdTile * d * 2; }
 constexpr int bwd_stat_base(int d) { return kBwdRing * 2 * bwd_tile_bytes(d); }
 constexpr int bwd_p_base(int d) { return bwd_stat_base(d) + kBwdRing * 256; }
-constexpr int bwd_smem(int d) { return bwd_p_base(d) + 2 * 4 * kBwdExchange; }
+constexpr int bwd_smem(int d) { return bwd_p_base(d) + 4 * kBwdExchange; }
 
 // 4 bytes per lane from global memory straight into LDS (see lds_dma16).
 __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsigned lds_addr) {
@@ -90,7 +92,7 @@ template <int D, bool KEYS>
 __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0) {
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32;
     constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2);
-    constexpr int LPI = D == 128 ? 2 : 1;                      // loads of a wavefront per step: a chunk of both tensors, or of one
+    constexpr int CPW = TILE / 4096;                           // chunks of 1 KB of a tile that a fetching wavefront brings
     constexpr int PF = 3;                                      // operand fragments read ahead
     extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
     const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))bwd_smem_;
@@ -108,62 +110,77 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
     const int64_t first = row0 + pair * 64;                    // this lane's resident rows: first + li and first + 32 + li
     const int nt = row0 < n_res ? (n_str + kBwdTile - 1) / kBwdTile : 0;
 
-    // ---- loads of the streamed tiles
-    const __bf16* s1 = KEYS ? qp : kp;
-    const __bf16* s2 = KEYS ? dop : vp;
-    auto issue = [&](int t) __attribute__((always_inline)) {
-        const int slot = t % kBwdRing;
-        const int last = n_str - 1 - t * kBwdTile;
-        const int j = D == 128 ? wave : pair, r = j * RPC + lane / G;
-        const int c = r < last ? r : last;                     // rows behind the last: that row again
-        const unsigned off = c * (D * 2) + (((lane % G) ^ swz_kv<D>(r)) * 16);
-        const unsigned to = lds0 + slot * 2 * TILE + j * 1024;
-        if (D == 128 || !second) lds_dma16(s1 + (int64_t)t * (kBwdTile * D), off, to);
-        if (D == 128 || second) lds_dma16(s2 + (int64_t)t * (kBwdTile * D), off, to + TILE);
-        if (KEYS && wave == 4) lds_dma4(stats + (int64_t)t * (2 * kBwdTile), lane * 4, lds0 + bwd_stat_base(D) + slot * 256);
-    };
-    // the end of step t: what step t + 1 needs is there, what was fetched in this step may be under way
-    auto step_end = [&](int t) __attribute__((always_inline)) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (t + 2 < nt) {
-            if (KEYS && wave == 4) wait_vmcnt<LPI + 1>();
-            else wait_vmcnt<LPI>();
-        } else {
-            wait_vmcnt<0>();
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    auto step = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+    auto barrier = [&]() __attribute__((always_inline)) {      // keeps the phases apart
+        step();
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
+        step();
     };
 
-    // ---- operand addresses in slot 0; blocks are XORed in
+    // ---- loads of the streamed tiles, by the second wavefronts: 1 KB chunks pair, pair + 4 of a tile; chunk j holds rows j RPC ..,
+    // lane -> row lane / G of them, granule lane % G.  Sixteen rows on, the lane's offset in its row is the same.
+    const __bf16* s1 = KEYS ? qp : kp;
+    const __bf16* s2 = KEYS ? dop : vp;
+    constexpr int LOADS = 2 * CPW;                             // of a wavefront per step, and in pair 0 one for the statistics
+    const unsigned whole = (pair * RPC + lane / G) * (D * 2) + (((lane % G) ^ swz_kv<D>(pair * RPC + lane / G)) * 16);
+    auto issue = [&](int t) __attribute__((always_inline)) {
+        const unsigned to = lds0 + t % kBwdRing * 2 * TILE + pair * 1024;
+        const __bf16* from1 = s1 + (int64_t)t * (kBwdTile * D);
+        const __bf16* from2 = s2 + (int64_t)t * (kBwdTile * D);
+        const int last = n_str - 1 - t * kBwdTile;
+        if (last >= kBwdTile - 1) {
+#pragma unroll
+            for (int i = 0; i < CPW; ++i) {
+                lds_dma16(from1 + i * 16 * D, whole, to + i * 4096);
+                lds_dma16(from2 + i * 16 * D, whole, to + TILE + i * 4096);
+            }
+        } else {                                               // rows behind the last: that row again
+#pragma unroll
+            for (int i = 0; i < CPW; ++i) {
+                const int l = opaque_lane(), r = (pair + 4 * i) * RPC + l / G;
+                const unsigned off = (r < last ? r : last) * (D * 2) + (((l % G) ^ swz_kv<D>(r)) * 16);
+                lds_dma16(from1, off, to + i * 4096);
+                lds_dma16(from2, off, to + TILE + i * 4096);
+            }
+        }
+        if (KEYS && pair == 0) lds_dma4(stats + (int64_t)t * (2 * kBwdTile), opaque_lane() * 4, lds0 + bwd_stat_base(D) + t % kBwdRing * 256);
+    };
+
+    // ---- operand addresses in buffer 0; blocks are XORed in
     const int t16 = lane & 15, tr_row = 4 * lh + (t16 >> 2), tr_g = 2 * (li >> 4) + ((t16 & 3) >> 1);
-    const unsigned rows_at = lds0 + li * (D * 2) + ((lh ^ swz_kv<D>(li)) * 16);
-    const unsigned tr_lo = lds0 + tr_row * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row)) * 16) + (t16 & 1) * 8;
-    const unsigned tr_hi = lds0 + (tr_row + 8) * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row + 8)) * 16) + (t16 & 1) * 8;
+    unsigned rows_at = lds0 + li * (D * 2) + ((lh ^ swz_kv<D>(li)) * 16);
+    unsigned tr_at = lds0 + tr_row * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row)) * 16) + (t16 & 1) * 8;
     auto block = [](unsigned at, auto n) __attribute__((always_inline)) {
         unsigned r = at;
         if constexpr (decltype(n)::value != 0) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(r) : "n"(decltype(n)::value), "v"(at));
         return r;
     };
-    auto rows_frag = [&](unsigned at, auto kk) __attribute__((always_inline)) {
-        return *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, decltype(kk)::value * 32>{});
+    bf16x8 frag[PF + 1];
+    auto rows_frag = [&](int t, int tensor, auto kk) __attribute__((always_inline)) {
+        const unsigned at = block(rows_at + t % kBwdRing * 2 * TILE + tensor * TILE, std::integral_constant<int, decltype(kk)::value * 32>{});
+        frag[decltype(kk)::value % (PF + 1)] = *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)at;
     };
-    auto tr_frag = [&](unsigned lo_at, unsigned hi_at, auto idx) __attribute__((always_inline)) {      // idx = u * NDB + db
+    auto tr_frag = [&](int t, int tensor, auto idx) __attribute__((always_inline)) {      // idx = u * NDB + db
         constexpr int db = decltype(idx)::value % NDB, u = decltype(idx)::value / NDB;
-        LDS_PTR(const unsigned char) x = (LDS_PTR(const unsigned char))(uintptr_t)block(lo_at, std::integral_constant<int, db * 64>{});
-        LDS_PTR(const unsigned char) y = (LDS_PTR(const unsigned char))(uintptr_t)block(hi_at, std::integral_constant<int, db * 64>{});
+        static_assert(swz_kv<D>(8) == 2 && swz_kv<D>(0) == 0, "eight rows on, the granule differs in one bit");
+        const unsigned at = tr_at + t % kBwdRing * 2 * TILE + tensor * TILE;
+        LDS_PTR(const unsigned char) x = (LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, db * 64>{});
+        LDS_PTR(const unsigned char) y = (LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, (db * 64) ^ 32>{});
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(x + u * 16 * (D * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + u * 16 * (D * 2)));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + (u * 16 + 8) * (D * 2)));
+        frag[decltype(idx)::value % (PF + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    const unsigned p_at = lds0 + bwd_p_base(D) + pair * kBwdExchange + lane * 16;
-    auto exchange = [&](int t, int i, int a) __attribute__((always_inline)) {
-        return (LDS_PTR(f32x4))(LDS_PTR(unsigned char))(uintptr_t)(p_at + (t & 1) * (4 * kBwdExchange) + (i * 4 + a) * 1024);
+    // A pair's probabilities of a step: group a of block i, 16 bytes a lane.  Statistics of a tile's rows: four rows of group a.
+    // (Addresses from a fresh lane index: they are not kept over the products.)
+    auto exchange_at = [&]() __attribute__((always_inline)) { return lds0 + bwd_p_base(D) + pair * kBwdExchange + opaque_lane() * 16; };
+    auto exchange = [](unsigned at, int i, int a) __attribute__((always_inline)) {
+        return (LDS_PTR(f32x4))(LDS_PTR(unsigned char))(uintptr_t)(at + (i * 4 + a) * 1024);
     };
-    auto stat_at = [&](int t, int which, int a) __attribute__((always_inline)) {
-        return *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(lds0 + bwd_stat_base(D) + (t % kBwdRing) * 256 + which * 128 + 32 * a + 16 * lh);
+    auto stat_at = [&](int t) __attribute__((always_inline)) { return lds0 + bwd_stat_base(D) + t % kBwdRing * 256 + (opaque_lane() >> 5) * 16; };
+    auto stat = [](unsigned at, int which, int a) __attribute__((always_inline)) {
+        return *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(at + which * 128 + 32 * a);
     };
 
     // ---- resident rows
@@ -171,8 +188,8 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
     float res_stat[2] = {0.f, 0.f};
     f32x16 acc[2][NDB];                                        // first wavefront of a pair: dV^T; second: dK^T or dQ^T
     if (nt > 0) {
-        issue(0);
-        if (nt > 1) issue(1);
+        if (second)
+            for (int t = 0; t < kBwdAhead && t < nt; ++t) issue(t);
         const __bf16* src = second ? (KEYS ? vp : dop) : (KEYS ? kp : qp);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -181,7 +198,15 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
             for (int kk = 0; kk < NKK; ++kk) res[i][kk] = *reinterpret_cast<const bf16x8*>(src + c * D + lh * 8 + kk * 16);
             if constexpr (!KEYS) res_stat[i] = stats[(c / kBwdTile) * (2 * kBwdTile) + (second ? kBwdTile : 0) + c % kBwdTile];
         }
-        wait_vmcnt<0>();
+        // The compiler's own count of loads under way starts from here: it knows this wait, and would otherwise wait inside the loops for
+        // loads of the resident rows, and so for the tiles that have just been requested.
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            asm volatile("" : "+v"(res_stat[i]));
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+v"(res[i][kk]));
+        }
         __syncthreads();
     }
 #pragma unroll
@@ -191,120 +216,156 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][db][r] = 0.f;
     const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    bf16x8 frag[PF + 1];
-    auto step = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+    f32x16 s[2];                                               // scores or <dout, v>; then p or ds, as operands in groups 0 and 2
+    // Four values (group a) as half an operand of bf16.
+    auto put = [&](int i, int a, const float (&x)[4]) __attribute__((always_inline)) {
+        s[i][a / 2 * 8 + a % 2 * 2] = __uint_as_float(pack_bf16(x[0], x[1]));
+        s[i][a / 2 * 8 + a % 2 * 2 + 1] = __uint_as_float(pack_bf16(x[2], x[3]));
+    };
+    // acc += (tile, transposed) operand: the first PF fragments are there; `next` reads those of what comes next.
+    auto nothing = [](auto) __attribute__((always_inline)) {};
+    auto sums = [&](int t, int tensor, auto next) __attribute__((always_inline)) {
+        static_for<0, 2 * NDB>([&](auto j) {
+            constexpr int n = decltype(j)::value, u = n / NDB * 8;
+            if constexpr (n + PF < 2 * NDB) tr_frag(t, tensor, std::integral_constant<int, n + PF>{});
+            else next(std::integral_constant<int, n + PF - 2 * NDB>{});
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(s[i], s[i], u, u + 1, u + 2, u + 3));
+                acc[i][n % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], x, acc[i][n % NDB], 0, 0, 0);
+            }
+            step();
+        });
+    };
+    // s = tile * resident rows; the first PF fragments are there
+    auto products = [&](int t, int tensor, auto next) __attribute__((always_inline)) {
+        static_for<0, NKK>([&](auto j) {
+            constexpr int n = decltype(j)::value;
+            if constexpr (n + PF < NKK) rows_frag(t, tensor, std::integral_constant<int, n + PF>{});
+            else next(std::integral_constant<int, n + PF - NKK>{});
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], res[i][n], n == 0 ? zero : s[i], 0, 0, 0);
+            step();
+        });
+    };
 
     if (!second) {
         const float c = p.scale_log2e;
-        for (int t = 0; t < nt; ++t) {
-            if (t + 2 < nt) issue(t + 2);
-            const unsigned slot = (t % kBwdRing) * 2 * TILE;
-            f32x16 s[2];
-            {
-                const unsigned at = rows_at + slot;
-                static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = rows_frag(at, j); });
-                static_for<0, NKK>([&](auto j) {
-                    constexpr int n = decltype(j)::value;
-                    if constexpr (n + PF < NKK) frag[(n + PF) % (PF + 1)] = rows_frag(at, std::integral_constant<int, n + PF>{});
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], res[i][n], n == 0 ? zero : s[i], 0, 0, 0);
-                    step();
-                });
-            }
-            const unsigned lo = tr_lo + slot + TILE, hi = tr_hi + slot + TILE;
-            if constexpr (KEYS) static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = tr_frag(lo, hi, j); });
-            u32x4 pk[2][2];
+        // -lse * log2 e of a step's rows, four at a time, into two fragments' registers as the last fragments go into products
+        auto read_l = [&](int t, int a) __attribute__((always_inline)) { if constexpr (KEYS) frag[a % 2] = __builtin_bit_cast(bf16x8, stat(stat_at(t), 0, a)); };
+        auto scores = [&](int t) __attribute__((always_inline)) {
+            products(t, 0, [&](auto n) __attribute__((always_inline)) { if constexpr (decltype(n)::value < 2) read_l(t, decltype(n)::value); });
+            barrier();
+        };
+        auto softmax = [&](int t) __attribute__((always_inline)) {
+            const unsigned to = exchange_at();
             const bool tail = !KEYS && (t + 1) * kBwdTile > n_str;
-            const int hidden = n_str - t * kBwdTile - 4 * lh;
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                f32x4 l;
-                if constexpr (KEYS) l = stat_at(t, 0, a);
+                const f32x4 l = __builtin_bit_cast(f32x4, frag[a % 2]);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if constexpr (!KEYS) l = f32x4{res_stat[i], res_stat[i], res_stat[i], res_stat[i]};
-                    f32x4 x;
+                    float x[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][4 * a + e], c, l[e]));
-                    if (tail)
+                    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][4 * a + e], c, KEYS ? l[e] : res_stat[i]));
+                    if (tail) {
+                        const int hidden = n_str - t * kBwdTile - (opaque_lane() >> 5) * 4;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = 8 * a + e >= hidden ? 0.f : x[e];
-                    *exchange(t, i, a) = x;
-                    if constexpr (KEYS) {
-                        pk[i][a / 2][(a % 2) * 2] = pack_bf16(x[0], x[1]);
-                        pk[i][a / 2][(a % 2) * 2 + 1] = pack_bf16(x[2], x[3]);
                     }
+                    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));      // in this order: no registers for another
+                    *exchange(to, i, a) = f32x4{x[0], x[1], x[2], x[3]};
+                    if constexpr (KEYS) put(i, a, x);
                 }
+                if (a < 2) read_l(t, a + 2);
                 step();
             }
-            if constexpr (KEYS) {
-                static_for<0, 2 * NDB>([&](auto j) {
-                    constexpr int n = decltype(j)::value;
-                    if constexpr (n + PF < 2 * NDB) frag[(n + PF) % (PF + 1)] = tr_frag(lo, hi, std::integral_constant<int, n + PF>{});
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        acc[i][n % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], __builtin_bit_cast(bf16x8, pk[i][n / NDB]), acc[i][n % NDB], 0, 0, 0);
-                    step();
-                });
-            }
-            step_end(t);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            // first fragments of what follows: dV of this step, or the scores of the next one, whose tile is there
+            if constexpr (KEYS) static_for<0, PF>([&](auto n) { tr_frag(t, 1, n); });
+            else static_for<0, PF>([&](auto n) { rows_frag(t + 1, 0, n); });
+            barrier();
+        };
+        if (nt > 0) {
+            static_for<0, PF>([&](auto n) { rows_frag(0, 0, n); });
+            scores(0);
+            softmax(0);
         }
+        for (int t = 1; t < nt; ++t) {
+            asm volatile("" : "+v"(rows_at), "+v"(tr_at));     // nothing formed from them is kept across steps
+            __builtin_amdgcn_s_setprio(1);                     // matrix instructions ahead of the other wavefront's arithmetic
+            if constexpr (KEYS) sums(t - 1, 1, [&](auto n) __attribute__((always_inline)) { rows_frag(t, 0, n); });
+            scores(t);
+            __builtin_amdgcn_s_setprio(0);
+            softmax(t);
+        }
+        if (KEYS && nt > 0) sums(nt - 1, 1, nothing);
     } else {
-        f32x16 dp[2];
-        // ds of step t - 1 (its p is there), its products, then dp of step t
-        auto sums = [&](int t) __attribute__((always_inline)) {
-            const unsigned slot = (t % kBwdRing) * 2 * TILE;
-            const unsigned lo = tr_lo + slot, hi = tr_hi + slot;
-            u32x4 ds[2][2];
-            static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = tr_frag(lo, hi, j); });
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x4 x = *exchange(t, i, a);
-                    float y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = x[e] * (KEYS ? dp[i][4 * a + e] : dp[i][4 * a + e] + res_stat[i]);
-                    ds[i][a / 2][(a % 2) * 2] = pack_bf16(y[0], y[1]);
-                    ds[i][a / 2][(a % 2) * 2 + 1] = pack_bf16(y[2], y[3]);
+        // ds from the probabilities that the other wavefront has left there.  They and -delta, four values of each at a time, are read into the
+        // registers of the fragments, which follow them, and one more.
+        auto differences = [&](int t) __attribute__((always_inline)) {
+            const unsigned p_at = exchange_at(), d_at = KEYS ? stat_at(t) : 0;
+            f32x4 odd = {0.f, 0.f, 0.f, 0.f};
+            auto read_p = [&](int n) __attribute__((always_inline)) { frag[n % 3] = __builtin_bit_cast(bf16x8, *exchange(p_at, n % 2, n / 2)); };
+            auto read_d = [&](int a) __attribute__((always_inline)) {
+                if constexpr (KEYS) {
+                    if (a % 2) odd = stat(d_at, 1, a);
+                    else frag[3] = __builtin_bit_cast(bf16x8, stat(d_at, 1, a));
                 }
-            }
+            };
+            read_d(0);
+            read_p(0);
+            read_p(1);
+            read_d(1);
+            read_p(2);
             step();
-            static_for<0, 2 * NDB>([&](auto j) {
-                constexpr int n = decltype(j)::value;
-                if constexpr (n + PF < 2 * NDB) frag[(n + PF) % (PF + 1)] = tr_frag(lo, hi, std::integral_constant<int, n + PF>{});
+            static_for<0, 8>([&](auto j) {
+                constexpr int n = decltype(j)::value, a = n / 2, i = n % 2;
+                const f32x4 x = __builtin_bit_cast(f32x4, frag[n % 3]), d = a % 2 ? odd : __builtin_bit_cast(f32x4, frag[3]);
+                float y[4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    acc[i][n % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], __builtin_bit_cast(bf16x8, ds[i][n / NDB]), acc[i][n % NDB], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) y[e] = x[e] * (s[i][4 * a + e] + (KEYS ? d[e] : res_stat[i]));
+                asm volatile("" : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));      // in this order: no registers for another
+                put(i, a, y);
+                if constexpr (n + 3 < 8) read_p(n + 3);
+                else tr_frag(t, 0, std::integral_constant<int, n % 3>{});
+                if constexpr (n % 2 == 1 && a < 2) read_d(a + 2);
                 step();
             });
         };
-        auto products = [&](int t) __attribute__((always_inline)) {
-            const unsigned at = rows_at + (t % kBwdRing) * 2 * TILE + TILE;
-            if constexpr (KEYS) {
-#pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const f32x4 x = stat_at(t, 1, a);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dp[0][4 * a + e] = dp[1][4 * a + e] = x[e];
-                }
+        // the end of step t: tile t + 2 is there, tile t + 3 may be under way
+        auto step_end = [&](int t) __attribute__((always_inline)) {
+            step();
+            if (t + kBwdAhead < nt) {
+                if (KEYS && pair == 0) wait_vmcnt<LOADS + 1>();
+                else wait_vmcnt<LOADS>();
+            } else {
+                wait_vmcnt<0>();
             }
-            static_for<0, PF>([&](auto j) { frag[decltype(j)::value] = rows_frag(at, j); });
-            static_for<0, NKK>([&](auto j) {
-                constexpr int n = decltype(j)::value;
-                if constexpr (n + PF < NKK) frag[(n + PF) % (PF + 1)] = rows_frag(at, std::integral_constant<int, n + PF>{});
-#pragma unroll
-                for (int i = 0; i < 2; ++i) dp[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % (PF + 1)], res[i][n], !KEYS && n == 0 ? zero : dp[i], 0, 0, 0);
-                step();
-            });
+            barrier();
         };
-        for (int t = 0; t < nt; ++t) {
-            if (t + 2 < nt) issue(t + 2);
-            if (t > 0) sums(t - 1);
-            products(t);
+        if (nt > 0) {
+            if (nt > kBwdAhead) issue(kBwdAhead);
+            static_for<0, PF>([&](auto n) { rows_frag(0, 1, n); });
+            barrier();
+            products(0, 1, nothing);
+            step_end(0);
+        }
+        for (int t = 1; t < nt; ++t) {
+            asm volatile("" : "+v"(rows_at), "+v"(tr_at));
+            if (t + kBwdAhead < nt) issue(t + kBwdAhead);
+            differences(t - 1);
+            barrier();
+            __builtin_amdgcn_s_setprio(1);
+            sums(t - 1, 0, [&](auto n) __attribute__((always_inline)) { rows_frag(t, 1, n); });
+            products(t, 1, nothing);
+            __builtin_amdgcn_s_setprio(0);
             step_end(t);
         }
-        if (nt > 0) sums(nt - 1);
+        if (nt > 0) {
+            differences(nt - 1);
+            sums(nt - 1, 0, nothing);
+        }
     }
 
     // ---- results: 16 bytes a lane (the lane pair's halves of eight columns trade places)
