@@ -260,26 +260,29 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
         auto softmax = [&](int t) __attribute__((always_inline)) {
             const unsigned to = exchange_at();
             const bool tail = !KEYS && (t + 1) * kBwdTile > n_str;
+            // Eight groups of four values in place, each written and packed while the next one's exponentials are under way.
+            static_for<0, 9>([&](auto j) {
+                constexpr int n = decltype(j)::value;
+                if constexpr (n < 8) {
+                    constexpr int a = n / 2, i = n % 2;
+                    const f32x4 l = __builtin_bit_cast(f32x4, frag[a % 2]);
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const f32x4 l = __builtin_bit_cast(f32x4, frag[a % 2]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float x[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][4 * a + e], c, KEYS ? l[e] : res_stat[i]));
+                    for (int e = 0; e < 4; ++e) s[i][4 * a + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][4 * a + e], c, KEYS ? l[e] : res_stat[i]));
                     if (tail) {
                         const int hidden = n_str - t * kBwdTile - (opaque_lane() >> 5) * 4;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = 8 * a + e >= hidden ? 0.f : x[e];
+                        for (int e = 0; e < 4; ++e) s[i][4 * a + e] = 8 * a + e >= hidden ? 0.f : s[i][4 * a + e];
                     }
-                    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));      // in this order: no registers for another
+                    if constexpr (i == 1 && a < 2) read_l(t, a + 2);
+                }
+                if constexpr (n > 0) {
+                    constexpr int a = (n - 1) / 2, i = (n - 1) % 2;
+                    const float x[4] = {s[i][4 * a], s[i][4 * a + 1], s[i][4 * a + 2], s[i][4 * a + 3]};
                     *exchange(to, i, a) = f32x4{x[0], x[1], x[2], x[3]};
                     if constexpr (KEYS) put(i, a, x);
                 }
-                if (a < 2) read_l(t, a + 2);
                 step();
-            }
+            });
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             // first fragments of what follows: dV of this step, or the scores of the next one, whose tile is there
             if constexpr (KEYS) static_for<0, PF>([&](auto n) { tr_frag(t, 1, n); });
