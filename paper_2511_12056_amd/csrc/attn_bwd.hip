@@ -70,8 +70,6 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
 }
 
 // ---- the products ---------------------------------------------------------------------------------------------
-constexpr int kBwdTile = 32;            // streamed rows of a step
-constexpr int kBwdRows = 256;           // resident rows of a workgroup: 64 for each of four pairs of wavefronts
 constexpr int kBwdRing = 5;             // tile buffers per streamed tensor
 constexpr int kBwdAhead = 3;            // tile t + kBwdAhead is fetched in step t, into the buffer of tile t - 2
 constexpr int kBwdExchange = 64 * kBwdTile * 4;          // bytes of the probabilities of a pair and step
@@ -88,8 +86,33 @@ __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsig
                  : "memory", "m0", "vcc");
 }
 
+// Results of 32 resident rows from f(db, e), element e of the accumulator of columns 32 db ..: 16 bytes a lane (the lane pair's halves of
+// eight columns trade places).  Rows from n_live on get zeros, rows from n_out on are not written.
+template <int D, typename F>
+__device__ __forceinline__ void store_rows(__bf16* base, int64_t first, int64_t n_live, int64_t n_out, float factor, F&& f) {
+    const int lane = opaque_lane(), col = (lane >> 5) * 8;     // formed here, not kept through the steps
+    const int64_t r = first + (lane & 31);
+    const bool hidden = r >= n_live;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int a = 0; a < 4; a += 2) {
+            unsigned x[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    x[j][e] = hidden ? 0u : pack_bf16(f(db, 4 * (a + j) + 2 * e) * factor, f(db, 4 * (a + j) + 2 * e + 1) * factor);
+            const auto l = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+            const auto u = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+            if (r < n_out) *reinterpret_cast<u32x4*>(base + r * D + db * 32 + a * 8 + col) = u32x4{l[0], u[0], l[1], u[1]};
+        }
+}
+
+// One block of resident rows against the streamed tiles [t0, t1).  part: where the sums go in fp32 if other work items have the
+// block's other tiles (dQ, or dK and behind it dV: kBwdRows * D floats each, in the order of the accumulator registers), else null.
 template <int D, bool KEYS>
-__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0) {
+__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32;
     constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2);
     constexpr int CPW = TILE / 4096;                           // chunks of 1 KB of a tile that a fetching wavefront brings
@@ -104,11 +127,12 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
     const __bf16* dop = p.dout + (int64_t)b * p.do_bs + (int64_t)h * p.do_hs;
     const __bf16* kp = p.k + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
     const __bf16* vp = p.v + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
-    const float* stats = p.stats + bh * p.stat_rows * 2;
+    const float* stats = p.stats + bh * p.stat_rows * 2 + (KEYS ? (int64_t)t0 * (2 * kBwdTile) : 0);
     const int64_t n_res = KEYS ? p.n_v : p.Sq;
-    const int n_str = (int)(KEYS ? p.Sq : p.n_v);
+    const int n_all = (int)(KEYS ? p.Sq : p.n_v);
+    const int n_str = (n_all < (int64_t)t1 * kBwdTile ? n_all : t1 * kBwdTile) - t0 * kBwdTile;        // streamed rows, counted from tile t0 on
     const int64_t first = row0 + pair * 64;                    // this lane's resident rows: first + li and first + 32 + li
-    const int nt = row0 < n_res ? (n_str + kBwdTile - 1) / kBwdTile : 0;
+    const int nt = row0 < n_res ? t1 - t0 : 0;
 
     auto step = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
     auto barrier = [&]() __attribute__((always_inline)) {      // keeps the phases apart
@@ -121,8 +145,8 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
 
     // ---- loads of the streamed tiles, by the second wavefronts: 1 KB chunks pair, pair + 4 of a tile; chunk j holds rows j RPC ..,
     // lane -> row lane / G of them, granule lane % G.  Sixteen rows on, the lane's offset in its row is the same.
-    const __bf16* s1 = KEYS ? qp : kp;
-    const __bf16* s2 = KEYS ? dop : vp;
+    const __bf16* s1 = (KEYS ? qp : kp) + (int64_t)t0 * (kBwdTile * D);
+    const __bf16* s2 = (KEYS ? dop : vp) + (int64_t)t0 * (kBwdTile * D);
     constexpr int LOADS = 2 * CPW;                             // of a wavefront per step, and in pair 0 one for the statistics
     const unsigned whole = (pair * RPC + lane / G) * (D * 2) + (((lane % G) ^ swz_kv<D>(pair * RPC + lane / G)) * 16);
     auto issue = [&](int t) __attribute__((always_inline)) {
@@ -371,49 +395,108 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
         }
     }
 
-    // ---- results: 16 bytes a lane (the lane pair's halves of eight columns trade places)
-    const int64_t n_out = KEYS ? p.Skv : p.Sq;
-    if (KEYS || second) {
-        const int end_lane = opaque_lane(), col = (end_lane >> 5) * 8;      // formed here, not kept through the steps
-        const float factor = second ? p.scale : 1.0f;
-        __bf16* base = p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
-        if constexpr (KEYS) {
-            base = p.dv + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs;
-            if (second) base += p.dk - p.dv;                   // (a choice of one of two arguments would put both into scratch memory)
-        }
+    // ---- results
+    if (!KEYS && !second) return;
+    if (part) {
+        f32x4* to = reinterpret_cast<f32x4*>(part + (KEYS && !second ? kBwdRows * D : 0)) + pair * (2 * NDB * 4 * 64) + opaque_lane();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t r = first + (end_lane & 31) + 32 * i;
-            const bool hidden = KEYS && r >= n_res;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
-                for (int a = 0; a < 4; a += 2) {
-                    unsigned x[2][2];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            x[j][e] = hidden ? 0u : pack_bf16(acc[i][db][4 * (a + j) + 2 * e] * factor, acc[i][db][4 * (a + j) + 2 * e + 1] * factor);
-                    const auto l = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
-                    const auto u = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
-                    if (r < n_out) *reinterpret_cast<u32x4*>(base + r * D + db * 32 + a * 8 + col) = u32x4{l[0], u[0], l[1], u[1]};
-                }
-        }
+                for (int a = 0; a < 4; ++a)
+                    to[((i * NDB + db) * 4 + a) * 64] = f32x4{acc[i][db][4 * a], acc[i][db][4 * a + 1], acc[i][db][4 * a + 2], acc[i][db][4 * a + 3]};
+        return;
     }
+    __bf16* base = p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
+    if constexpr (KEYS) {
+        base = p.dv + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs;
+        if (second) base += p.dk - p.dv;                       // (a choice of one of two arguments would put both into scratch memory)
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        store_rows<D>(base, first + 32 * i, n_res, KEYS ? p.Skv : p.Sq, second ? p.scale : 1.0f, [&](int db, int e) __attribute__((always_inline)) { return acc[i][db][e]; });
 }
 
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams p) {
-    const int key_blocks = (int)((p.Skv + kBwdRows - 1) / kBwdRows), query_blocks = (int)((p.Sq + kBwdRows - 1) / kBwdRows);
+    const BwdPlan& w = p.plan;
     int i = (int)blockIdx.x;
-    const int key_items = key_blocks * p.B * p.H;
-    if (i < key_items) {
-        attn_bwd_item<D, true>(p, i / key_blocks, (int64_t)(i % key_blocks) * kBwdRows);
-    } else {
-        i -= key_items;
-        attn_bwd_item<D, false>(p, i / query_blocks, (int64_t)(i % query_blocks) * kBwdRows);
+    const int nk = w.key_blocks * w.key_parts;
+    if (i < nk) {
+        const int j = i / w.key_blocks, blk = i - j * w.key_blocks, bh = blk / w.key_per_head;
+        const int nt = (int)((p.Sq + kBwdTile - 1) / kBwdTile);
+        attn_bwd_item<D, true>(p, bh, (int64_t)(blk - bh * w.key_per_head) * kBwdRows, (int)((int64_t)nt * j / w.key_parts), (int)((int64_t)nt * (j + 1) / w.key_parts),
+                               w.key_parts > 1 ? p.parts + (int64_t)(blk * w.key_parts + j) * (2 * kBwdRows * D) : nullptr);
+        return;
     }
+    i -= nk;
+    const int whole = w.query_blocks - w.query_cut, nq = whole + w.query_cut * w.query_parts;
+    if (i < nq) {
+        const int j = i < whole ? 0 : (i - whole) / w.query_cut, c = i - whole - j * w.query_cut;      // part j of cut block c
+        const int blk = i < whole ? i : whole + c, bh = blk / w.query_per_head, parts = i < whole ? 1 : w.query_parts;
+        const int nt = (int)((p.n_v + kBwdTile - 1) / kBwdTile);
+        attn_bwd_item<D, false>(p, bh, (int64_t)(blk - bh * w.query_per_head) * kBwdRows, (int)((int64_t)nt * j / parts), (int)((int64_t)nt * (j + 1) / parts),
+                                i < whole ? nullptr : p.parts + bwd_key_floats(w, D) + (int64_t)(c * w.query_parts + j) * (kBwdRows * D));
+        return;
+    }
+    // keys that nobody sees: zeros from the first row behind the last block of valid ones
+    i -= nq;
+    const int64_t from = (int64_t)w.key_per_head * kBwdRows, rows = p.Skv - from;
+    const int per_head = (int)((rows + kBwdRows - 1) / kBwdRows), bh = i / per_head, b = bh / p.H, h = bh - b * p.H;
+    const int64_t first = from + (int64_t)(i - bh * per_head) * kBwdRows, at = (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs + first * D;
+    const int n = (int)(p.Skv - first < kBwdRows ? p.Skv - first : kBwdRows) * (D / 8);
+    for (int x = threadIdx.x; x < n; x += 512) {
+        reinterpret_cast<u32x4*>(p.dk + at)[x] = u32x4{0, 0, 0, 0};
+        reinterpret_cast<u32x4*>(p.dv + at)[x] = u32x4{0, 0, 0, 0};
+    }
+}
+
+// Sums of the parts of cut blocks, part after part: a wavefront for 32 rows of dq, dk or dv.
+template <int D>
+__global__ __launch_bounds__(256) void attn_bwd_join_kernel(const AttnBwdParams p) {
+    constexpr int NDB = D / 32;
+    const BwdPlan& w = p.plan;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), sub = (blockIdx.x & 1) * 4 + wave;       // 32 of the 256 rows
+    int i = (int)blockIdx.x >> 1;
+    const int nk = w.key_parts > 1 ? w.key_blocks * 2 : 0;
+    const bool keys = i < nk;
+    const float* src;
+    int blk, parts;
+    int64_t stride;
+    bool is_dv = false;
+    if (keys) {
+        blk = i >> 1;
+        is_dv = i & 1;
+        parts = w.key_parts;
+        stride = 2 * kBwdRows * D;
+        src = p.parts + (int64_t)blk * parts * stride + (is_dv ? kBwdRows * D : 0);
+    } else {
+        i -= nk;
+        blk = w.query_blocks - w.query_cut + i;
+        parts = w.query_parts;
+        stride = kBwdRows * D;
+        src = p.parts + bwd_key_floats(w, D) + (int64_t)i * parts * stride;
+    }
+    const int per_head = keys ? w.key_per_head : w.query_per_head, bh = blk / per_head, b = bh / p.H, h = bh - b * p.H;
+    const int64_t first = (int64_t)(blk - bh * per_head) * kBwdRows + sub * 32;
+    const int64_t n_live = keys ? p.n_v : p.Sq, n_out = keys ? p.Skv : p.Sq;
+    if (first >= n_out) return;
+    const f32x4* from = reinterpret_cast<const f32x4*>(src) + sub * (NDB * 4 * 64) + (threadIdx.x & 63);
+    f32x4 acc[NDB * 4];
+#pragma unroll
+    for (int x = 0; x < NDB * 4; ++x) acc[x] = from[x * 64];
+    for (int j = 1; j < parts; ++j) {
+        from += stride / 4;
+#pragma unroll
+        for (int x = 0; x < NDB * 4; ++x) acc[x] += from[x * 64];
+    }
+    __bf16* base = p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
+    if (keys) {
+        base = p.dk + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs;
+        if (is_dv) base += p.dv - p.dk;
+    }
+    store_rows<D>(base, first, n_live, n_out, is_dv ? 1.0f : p.scale, [&](int db, int e) __attribute__((always_inline)) { return acc[db * 4 + e / 4][e % 4]; });
 }
 
 template <int D>
@@ -427,12 +510,18 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int64_t items = ((p.Skv + kBwdRows - 1) / kBwdRows + (p.Sq + kBwdRows - 1) / kBwdRows) * BH;
+    const BwdPlan& w = p.plan;
+    const int64_t hidden = p.Skv > (int64_t)w.key_per_head * kBwdRows ? (p.Skv - (int64_t)w.key_per_head * kBwdRows + kBwdRows - 1) / kBwdRows * BH : 0;
+    const int64_t items = (int64_t)w.key_blocks * w.key_parts + w.query_blocks + (int64_t)w.query_cut * (w.query_parts - 1) + hidden;
     if (items > 0x7fffffff) return hipErrorInvalidValue;
     static KernelSetup setup;
-    const hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), bwd_smem(D), nullptr);
+    hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), bwd_smem(D), nullptr);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(512), bwd_smem(D), st, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t joins = (w.key_parts > 1 ? (int64_t)w.key_blocks * 2 : 0) + w.query_cut;
+    if (joins == 0) return hipSuccess;
+    hipLaunchKernelGGL(attn_bwd_join_kernel<D>, dim3((unsigned)(joins * 2)), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 

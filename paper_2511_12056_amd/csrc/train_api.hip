@@ -57,12 +57,16 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
         for (int j = 0; j < i; ++j)
             if (overlap(res[i].p, n, res[j].p, compact ? res[j].bytes : (res[j].bytes > 0 ? 1 : 0))) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", res[i].name, res[j].name);
     }
-    int64_t need = 0;
-    if ((rc = pda_attn_bwd_workspace(B, H, Sq, Skv, d, n_v, 0, &need)) != PDA_OK) return rc;
-    if (need > 0 && (!workspace || workspace_bytes < need))
-        return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", workspace ? (long long)workspace_bytes : 0LL, (long long)need);
-    if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
     pda::AttnBwdParams p{};
+    const int64_t stat_bytes = pda::bwd_stat_bytes((int64_t)B * H, Sq), given = workspace ? workspace_bytes : 0;
+    if (given < stat_bytes) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, at least %lld needed", (long long)given, (long long)stat_bytes);
+    if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
+    int n_cu = 0;
+    hipError_t e = pda::device_cu_count(&n_cu);
+    if (e != hipSuccess) return hip_error(e, "device query");
+    p.plan = pda::plan_bwd(Sq, n_v, (int64_t)B * H, n_cu);
+    const int64_t need = pda::bwd_workspace_bytes(p.plan, (int64_t)B * H, Sq, d);
+    if (given < need) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)given, (long long)need);
     p.dout = static_cast<const __bf16*>(dout);
     p.q = static_cast<const __bf16*>(q);
     p.k = static_cast<const __bf16*>(k);
@@ -75,6 +79,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     p.Sq = Sq; p.Skv = Skv; p.n_v = n_v;
     p.stat_rows = pda::bwd_stat_rows(Sq);
     p.stats = static_cast<float*>(workspace);
+    p.parts = p.stats + stat_bytes / 4;
     p.do_bs = s.dout_batch; p.do_hs = s.dout_head;
     p.q_bs = s.q_batch; p.q_hs = s.q_head;
     p.kv_bs = s.kv_batch; p.kv_hs = s.kv_head;
@@ -86,7 +91,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     p.out_bf16 = out_type == PDA_BF16 ? 1 : 0;
     p.scale = scale;
     p.scale_log2e = (float)((double)scale * 1.4426950408889634);     // exactly 1 for scale = (float)ln 2
-    const hipError_t e = pda::launch_attn_bwd(p, d, static_cast<hipStream_t>(stream));
+    e = pda::launch_attn_bwd(p, d, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? (int)PDA_OK : hip_error(e, "attention gradient launch");
 }
 
@@ -120,7 +125,15 @@ int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t
     if (rc != PDA_OK) return rc;
     if (n_cu < 0) return report(PDA_ERR_INVALID_ARG, "n_cu=%d is negative", n_cu);
     if (!bytes) return report(PDA_ERR_INVALID_ARG, "null bytes");
-    *bytes = pda::bwd_workspace_bytes((int64_t)B * H, Sq);
+    if (B == 0 || H == 0) {
+        *bytes = 0;
+        return PDA_OK;
+    }
+    if (n_cu == 0) {
+        const hipError_t e = pda::device_cu_count(&n_cu);
+        if (e != hipSuccess) return hip_error(e, "device query");
+    }
+    *bytes = pda::bwd_workspace_bytes(pda::plan_bwd(Sq, kv_valid_len, (int64_t)B * H, n_cu), (int64_t)B * H, Sq, d);
     return PDA_OK;
 }
 

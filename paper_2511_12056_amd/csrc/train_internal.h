@@ -9,6 +9,107 @@ namespace pda {
 int report(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
 // ---- attention, backward (attn_bwd.hip) ---------------------------------------------------------
+constexpr int kBwdTile = 32;            // streamed rows of a step
+constexpr int kBwdRows = 256;           // resident rows of a workgroup
+
+// The work items of a launch, in the order in which they start: the blocks of 256 valid keys (dk and dv; a step is four products), each
+// against `key_parts` ranges of the query rows; the blocks of 256 query rows (dq; three products), the last `query_cut` of them each
+// against `query_parts` ranges of the keys; blocks of hidden keys only (zeros).
+struct BwdPlan {
+    int key_per_head, query_per_head;   // blocks
+    int key_blocks, query_blocks;       // of all heads
+    int key_parts;                      // 1: none is cut
+    int query_cut, query_parts;         // 0, 1: none is cut
+};
+constexpr int kBwdMaxParts = 16;
+// Steps of a block against n streamed rows.
+inline int64_t bwd_steps(int64_t n) { return (n + kBwdTile - 1) / kBwdTile; }
+// Time of an item in tenths of a query step (1 us at d = 128): a key step takes 1.2 of it, start and end of an item about six.
+inline int64_t bwd_key_time(int64_t steps) { return steps * 12 + 60; }
+inline int64_t bwd_query_time(int64_t steps) { return steps * 10 + 60; }
+// Partial sums of kBwdRows rows that a plan writes and a second kernel adds: half of such a unit each, and that kernel's launch.
+inline int64_t bwd_part_slots(const BwdPlan& w) { return (w.key_parts > 1 ? (int64_t)w.key_blocks * w.key_parts * 2 : 0) + (int64_t)w.query_cut * (w.query_cut ? w.query_parts : 0); }
+inline int64_t bwd_join_time(const BwdPlan& w) { const int64_t n = bwd_part_slots(w); return n ? 50 + n / 2 : 0; }
+// When the last item of a launch ends if each goes, in order, to the compute unit that is free first.
+inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
+    struct Free { int64_t at, units; } f[8] = {{0, n_cu}};     // compute units by the time at which they become free
+    int groups = 1;
+    const int64_t sk = bwd_steps(Sq), sq = bwd_steps(n_v);
+    const struct { int64_t n, time; } jobs[3] = {{(int64_t)w.key_blocks * w.key_parts, bwd_key_time((sk + w.key_parts - 1) / w.key_parts)},
+                                                 {w.query_blocks - w.query_cut, bwd_query_time(sq)},
+                                                 {(int64_t)w.query_cut * w.query_parts, bwd_query_time((sq + w.query_parts - 1) / w.query_parts)}};
+    int64_t end = 0;
+    for (const auto& j : jobs) {
+        for (int64_t left = j.n; left > 0;) {
+            int g = 0;
+            for (int i = 1; i < groups; ++i)
+                if (f[i].at < f[g].at) g = i;
+            const int64_t n = f[g].units < left ? f[g].units : left, at = f[g].at + j.time;
+            left -= n;
+            if (at > end) end = at;
+            int same = 0;
+            while (same < groups && f[same].at != at) ++same;
+            if (n == f[g].units && same == groups) f[g].at = at;               // all of them
+            else {
+                f[g].units -= n;
+                if (same < groups) f[same].units += n;
+                else f[groups++] = {at, n};
+                if (f[g].units == 0) f[g] = f[--groups];
+            }
+        }
+    }
+    return end;
+}
+// Cuts.  A launch of fewer blocks than compute units is cut so that its parts fill them in one round, key and query blocks into parts of
+// about equal time; one of more blocks has the blocks that start last cut where that ends it earlier, and its key blocks, which start
+// first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel.
+// us, uncut -> cut: see attn_bwd.hip.
+inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int n_cu) {
+    BwdPlan w{};
+    w.key_per_head = (int)((n_v + kBwdRows - 1) / kBwdRows);
+    w.query_per_head = (int)((Sq + kBwdRows - 1) / kBwdRows);
+    w.key_blocks = (int)(BH * w.key_per_head);
+    w.query_blocks = (int)(BH * w.query_per_head);
+    w.key_parts = w.query_parts = 1;
+    const int64_t sk = bwd_steps(Sq), sq = bwd_steps(n_v), blocks = (int64_t)w.key_blocks + w.query_blocks;
+    if (w.key_blocks == 0 || w.query_blocks == 0) return w;
+    const int max_k = (int)(sk / 2 < kBwdMaxParts ? sk / 2 : kBwdMaxParts), max_q = (int)(sq / 2 < kBwdMaxParts ? sq / 2 : kBwdMaxParts);
+    BwdPlan best = w;
+    int64_t best_time = bwd_end(w, Sq, n_v, n_cu);
+    auto consider = [&](int key_parts, int query_cut, int query_parts) {
+        BwdPlan c = w;
+        c.key_parts = key_parts;
+        if (query_parts > 1) {
+            c.query_cut = query_cut;
+            c.query_parts = query_parts;
+        }
+        if (bwd_part_slots(c) > 4 * (int64_t)n_cu) return;
+        const int64_t t = bwd_end(c, Sq, n_v, n_cu) + bwd_join_time(c);
+        if (t < best_time) {
+            best = c;
+            best_time = t;
+        }
+    };
+    if (blocks <= n_cu) {
+        for (int k = 1; k <= max_k && w.key_blocks * k + w.query_blocks <= n_cu; ++k) {
+            const int64_t q = (n_cu - (int64_t)w.key_blocks * k) / w.query_blocks;
+            consider(k, w.query_blocks, (int)(q < max_q ? q : max_q));
+        }
+        return best;
+    }
+    if (blocks > 64 * (int64_t)n_cu) return w;                 // nothing to gain at the end of so long a launch
+    for (int k = 1; k <= max_k && (k == 1 || (int64_t)w.key_blocks * k <= 2 * (int64_t)n_cu); ++k) {
+        if (k > 1) consider(k, 0, 1);
+        for (int r = 1; r <= 4; ++r) {
+            const int64_t cut = r * (int64_t)n_cu / 4;
+            for (int q = 2; q <= 4 && q <= max_q; ++q) consider(k, (int)(cut < w.query_blocks ? cut : w.query_blocks), q);
+            if (cut >= w.query_blocks) break;
+        }
+    }
+    return best;
+}
+__host__ __device__ inline int64_t bwd_key_floats(const BwdPlan& w, int d) { return w.key_parts > 1 ? (int64_t)w.key_blocks * w.key_parts * 2 * kBwdRows * d : 0; }
+
 struct AttnBwdParams {
     const __bf16* dout;
     const __bf16* q;
@@ -27,9 +128,12 @@ struct AttnBwdParams {
     int B, H;
     int out_bf16;
     float scale, scale_log2e;
+    float* parts;            // partial sums of cut blocks: the key blocks' (dk, dv of a part, part after part, block after block), the query blocks'
+    BwdPlan plan;
 };
 inline int64_t bwd_stat_rows(int64_t Sq) { return (Sq + 63) / 64 * 64; }
-inline int64_t bwd_workspace_bytes(int64_t BH, int64_t Sq) { return (BH * bwd_stat_rows(Sq) * 8 + 255) / 256 * 256; }
+inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq) { return (BH * bwd_stat_rows(Sq) * 8 + 255) / 256 * 256; }
+inline int64_t bwd_workspace_bytes(const BwdPlan& w, int64_t BH, int64_t Sq, int d) { return bwd_stat_bytes(BH, Sq) + bwd_part_slots(w) * kBwdRows * d * 4; }
 hipError_t launch_attn_bwd(const AttnBwdParams& p, int d, hipStream_t st);
 
 // ---- layer norm (layer_norm.hip) ----------------------------------------------------------------
