@@ -86,15 +86,15 @@ __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsig
                  : "memory", "m0", "vcc");
 }
 
-// Results of 32 resident rows from f(db, e), element e of the accumulator of columns 32 db ..: 16 bytes a lane (the lane pair's halves of
+// Results of 32 resident rows and NDB blocks of 32 columns from f(db, e), element e of the accumulator of block db: 16 bytes a lane (the lane pair's halves of
 // eight columns trade places).  Rows from n_live on get zeros, rows from n_out on are not written.
-template <int D, typename F>
+template <int D, int NDB, typename F>
 __device__ __forceinline__ void store_rows(__bf16* base, int64_t first, int64_t n_live, int64_t n_out, float factor, F&& f) {
     const int lane = opaque_lane(), col = (lane >> 5) * 8;     // formed here, not kept through the steps
     const int64_t r = first + (lane & 31);
     const bool hidden = r >= n_live;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+    for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int a = 0; a < 4; a += 2) {
             unsigned x[2][2];
@@ -415,7 +415,7 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        store_rows<D>(base, first + 32 * i, n_res, KEYS ? p.Skv : p.Sq, second ? p.scale : 1.0f, [&](int db, int e) __attribute__((always_inline)) { return acc[i][db][e]; });
+        store_rows<D, NDB>(base, first + 32 * i, n_res, KEYS ? p.Skv : p.Sq, second ? p.scale : 1.0f, [&](int db, int e) __attribute__((always_inline)) { return acc[i][db][e]; });
 }
 
 template <int D>
@@ -452,13 +452,14 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams p)
     }
 }
 
-// Sums of the parts of cut blocks, part after part: a wavefront for 32 rows of dq, dk or dv.
+// Sums of the parts of cut blocks, part after part: a wavefront for 32 rows and 32 columns of dq, dk or dv, a workgroup for 128 rows.
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_join_kernel(const AttnBwdParams p) {
     constexpr int NDB = D / 32;
     const BwdPlan& w = p.plan;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), sub = (blockIdx.x & 1) * 4 + wave;       // 32 of the 256 rows
-    int i = (int)blockIdx.x >> 1;
+    const int db = blockIdx.x % NDB;
+    const int sub = (blockIdx.x / NDB & 1) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);       // 32 of the 256 rows
+    int i = (int)blockIdx.x / (2 * NDB);
     const int nk = w.key_parts > 1 ? w.key_blocks * 2 : 0;
     const bool keys = i < nk;
     const float* src;
@@ -482,21 +483,27 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(const AttnBwdParams 
     const int64_t first = (int64_t)(blk - bh * per_head) * kBwdRows + sub * 32;
     const int64_t n_live = keys ? p.n_v : p.Sq, n_out = keys ? p.Skv : p.Sq;
     if (first >= n_out) return;
-    const f32x4* from = reinterpret_cast<const f32x4*>(src) + sub * (NDB * 4 * 64) + (threadIdx.x & 63);
-    f32x4 acc[NDB * 4];
+    const f32x4* from = reinterpret_cast<const f32x4*>(src) + (sub * NDB + db) * (4 * 64) + (threadIdx.x & 63);
+    f32x4 acc[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int j = 0; j < parts; j += 4) {                       // loads of four parts in flight together
+        f32x4 x[4][4];
 #pragma unroll
-    for (int x = 0; x < NDB * 4; ++x) acc[x] = from[x * 64];
-    for (int j = 1; j < parts; ++j) {
-        from += stride / 4;
+        for (int k = 0; k < 4; ++k)
+            if (j + k < parts)
 #pragma unroll
-        for (int x = 0; x < NDB * 4; ++x) acc[x] += from[x * 64];
+                for (int a = 0; a < 4; ++a) x[k][a] = from[(j + k) * (stride / 4) + a * 64];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (j + k < parts)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) acc[a] += x[k][a];
     }
     __bf16* base = p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
     if (keys) {
         base = p.dk + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs;
         if (is_dv) base += p.dv - p.dk;
     }
-    store_rows<D>(base, first, n_live, n_out, is_dv ? 1.0f : p.scale, [&](int db, int e) __attribute__((always_inline)) { return acc[db * 4 + e / 4][e % 4]; });
+    store_rows<D, 1>(base + db * 32, first, n_live, n_out, is_dv ? 1.0f : p.scale, [&](int, int e) __attribute__((always_inline)) { return acc[e / 4][e % 4]; });
 }
 
 template <int D>
@@ -521,7 +528,7 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t joins = (w.key_parts > 1 ? (int64_t)w.key_blocks * 2 : 0) + w.query_cut;
     if (joins == 0) return hipSuccess;
-    hipLaunchKernelGGL(attn_bwd_join_kernel<D>, dim3((unsigned)(joins * 2)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL(attn_bwd_join_kernel<D>, dim3((unsigned)(joins * (2 * (D / 32)))), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 

@@ -64,7 +64,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     int n_cu = 0;
     hipError_t e = pda::device_cu_count(&n_cu);
     if (e != hipSuccess) return hip_error(e, "device query");
-    p.plan = pda::plan_bwd(Sq, n_v, (int64_t)B * H, n_cu);
+    p.plan = pda::plan_bwd(Sq, n_v, (int64_t)B * H, d, n_cu);
     const int64_t need = pda::bwd_workspace_bytes(p.plan, (int64_t)B * H, Sq, d);
     if (given < need) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)given, (long long)need);
     p.dout = static_cast<const __bf16*>(dout);
@@ -133,7 +133,7 @@ int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t
         const hipError_t e = pda::device_cu_count(&n_cu);
         if (e != hipSuccess) return hip_error(e, "device query");
     }
-    *bytes = pda::bwd_workspace_bytes(pda::plan_bwd(Sq, kv_valid_len, (int64_t)B * H, n_cu), (int64_t)B * H, Sq, d);
+    *bytes = pda::bwd_workspace_bytes(pda::plan_bwd(Sq, kv_valid_len, (int64_t)B * H, d, n_cu), (int64_t)B * H, Sq, d);
     return PDA_OK;
 }
 

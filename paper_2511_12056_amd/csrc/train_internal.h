@@ -27,9 +27,10 @@ inline int64_t bwd_steps(int64_t n) { return (n + kBwdTile - 1) / kBwdTile; }
 // Time of an item in tenths of a query step (1 us at d = 128): a key step takes 1.2 of it, start and end of an item about six.
 inline int64_t bwd_key_time(int64_t steps) { return steps * 12 + 60; }
 inline int64_t bwd_query_time(int64_t steps) { return steps * 10 + 60; }
-// Partial sums of kBwdRows rows that a plan writes and a second kernel adds: half of such a unit each, and that kernel's launch.
+// Partial sums of kBwdRows rows and d columns that a plan writes and a second kernel adds: written and read at about 4 TB/s, and that
+// kernel's launch.
 inline int64_t bwd_part_slots(const BwdPlan& w) { return (w.key_parts > 1 ? (int64_t)w.key_blocks * w.key_parts * 2 : 0) + (int64_t)w.query_cut * (w.query_cut ? w.query_parts : 0); }
-inline int64_t bwd_join_time(const BwdPlan& w) { const int64_t n = bwd_part_slots(w); return n ? 50 + n / 2 : 0; }
+inline int64_t bwd_join_time(const BwdPlan& w, int d) { const int64_t n = bwd_part_slots(w); return n ? 30 + n * d / 200 : 0; }
 // When the last item of a launch ends if each goes, in order, to the compute unit that is free first.
 inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
     struct Free { int64_t at, units; } f[8] = {{0, n_cu}};     // compute units by the time at which they become free
@@ -64,7 +65,7 @@ inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
 // about equal time; one of more blocks has the blocks that start last cut where that ends it earlier, and its key blocks, which start
 // first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel.
 // us, uncut -> cut: see attn_bwd.hip.
-inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int n_cu) {
+inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     BwdPlan w{};
     w.key_per_head = (int)((n_v + kBwdRows - 1) / kBwdRows);
     w.query_per_head = (int)((Sq + kBwdRows - 1) / kBwdRows);
@@ -84,7 +85,7 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int n_cu) {
             c.query_parts = query_parts;
         }
         if (bwd_part_slots(c) > 4 * (int64_t)n_cu) return;
-        const int64_t t = bwd_end(c, Sq, n_v, n_cu) + bwd_join_time(c);
+        const int64_t t = bwd_end(c, Sq, n_v, n_cu) + bwd_join_time(c, d);
         if (t < best_time) {
             best = c;
             best_time = t;
@@ -92,8 +93,11 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int n_cu) {
     };
     if (blocks <= n_cu) {
         for (int k = 1; k <= max_k && w.key_blocks * k + w.query_blocks <= n_cu; ++k) {
-            const int64_t q = (n_cu - (int64_t)w.key_blocks * k) / w.query_blocks;
-            consider(k, w.query_blocks, (int)(q < max_q ? q : max_q));
+            const int64_t most = (n_cu - (int64_t)w.key_blocks * k) / w.query_blocks, even = (sq * 10 * k + sk * 12 - 1) / (sk * 12);
+            const int64_t q = most < max_q ? most : max_q;
+            consider(k, w.query_blocks, (int)q);
+            if (even < q) consider(k, w.query_blocks, (int)even);
+            if (even - 1 < q) consider(k, w.query_blocks, (int)(even - 1));
         }
         return best;
     }
