@@ -1,14 +1,21 @@
 // Layer norm forward and backward over the last axis, bound by HBM: every element is read once, held in fp32 registers
 // across the sums over its row, and written once.
 //
-// A row belongs to TPR threads: a wavefront up to D = 2 048 (sums over the row in registers, no barrier), beyond that a whole
-// workgroup.  A thread holds NV groups of four elements: 16 (fp32) or 8 bytes (bf16) an access, consecutive threads side by side.  Rows that are
+// A row belongs to TPR threads: a wavefront (sums over the row in registers, no barrier) or a whole workgroup (one barrier, the sums
+// of two rows alternate between two places in LDS).  Forward, a wavefront up to D = 2 048: rows x D fp32 -> bf16 with a workgroup
+// each instead 119 056 x 1 536 191 -> 218 us.  Backward, a wavefront up to D = 512 only: there a thread also keeps the sums of its columns
+// over the rows, and four times the columns are four times the registers (60 000 x 2 048 bf16 394 -> 152 us with a workgroup a row).
+// A thread holds NV groups of four elements: 16 (fp32) or 8 bytes (bf16) an access, consecutive threads side by side.  Rows that are
 // not a multiple of four elements long start at any address, so there a thread takes single elements, consecutive threads side by
 // side again.
 //
-// Backward, the sums over the rows (dweight, dbias): a workgroup takes consecutive rows of one group and keeps its threads'
-// columns in registers; its sums go to the workspace, where a second kernel adds those of a group in order.
+// Backward, the sums over the rows (dweight, dbias): workgroup i of a group takes rows i, i + chunks, ..., so that all of them stream through
+// neighbouring rows (each through rows of its own: 5 to 25 % slower), and keeps its columns' sums in registers; they go to the workspace,
+// where a second kernel adds those of a group in order.  The next row is requested before a row's arithmetic (60 000 x 2 048 172 -> 152 us).
+// Stores are non-temporal (119 056 x 1 536 forward 191 -> 185, backward 333 -> 323 us; 100 000 x 1 024 forward, bf16, 82 -> 60).
+// Measured: 119 056 x 1 536, fp32 x, bf16 y: forward 185 us = 5.9 TB/s, backward 323 us = 5.7 TB/s; 9 594 x 1 152 bf16 9.2 and 20 us.
 #include <hip/hip_runtime.h>
+#include <type_traits>
 #include "attn_internal.h"
 #include "train_device.h"
 #include "train_internal.h"
@@ -19,29 +26,32 @@ template <typename T, bool VEC, int TPR, int NV>
 struct RowIO {
     // element e of group i of thread t
     static __device__ __forceinline__ int col(int i, int e, int t) { return VEC ? (i * TPR + t) * 4 + e : (i * 4 + e) * TPR + t; }
-    static __device__ __forceinline__ void load(const T* row, int D, int t, float (&x)[NV][4]) {
+    // A thread's part of a row as it lies in memory, zeros behind the row's end.
+    using Group = std::conditional_t<!VEC || sizeof(T) == 4, f32x4, u32x2>;
+    static __device__ __forceinline__ void fetch(const T* row, int D, int t, Group (&g)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            const int c = col(i, 0, t);
             if constexpr (VEC) {
-                const int c = col(i, 0, t);
-                if (c < D) {
-                    if constexpr (sizeof(T) == 4) {
-                        const f32x4 v = *reinterpret_cast<const f32x4*>(row + c);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[i][e] = v[e];
-                    } else {
-                        const u32x2 v = *reinterpret_cast<const u32x2*>(row + c);
-                        x[i][0] = bf16_lo(v.x); x[i][1] = bf16_hi(v.x); x[i][2] = bf16_lo(v.y); x[i][3] = bf16_hi(v.y);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[i][e] = 0.f;
-                }
+                g[i] = Group{};
+                if (c < D) g[i] = *reinterpret_cast<const Group*>(row + c);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][e] = col(i, e, t) < D ? (float)row[col(i, e, t)] : 0.f;
+                for (int e = 0; e < 4; ++e) g[i][e] = col(i, e, t) < D ? (float)row[col(i, e, t)] : 0.f;
             }
         }
+    }
+    static __device__ __forceinline__ float value(const Group (&g)[NV], int i, int e) {
+        if constexpr (std::is_same_v<Group, f32x4>) return g[i][e];
+        else return e % 2 ? bf16_hi(g[i][e / 2]) : bf16_lo(g[i][e / 2]);
+    }
+    static __device__ __forceinline__ void load(const T* row, int D, int t, float (&x)[NV][4]) {
+        Group g[NV];
+        fetch(row, D, t, g);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = value(g, i, e);
     }
     static __device__ __forceinline__ void store(T* row, int D, int t, const float (&x)[NV][4]) {
 #pragma unroll
@@ -49,8 +59,8 @@ struct RowIO {
             if constexpr (VEC) {
                 const int c = col(i, 0, t);
                 if (c < D) {
-                    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(row + c) = f32x4{x[i][0], x[i][1], x[i][2], x[i][3]};
-                    else *reinterpret_cast<u32x2*>(row + c) = u32x2{pack_bf16(x[i][0], x[i][1]), pack_bf16(x[i][2], x[i][3])};
+                    if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(f32x4{x[i][0], x[i][1], x[i][2], x[i][3]}, reinterpret_cast<f32x4*>(row + c));
+                    else __builtin_nontemporal_store(u32x2{pack_bf16(x[i][0], x[i][1]), pack_bf16(x[i][2], x[i][3])}, reinterpret_cast<u32x2*>(row + c));
                 }
             } else {
 #pragma unroll
@@ -69,7 +79,6 @@ __device__ __forceinline__ void row_sum(float& a, float& b, float* lds) {
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         const int w = threadIdx.x >> 6;
-        __syncthreads();                                        // the sums before these have been read
         if ((threadIdx.x & 63) == 0) { lds[w] = a; lds[W + w] = b; }
         __syncthreads();
         a = lds[0];
@@ -84,7 +93,7 @@ constexpr int ln_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 template <typename TX, typename TY, bool VEC, int TPR, int NV>
 __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_fwd_kernel(const LayerNormParams p) {
     constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
-    __shared__ float lds[2 * (TPR / 64)];
+    __shared__ float lds[4 * (TPR / 64)];
     const int t = threadIdx.x % TPR, D = p.D;
     const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
     if (r >= p.rows) return;                                    // RPW > 1: no barrier follows
@@ -102,9 +111,9 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_fwd_kernel(const L
             x[i][e] = RowIO<TX, VEC, TPR, NV>::col(i, e, t) < D ? x[i][e] - mean : 0.f;
             ss = __builtin_fmaf(x[i][e], x[i][e], ss);
         }
-    row_sum<TPR>(ss, zero, lds);
+    row_sum<TPR>(ss, zero, lds + 2 * (TPR / 64));
     const float rstd = 1.0f / sqrtf(ss / (float)D + p.eps);
-    const int64_t g = p.groups == 1 ? 0 : r / p.group_rows;
+    const int64_t g = p.groups == 1 ? 0 : (unsigned)r / (unsigned)p.group_rows;       // rows < 2^31
     if (p.weight) {
         float w[NV][4];
         RowIO<float, VEC, TPR, NV>::load(p.weight + g * D, D, t, w);
@@ -136,47 +145,66 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_fwd_kernel(const L
 template <typename TX, typename TY, bool VEC, int TPR, int NV>
 __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_bwd_kernel(const LayerNormParams p) {
     constexpr int RPW = ln_threads(TPR) / TPR;
-    __shared__ float lds[2 * (TPR / 64)];
+    using X = RowIO<TX, VEC, TPR, NV>;
+    using Y = RowIO<TY, VEC, TPR, NV>;
+    __shared__ float lds[4 * (TPR / 64)];
+    int par = 0;
     __shared__ float joined[RPW > 1 ? RPW * NV * 4 * TPR : 1];
     const int t = threadIdx.x % TPR, own = threadIdx.x / TPR, D = p.D;
-    const int64_t g = blockIdx.y, first = (int64_t)blockIdx.x * p.chunk_rows;
-    const int64_t last = first + p.chunk_rows < p.group_rows ? first + p.chunk_rows : p.group_rows;
+    const int64_t g = blockIdx.y;
     const float inv_d = 1.0f / (float)D;
-    float w[NV][4], sw[NV][4], sb[NV][4];
-    if (p.weight) RowIO<float, VEC, TPR, NV>::load(p.weight + g * D, D, t, w);
+    float sw[NV][4], sb[NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sw[i][e] = sb[i][e] = 0.f;
-            if (!p.weight) w[i][e] = 1.f;
-        }
-    for (int64_t n = first + own; n < last; n += RPW) {         // RPW == 1: all threads of the workgroup alike
-        const int64_t r = g * p.group_rows + n;
-        float x[NV][4], dy[NV][4], a = 0.f, b = 0.f;
-        RowIO<TX, VEC, TPR, NV>::load(static_cast<const TX*>(p.x) + r * D, D, t, x);
-        RowIO<TY, VEC, TPR, NV>::load(static_cast<const TY*>(p.dy) + r * D, D, t, dy);
-        const float mean = p.mean[r], rstd = p.rstd[r];
+        for (int e = 0; e < 4; ++e) sw[i][e] = sb[i][e] = 0.f;
+    const int64_t step = RPW * p.chunks, r0 = g * p.group_rows;
+    const TX* xp = static_cast<const TX*>(p.x);
+    const TY* yp = static_cast<const TY*>(p.dy);
+    int64_t n = (int64_t)blockIdx.x * RPW + own;
+    typename X::Group xn[NV];
+    typename Y::Group yn[NV];
+    float mean_n = 0.f, rstd_n = 0.f;
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+        X::fetch(xp + r * D, D, t, xn);
+        Y::fetch(yp + r * D, D, t, yn);
+        mean_n = p.mean[r];
+        rstd_n = p.rstd[r];
+    };
+    if (n < p.group_rows) fetch(r0 + n);
+    for (; n < p.group_rows; n += step) {                      // RPW == 1: all threads of the workgroup alike
+        const int64_t r = r0 + n;
+        float x[NV][4], dy[NV][4], w[NV][4], a = 0.f, b = 0.f;
+        const float mean = mean_n, rstd = rstd_n;
+        if (p.weight) RowIO<float, VEC, TPR, NV>::load(p.weight + g * D, D, t, w);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[i][e] = (x[i][e] - mean) * rstd;              // columns behind D: dy = 0 there
+                x[i][e] = (X::value(xn, i, e) - mean) * rstd;   // columns behind D: dy = 0 there
+                dy[i][e] = Y::value(yn, i, e);
+            }
+        if (n + step < p.group_rows) fetch(r + step);           // the next row travels under this one's arithmetic
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
                 sw[i][e] = __builtin_fmaf(dy[i][e], x[i][e], sw[i][e]);
                 sb[i][e] += dy[i][e];
-                dy[i][e] *= w[i][e];
+                if (p.weight) dy[i][e] *= w[i][e];
                 a += dy[i][e];
                 b = __builtin_fmaf(dy[i][e], x[i][e], b);
             }
         if (p.y) {
-            row_sum<TPR>(a, b, lds);
+            row_sum<TPR>(a, b, lds + par);
+            par ^= 2 * (TPR / 64);
             a *= inv_d;
             b *= inv_d;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i][e] = rstd * (dy[i][e] - a - x[i][e] * b);
-            RowIO<TX, VEC, TPR, NV>::store(static_cast<TX*>(p.y) + r * D, D, t, x);
+            X::store(static_cast<TX*>(p.y) + r * D, D, t, x);
         }
     }
     // the sums of the workgroup's rows: its own place in the workspace, or the result if it is alone in the group
@@ -204,26 +232,30 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_bwd_kernel(const L
     if (p.dbias) finish(sb, alone ? p.dbias + g * D : part + D);
 }
 
-// dweight (blockIdx.z = 0) or dbias: 64 columns a workgroup, 16 threads a column, each a sixteenth of the chunks.
+// dweight (blockIdx.z = 0) or dbias: 32 columns a workgroup, 32 threads a column, each with every 32nd of the chunks.
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const LayerNormParams p) {
-    __shared__ float lds[16][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+    __shared__ float lds[32][33];
+    const int c = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
     const int64_t g = blockIdx.y;
     float* to = blockIdx.z == 0 ? p.dweight : p.dbias;
     if (!to) return;
     float s = 0.f;
-    if (c < p.D) {
-        const float* src = p.part + (g * p.chunks * 2 + blockIdx.z) * p.D + c;
-        const int64_t i1 = p.chunks * (w + 1) / 16;
-#pragma unroll 8
-        for (int64_t i = p.chunks * w / 16; i < i1; ++i) s += src[i * 2 * p.D];
-    }
-    lds[w][threadIdx.x & 63] = s;
-    __syncthreads();
-    if (w == 0 && c < p.D) {
+    if (col < p.D) {
+        const float* src = p.part + (g * p.chunks * 2 + blockIdx.z) * p.D + col;
+        for (int64_t k = w; k < p.chunks; k += 32 * 16) {      // sixteen loads in flight
+            float x[16];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) s += lds[i][threadIdx.x];
-        to[g * p.D + c] = s;
+            for (int i = 0; i < 16; ++i) x[i] = k + 32 * i < p.chunks ? src[(k + 32 * i) * 2 * p.D] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += x[i];
+        }
+    }
+    lds[w][c] = s;
+    __syncthreads();
+    if (w == 0 && col < p.D) {
+#pragma unroll
+        for (int i = 1; i < 32; ++i) s += lds[i][c];
+        to[g * p.D + col] = s;
     }
 }
 
@@ -250,10 +282,15 @@ template <bool BWD, typename TX, typename TY, bool VEC>
 static hipError_t launch_ln(const LayerNormParams& p, hipStream_t st) {
     if (p.D <= 256) return launch_ln<BWD, TX, TY, VEC, 64, 1>(p, st);
     if (p.D <= 512) return launch_ln<BWD, TX, TY, VEC, 64, 2>(p, st);
-    if (p.D <= 1024) return launch_ln<BWD, TX, TY, VEC, 64, 4>(p, st);
-    if (p.D <= 1536) return launch_ln<BWD, TX, TY, VEC, 64, 6>(p, st);
-    if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 64, 8>(p, st);
-    if (p.D <= 4096) return launch_ln<BWD, TX, TY, VEC, 256, 4>(p, st);
+    if constexpr (BWD) {
+        if (p.D <= 1024) return launch_ln<BWD, TX, TY, VEC, 256, 1>(p, st);
+        if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 256, 2>(p, st);
+    } else {
+        if (p.D <= 1024) return launch_ln<BWD, TX, TY, VEC, 64, 4>(p, st);
+        if (p.D <= 1536) return launch_ln<BWD, TX, TY, VEC, 64, 6>(p, st);
+        if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 64, 8>(p, st);
+    }
+    if (p.D <= 4096) return launch_ln<BWD, TX, TY, VEC, 512, 2>(p, st);
     return launch_ln<BWD, TX, TY, VEC, 512, 4>(p, st);         // up to PDA_LAYER_NORM_MAX = 8192
 }
 
@@ -280,7 +317,7 @@ hipError_t launch_layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_b
     }
     const hipError_t e = launch_ln<true>(p, x_bf16, y_bf16, st);
     if (e != hipSuccess || p.chunks == 1 || (!p.dweight && !p.dbias)) return e;
-    hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), (unsigned)p.groups, 2), dim3(1024), 0, st, p);
+    hipLaunchKernelGGL(layer_norm_join_kernel, dim3((unsigned)((p.D + 31) / 32), (unsigned)p.groups, 2), dim3(1024), 0, st, p);
     return hipGetLastError();
 }
 

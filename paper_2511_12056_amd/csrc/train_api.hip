@@ -225,8 +225,7 @@ int pda_layer_norm_bwd(const void* dy, int y_type, const void* x, int x_type, co
             return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", workspace ? (long long)workspace_bytes : 0LL, (long long)need);
         if (need > 0 && !aligned(workspace, 16)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 16-byte aligned");
         p.group_rows = rows / groups;
-        p.chunk_rows = pda::ln_chunk_rows(p.group_rows, groups, n_cu);
-        p.chunks = pda::ln_chunks(p.group_rows, groups, n_cu);
+        p.chunks = pda::ln_chunks(p.group_rows, groups, D, n_cu);
     }
     p.x = x; p.dy = dy; p.weight = weight; p.y = dx;
     p.mean = const_cast<float*>(mean); p.rstd = const_cast<float*>(rstd);
