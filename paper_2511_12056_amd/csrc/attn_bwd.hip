@@ -1,16 +1,34 @@
 // Attention backward, gfx950, d = 128 and 64: dq, dk, dv from dout and the forward call's log-sum-exp.
 //
+//   P = exp(scale Q K^T - lse),  delta_i = <dout_i, out_i>,  dS = P (dO V^T - delta),
+//   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
+//
 // Two kinds of work items in one launch, both of which compute the probabilities again:
-//   * keys:    128 keys of a head stay (k and v rows as MFMA operands in registers), its query rows stream by:
+//   * keys:    256 keys of a head stay (k and v rows as MFMA operands in registers), its query rows stream by, 32 a step:
 //              S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS                        4 products
-//   * queries: 128 query rows stay (q and dout), the head's keys stream by:
+//   * queries: 256 query rows stay (q and dout), the head's valid keys stream by:
 //              S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T                                   3 products
-// Seven products where five are the least: one item kind that also summed dq would have to add to the same dq rows
-// from every block of keys, in an order that changes from run to run (atomics), or keep dq partials of every block.
+// Seven products where five are the least: one kind of item that also summed dq would have to add to the same dq rows from every block of keys, in an
+// order that changes from run to run (atomics), or keep dq partials of every block (256 rows' worth of reads and writes for a step's work).
+// The same call gives the same bits.
 //
 // As in the forward kernels the products are taken so that one resident row lies in each lane pair (l, l + 32) of a wavefront, and
 // the exponentiated scores in their accumulator registers are the operand of the next product as they stand, because the
 // contraction index is permuted identically on both sides (the transposing LDS reads).
+//
+// What bounds it: the matrix cores and, beside them, the arithmetic of the softmax, which both kinds of items do.  On a SIMD that is full of matrix
+// instructions a vector instruction costs 6 cycles and an exponential 11, a 32x32x16 product 33.  So each SIMD has two wavefronts, of which one is in matrix
+// instructions while the other computes, held in step by barriers: the split differs by d.
+//   * d = 128: a step has twice the products for the same exponentials, and the sums of 64 rows and two gradients do not fit one wavefront's registers.  Two
+//     wavefronts share 64 resident rows (attn_bwd_pair_item): one has the scores, the probabilities and dV, the other dP, dS and dK or dQ.
+//     Without the phases, both wavefronts through their steps as they come, 24 x 9 600 3.80 instead of 3.40 ms.
+//   * d = 64: a wavefront has 32 resident rows to itself (attn_bwd_lone_item), so that the probabilities stay in its registers.  Pairs instead:
+//     24 x 9 600 2 146 us and now 2 058, 6 x 33 000 6 457 and 6 020, 24 x 4 797 on 4 701 559 and 545, 2 x 1 024 23.5 and 22.2.  (At d = 128 such wavefronts spill.)
+// Rounding to bf16: P as the operand of dV and dS as the operand of dK and dQ, as in the forward call; the P in dS stays fp32 (rounded there too,
+// dq and dk are off by 0.0029 instead of 0.0024 of the largest value).
+// Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.8 ms
+// = 930 TFLOP/s (the seven products run at 1 300), 24 x 9 600 3.13 ms = 904, 1 x 9 600 157 us = 750, 24 x 16 384 on 570 461 us = 622; d = 64: 6 x 33 000
+// 6.02 ms = 695, 24 x 4 797 on 4 701 545 us = 635, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"
@@ -109,10 +127,42 @@ __device__ __forceinline__ void store_rows(__bf16* base, int64_t first, int64_t 
         }
 }
 
+// Operand fragments of a streamed tile in LDS.  rows: 16 columns from 16 * KK on of 32 rows; tr: 16 rows from 16 * (IDX / (D / 32)) on, transposed, of the columns of
+// block IDX % (D / 32).  `at` is the lane's address in the tile (frag_rows_at, frag_tr_at); what moves it by a granule is XORed in where it is used.
+template <int D>
+__device__ __forceinline__ unsigned frag_rows_at(int lane) { return (lane & 31) * (D * 2) + (((lane >> 5) ^ swz_kv<D>(lane & 31)) * 16); }
+template <int D>
+__device__ __forceinline__ unsigned frag_tr_at(int lane) {
+    const int li = lane & 31, t16 = lane & 15, row = 4 * (lane >> 5) + (t16 >> 2), g = 2 * (li >> 4) + ((t16 & 3) >> 1);
+    return row * (D * 2) + ((g ^ swz_kv<D>(row)) * 16) + (t16 & 1) * 8;
+}
+template <int N>
+__device__ __forceinline__ LDS_PTR(const unsigned char) frag_block(unsigned at) {
+    unsigned r = at;
+    if constexpr (N != 0) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(r) : "n"(N), "v"(at));
+    return (LDS_PTR(const unsigned char))(uintptr_t)r;
+}
+template <int KK>
+__device__ __forceinline__ bf16x8 read_rows(unsigned at) { return *(LDS_PTR(const bf16x8))frag_block<KK * 32>(at); }
+template <int D, int IDX>
+__device__ __forceinline__ bf16x8 read_tr(unsigned at) {
+    constexpr int db = IDX % (D / 32), u = IDX / (D / 32);
+    static_assert(swz_kv<D>(8) == 2 && swz_kv<D>(0) == 0, "eight rows on, the granule differs in one bit");
+    LDS_PTR(const unsigned char) x = frag_block<db * 64>(at);
+    LDS_PTR(const unsigned char) y = frag_block<(db * 64) ^ 32>(at);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(x + u * 16 * (D * 2)));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + (u * 16 + 8) * (D * 2)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// ---- d = 128: two wavefronts for 64 resident rows ----------------------------------------------------------------
+// A step is two phases with a barrier behind each:
+//   1  first: sums of dV of step t - 1, scores of step t (matrix)     second: dS of step t - 1 (vector)
+//   2  first: probabilities of step t, into LDS for the other (vector)   second: sums of dK or dQ of step t - 1, dP of step t (matrix)
 // One block of resident rows against the streamed tiles [t0, t1).  part: where the sums go in fp32 if other work items have the
 // block's other tiles (dQ, or dK and behind it dV: kBwdRows * D floats each, in the order of the accumulator registers), else null.
 template <int D, bool KEYS>
-__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
+__device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32;
     constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2);
     constexpr int CPW = TILE / 4096;                           // chunks of 1 KB of a tile that a fetching wavefront brings
@@ -172,29 +222,14 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
         if (KEYS && pair == 0) lds_dma4(stats + (int64_t)t * (2 * kBwdTile), opaque_lane() * 4, lds0 + bwd_stat_base(D) + t % kBwdRing * 256);
     };
 
-    // ---- operand addresses in buffer 0; blocks are XORed in
-    const int t16 = lane & 15, tr_row = 4 * lh + (t16 >> 2), tr_g = 2 * (li >> 4) + ((t16 & 3) >> 1);
-    unsigned rows_at = lds0 + li * (D * 2) + ((lh ^ swz_kv<D>(li)) * 16);
-    unsigned tr_at = lds0 + tr_row * (D * 2) + ((tr_g ^ swz_kv<D>(tr_row)) * 16) + (t16 & 1) * 8;
-    auto block = [](unsigned at, auto n) __attribute__((always_inline)) {
-        unsigned r = at;
-        if constexpr (decltype(n)::value != 0) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(r) : "n"(decltype(n)::value), "v"(at));
-        return r;
-    };
+    // ---- operand fragments, in buffer 0 from these addresses on
+    unsigned rows_at = lds0 + frag_rows_at<D>(lane), tr_at = lds0 + frag_tr_at<D>(lane);
     bf16x8 frag[PF + 1];
     auto rows_frag = [&](int t, int tensor, auto kk) __attribute__((always_inline)) {
-        const unsigned at = block(rows_at + t % kBwdRing * 2 * TILE + tensor * TILE, std::integral_constant<int, decltype(kk)::value * 32>{});
-        frag[decltype(kk)::value % (PF + 1)] = *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)at;
+        frag[decltype(kk)::value % (PF + 1)] = read_rows<decltype(kk)::value>(rows_at + t % kBwdRing * 2 * TILE + tensor * TILE);
     };
-    auto tr_frag = [&](int t, int tensor, auto idx) __attribute__((always_inline)) {      // idx = u * NDB + db
-        constexpr int db = decltype(idx)::value % NDB, u = decltype(idx)::value / NDB;
-        static_assert(swz_kv<D>(8) == 2 && swz_kv<D>(0) == 0, "eight rows on, the granule differs in one bit");
-        const unsigned at = tr_at + t % kBwdRing * 2 * TILE + tensor * TILE;
-        LDS_PTR(const unsigned char) x = (LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, db * 64>{});
-        LDS_PTR(const unsigned char) y = (LDS_PTR(const unsigned char))(uintptr_t)block(at, std::integral_constant<int, (db * 64) ^ 32>{});
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(x + u * 16 * (D * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + (u * 16 + 8) * (D * 2)));
-        frag[decltype(idx)::value % (PF + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    auto tr_frag = [&](int t, int tensor, auto idx) __attribute__((always_inline)) {
+        frag[decltype(idx)::value % (PF + 1)] = read_tr<D, decltype(idx)::value>(tr_at + t % kBwdRing * 2 * TILE + tensor * TILE);
     };
     // A pair's probabilities of a step: group a of block i, 16 bytes a lane.  Statistics of a tile's rows: four rows of group a.
     // (Addresses from a fresh lane index: they are not kept over the products.)
@@ -418,6 +453,258 @@ __device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, in
         store_rows<D, NDB>(base, first + 32 * i, n_res, KEYS ? p.Skv : p.Sq, second ? p.scale : 1.0f, [&](int db, int e) __attribute__((always_inline)) { return acc[i][db][e]; });
 }
 
+// A pointer that is the same in all lanes, in scalar registers (the compiler may choose one of two by vector instructions).
+template <typename T>
+__device__ __forceinline__ T* uniform(T* p) {
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<T*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x));
+}
+
+// ---- d = 64: a wavefront for 32 resident rows -------------------------------------------------------------------
+// A wavefront alternates between a matrix phase (sums of step t - 1, products of step t) and a vector phase (probabilities and dS of step t); of the two
+// on a SIMD the second is half a step behind the first.
+constexpr int kLoneRing = 4;            // tile buffers per streamed tensor
+constexpr int lone_stat_base(int d) { return kLoneRing * 2 * bwd_tile_bytes(d); }
+constexpr int lone_smem(int d) { return lone_stat_base(d) + kLoneRing * 256; }
+
+template <int D, bool KEYS>
+__device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
+    constexpr int G = D / 8, NKK = D / 16, NDB = D / 32, R = kLoneRing;
+    constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2), CPW = TILE / 4096;
+    constexpr int NF = 8;                                      // operand fragments under way
+    extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))bwd_smem_;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), quarter = wave & 3;
+    const int lane = opaque_lane(), li = lane & 31, lh = lane >> 5;
+    const bool second = wave >= 4;                             // the wavefronts that run a phase behind
+    const int b = bh / p.H, h = bh - b * p.H;
+    const __bf16* qp = p.q + (int64_t)b * p.q_bs + (int64_t)h * p.q_hs;
+    const __bf16* dop = p.dout + (int64_t)b * p.do_bs + (int64_t)h * p.do_hs;
+    const __bf16* kp = p.k + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
+    const __bf16* vp = p.v + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
+    const float* stats = p.stats + bh * p.stat_rows * 2 + (KEYS ? (int64_t)t0 * (2 * kBwdTile) : 0);
+    const int64_t n_res = KEYS ? p.n_v : p.Sq;
+    const int n_all = (int)(KEYS ? p.Sq : p.n_v);
+    const int n_str = (n_all < (int64_t)t1 * kBwdTile ? n_all : t1 * kBwdTile) - t0 * kBwdTile;        // streamed rows, counted from tile t0 on
+    const int64_t first = row0 + wave * 32;                    // this lane's resident row: first + li
+    const int nt = row0 < n_res ? t1 - t0 : 0;
+
+    auto step = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+    auto barrier = [&]() __attribute__((always_inline)) {      // keeps the phases apart
+        step();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        step();
+    };
+
+    // ---- loads of the streamed tiles: one tensor by either group, 1 KB chunks quarter, quarter + 4 .. of a tile (see attn_bwd_pair_item)
+    const __bf16* from = (second ? (KEYS ? dop : vp) : (KEYS ? qp : kp)) + (int64_t)t0 * (kBwdTile * D);
+    const unsigned whole = (quarter * RPC + lane / G) * (D * 2) + (((lane % G) ^ swz_kv<D>(quarter * RPC + lane / G)) * 16);
+    const bool with_stats = KEYS && wave == 4;
+    auto issue = [&](int t) __attribute__((always_inline)) {
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + t % R * 2 * TILE + (second ? TILE : 0) + quarter * 1024);
+        const __bf16* src = uniform(from + (int64_t)t * (kBwdTile * D));
+        const int last = n_str - 1 - t * kBwdTile;
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) {
+            if (last >= kBwdTile - 1) {
+                lds_dma16(src + i * 16 * D, whole, to + i * 4096);
+            } else {                                           // rows behind the last: that row again
+                const int l = opaque_lane(), r = (quarter + 4 * i) * RPC + l / G;
+                lds_dma16(src, (r < last ? r : last) * (D * 2) + (((l % G) ^ swz_kv<D>(r)) * 16), to + i * 4096);
+            }
+        }
+        if (with_stats) lds_dma4(uniform(stats + (int64_t)t * (2 * kBwdTile)), opaque_lane() * 4, __builtin_amdgcn_readfirstlane(lds0 + lone_stat_base(D) + t % R * 256));
+    };
+    // what was fetched before tile t is there, tile t may be under way
+    auto arrived = [&](int t) __attribute__((always_inline)) {
+        step();
+        if (t < nt) {
+            if (with_stats) wait_vmcnt<CPW + 1>();
+            else wait_vmcnt<CPW>();
+        } else {
+            wait_vmcnt<0>();
+        }
+    };
+
+    // ---- operand fragments, number n of a matrix phase into frag[n % NF]
+    unsigned rows_at = lds0 + frag_rows_at<D>(lane), tr_at = lds0 + frag_tr_at<D>(lane);
+    bf16x8 frag[NF];
+    auto rows_frag = [&](int t, int tensor, auto kk, auto n) __attribute__((always_inline)) {
+        frag[decltype(n)::value % NF] = read_rows<decltype(kk)::value>(rows_at + t % R * 2 * TILE + tensor * TILE);
+    };
+    auto tr_frag = [&](int t, int tensor, auto idx, auto n) __attribute__((always_inline)) {
+        frag[decltype(n)::value % NF] = read_tr<D, decltype(idx)::value>(tr_at + t % R * 2 * TILE + tensor * TILE);
+    };
+
+    // ---- resident rows
+    bf16x8 res[2][NKK];                                        // k and v rows, or q and dout rows
+    float l_res = 0.f, d_res = 0.f;
+    if (nt > 0) {
+        for (int t = 0; t < 2 && t < nt; ++t) issue(t);
+        const int64_t c = first + li < n_res ? first + li : n_res - 1;
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) {
+            res[0][kk] = *reinterpret_cast<const bf16x8*>((KEYS ? kp : qp) + c * D + lh * 8 + kk * 16);
+            res[1][kk] = *reinterpret_cast<const bf16x8*>((KEYS ? vp : dop) + c * D + lh * 8 + kk * 16);
+        }
+        if constexpr (!KEYS) {
+            l_res = stats[(c / kBwdTile) * (2 * kBwdTile) + c % kBwdTile];
+            d_res = stats[(c / kBwdTile) * (2 * kBwdTile) + kBwdTile + c % kBwdTile];
+        }
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
+        asm volatile("" : "+v"(l_res), "+v"(d_res));
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+v"(res[i][kk]));
+        __syncthreads();
+    }
+    f32x16 acc[2][NDB];                                        // dK^T or dQ^T; dV^T
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][db][r] = 0.f;
+    const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    f32x16 s, dp;                                              // scores, then p; <dout, v>, then ds: as operands in groups 0 and 2
+    f32x4 st[2][4];                                            // -lse * log2 e and -delta of the step's rows
+
+    // Matrix phase: the sums of step t - 1 (SUMS), then the products of step t (PRODS).  Product n of the phase:
+    constexpr int N_SUM = (KEYS ? 2 : 1) * 2 * NDB, N_PROD = 2 * NKK;
+    auto matrix = [&](int t, auto has_sums, auto has_prods) __attribute__((always_inline)) {
+        constexpr int N0 = decltype(has_sums)::value ? 0 : N_SUM, N1 = N_SUM + (decltype(has_prods)::value ? N_PROD : 0);
+        auto load = [&](auto j) __attribute__((always_inline)) {
+            constexpr int n = decltype(j)::value;
+            if constexpr (n < N_SUM) {
+                if constexpr (KEYS) tr_frag(t - 1, 1 - n % 2, std::integral_constant<int, n / 2>{}, j);       // dout for dV, q for dK
+                else tr_frag(t - 1, 0, j, j);
+            } else if constexpr (n < N1) {
+                rows_frag(t, (n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM) / 2>{}, j);
+            } else if constexpr (KEYS && decltype(has_prods)::value && n < N1 + 8) {
+                constexpr int which = (n - N1) % 2, a = (n - N1) / 2;
+                const unsigned at = lds0 + lone_stat_base(D) + t % R * 256 + (opaque_lane() >> 5) * 16;
+                st[which][a] = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(at + which * 128 + 32 * a);
+            }
+        };
+        static_for<N0, N0 + NF - 1>([&](auto j) { load(j); });
+        step();
+        __builtin_amdgcn_s_setprio(1);
+        static_for<N0, N1>([&](auto j) {
+            constexpr int n = decltype(j)::value;
+            load(std::integral_constant<int, n + NF - 1>{});
+            if constexpr (n < N_SUM) {
+                constexpr bool dv = KEYS && n % 2 == 0;
+                constexpr int idx = KEYS ? n / 2 : n, u = idx / NDB * 8;
+                const f32x16& v = dv ? s : dp;
+                const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v, v, u, u + 1, u + 2, u + 3));
+                acc[dv][idx % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], x, acc[dv][idx % NDB], 0, 0, 0);
+            } else {
+                constexpr int kk = (n - N_SUM) / 2;
+                if constexpr ((n - N_SUM) % 2 == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[0][kk], kk == 0 ? zero : s, 0, 0, 0);
+                else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[1][kk], kk == 0 ? zero : dp, 0, 0, 0);
+            }
+            step();
+        });
+        static_for<N1 + NF - 1, N1 + 8>([&](auto j) { load(j); });
+        step();
+        __builtin_amdgcn_s_setprio(0);
+    };
+    const float c = p.scale_log2e;
+    auto vector = [&](int t) __attribute__((always_inline)) {
+        const bool tail = !KEYS && (t + 1) * kBwdTile > n_str;
+        // groups of four values in place, the exponentials of one beside the products of the one before
+        static_for<0, 5>([&](auto j) {
+            constexpr int n = decltype(j)::value;
+            if constexpr (n < 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[4 * n + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * n + e], c, KEYS ? st[0][n][e] : l_res));
+                if (tail) {
+                    const int hidden = n_str - t * kBwdTile - (opaque_lane() >> 5) * 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[4 * n + e] = 8 * n + e >= hidden ? 0.f : s[4 * n + e];
+                }
+            }
+            if constexpr (n > 0) {
+                constexpr int a = n - 1, at = a / 2 * 8 + a % 2 * 2;
+                float x[4], y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = s[4 * a + e];
+                    y[e] = x[e] * (dp[4 * a + e] + (KEYS ? st[1][a][e] : d_res));
+                }
+                if constexpr (KEYS) {
+                    s[at] = __uint_as_float(pack_bf16(x[0], x[1]));
+                    s[at + 1] = __uint_as_float(pack_bf16(x[2], x[3]));
+                }
+                dp[at] = __uint_as_float(pack_bf16(y[0], y[1]));
+                dp[at + 1] = __uint_as_float(pack_bf16(y[2], y[3]));
+            }
+            step();
+        });
+        asm volatile("" : "+v"(s), "+v"(dp));                  // here, not where they are used
+    };
+    constexpr std::false_type no{};
+    constexpr std::true_type yes{};
+    // Half a step each, a barrier behind it: the first group's matrix phase of step t is half step 2 t, the second's 2 t + 1; a vector phase follows.  Tile
+    // u goes into the buffer of tile u - 4, which is last read in half step 2 u - 5 (sums of the second group), and is first read in 2 u.
+    // Key items, whose matrix phase is the longer one, request it in the vector phase (half step 2 u - 3 of the first group, 2 u - 4 of the second),
+    // query items in the matrix phase (2 u - 4 and 2 u - 3); each group waits for it at the end of half step 2 u - 1.
+    // (Query items' requests in the vector phase too: 24 x 9 600 2 094 instead of 2 032 us; key items' in the matrix phase: 2 083.)
+    if (nt > 0) {
+        if (second) {
+            if (KEYS && nt > 2) issue(2);
+            barrier();
+        }
+        if (!KEYS && nt > 2) issue(2);
+        matrix(0, no, yes);
+        if (second) arrived(2);
+        barrier();
+        for (int t = 1; t < nt; ++t) {
+            asm volatile("" : "+v"(rows_at), "+v"(tr_at));     // nothing formed from them is kept across steps
+            const int next = t + 1 + (second ? 1 : 0);
+            if (KEYS && next < nt) issue(next);
+            vector(t - 1);
+            if (!second) arrived(t + 1);
+            barrier();
+            if (!KEYS && t + 2 < nt) issue(t + 2);
+            matrix(t, yes, yes);
+            if (second) arrived(t + 2);
+            barrier();
+        }
+        vector(nt - 1);
+        barrier();
+        matrix(nt, yes, no);
+        if (!second) barrier();                                // the second group's half step
+    }
+
+    // ---- results
+    static_for<0, KEYS ? 2 : 1>([&](auto k) {
+        constexpr int i = decltype(k)::value;
+        if (part) {
+            f32x4* to = reinterpret_cast<f32x4*>(part + i * kBwdRows * D) + wave * (NDB * 4 * 64) + opaque_lane();
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) to[(db * 4 + a) * 64] = f32x4{acc[i][db][4 * a], acc[i][db][4 * a + 1], acc[i][db][4 * a + 2], acc[i][db][4 * a + 3]};
+        } else {
+            __bf16* base = i == 1 ? p.dv + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs
+                          : KEYS ? p.dk + (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs : p.dq + (int64_t)b * p.dq_bs + (int64_t)h * p.dq_hs;
+            store_rows<D, NDB>(base, first, n_res, KEYS ? p.Skv : p.Sq, i == 1 ? 1.0f : p.scale, [&](int db, int e) __attribute__((always_inline)) { return acc[i][db][e]; });
+        }
+    });
+}
+
+template <int D>
+constexpr int item_smem() { return D == 128 ? bwd_smem(D) : lone_smem(D); }
+template <int D, bool KEYS>
+__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
+    if constexpr (D == 128) attn_bwd_pair_item<D, KEYS>(p, bh, row0, t0, t1, part);
+    else attn_bwd_lone_item<D, KEYS>(p, bh, row0, t0, t1, part);
+}
+
 template <int D>
 __global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams p) {
     const BwdPlan& w = p.plan;
@@ -522,9 +809,9 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
     const int64_t items = (int64_t)w.key_blocks * w.key_parts + w.query_blocks + (int64_t)w.query_cut * (w.query_parts - 1) + hidden;
     if (items > 0x7fffffff) return hipErrorInvalidValue;
     static KernelSetup setup;
-    hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), bwd_smem(D), nullptr);
+    hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), item_smem<D>(), nullptr);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(512), bwd_smem(D), st, p);
+    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(512), item_smem<D>(), st, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t joins = (w.key_parts > 1 ? (int64_t)w.key_blocks * 2 : 0) + w.query_cut;
     if (joins == 0) return hipSuccess;

@@ -64,7 +64,8 @@ inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
 // Cuts.  A launch of fewer blocks than compute units is cut so that its parts fill them in one round, key and query blocks into parts of
 // about equal time; one of more blocks has the blocks that start last cut where that ends it earlier, and its key blocks, which start
 // first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel.
-// us, uncut -> cut: see attn_bwd.hip.
+// us, uncut -> cut: d = 128: 1 x 9 600 343 -> 157, 12 x 3 000 240 -> 201, 24 x 2 048 184 -> 172, 24 x 16 384 on 570 628 -> 461, 24 x 9 600 3 329 -> 3 131,
+// 3 x 67 576 20 132 -> 18 822; d = 64: 2 x 1 024 39 -> 22, 1 x 9 600 294 -> 113, 24 x 4 797 569 -> 545, 6 x 33 000 6 891 -> 6 020.
 inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     BwdPlan w{};
     w.key_per_head = (int)((n_v + kBwdRows - 1) / kBwdRows);
