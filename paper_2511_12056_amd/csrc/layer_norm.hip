@@ -95,7 +95,7 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_fwd_kernel(const L
     constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
     __shared__ float lds[4 * (TPR / 64)];
     const int t = threadIdx.x % TPR, D = p.D;
-    const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW + threadIdx.x / TPR;
     if (r >= p.rows) return;                                    // RPW > 1: no barrier follows
     float x[NV][4], a = 0.f, zero = 0.f;
     RowIO<TX, VEC, TPR, NV>::load(static_cast<const TX*>(p.x) + r * D, D, t, x);
@@ -273,7 +273,8 @@ static hipError_t launch_ln(const LayerNormParams& p, hipStream_t st) {
         hipLaunchKernelGGL((layer_norm_bwd_kernel<TX, TY, VEC, TPR, NV>), dim3((unsigned)p.chunks, (unsigned)p.groups), dim3(ln_threads(TPR)), 0, st, p);
     } else {
         constexpr int rpw = ln_threads(TPR) / TPR;
-        hipLaunchKernelGGL((layer_norm_fwd_kernel<TX, TY, VEC, TPR, NV>), dim3((unsigned)((p.rows + rpw - 1) / rpw)), dim3(ln_threads(TPR)), 0, st, p);
+        const int64_t n = (p.rows + rpw - 1) / rpw, x = n < 1 << 21 ? n : 1 << 21;       // a launch has fewer than 2^32 threads along x
+        hipLaunchKernelGGL((layer_norm_fwd_kernel<TX, TY, VEC, TPR, NV>), dim3((unsigned)x, (unsigned)((n + x - 1) / x)), dim3(ln_threads(TPR)), 0, st, p);
     }
     return hipGetLastError();
 }

@@ -215,3 +215,100 @@ def test_pack_gradient(B, S, H, d, unit_rms):
         again = x.clone()
         pda.pack_heads_bwd(dy, again, again, True, 0.3)
         assert torch.equal(again, to)
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """2^23 rows are as many as one axis of a launch takes."""
+    import torch
+    import paper_2511_12056_amd as pda
+    rows, D = (1 << 23) + 4099, 8
+    x = torch.randn(rows, D, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    y, mean, rstd = torch.full_like(x, float("nan")), *(torch.full((rows,), float("nan"), device="cuda") for _ in range(2))
+    pda.layer_norm_fwd(x, None, None, y, mean, rstd, 1e-6)
+    m = x.mean(-1)
+    assert (mean - m).abs().max() <= 2.0 ** -20 * x.abs().max()          # seven additions and a division, in fp32, on either side
+    at = [0, 1, (1 << 23) - 1, 1 << 23, rows - 4097, rows - 1]
+    part, pm, pr = x[at].contiguous(), torch.empty(len(at), device="cuda"), torch.empty(len(at), device="cuda")
+    py = torch.empty_like(part)
+    pda.layer_norm_fwd(part, None, None, py, pm, pr, 1e-6)
+    assert torch.equal(y[at], py) and torch.equal(mean[at], pm) and torch.equal(rstd[at], pr)
+    assert torch.isfinite(y).all() and torch.isfinite(rstd).all()
+    dx, dw = torch.full_like(x, float("nan")), torch.empty(D, device="cuda")
+    pda.layer_norm_bwd(y, x, None, mean, rstd, dx, dw, None)
+    pdx = torch.empty_like(part)
+    pda.layer_norm_bwd(py, part, None, pm, pr, pdx, None, None)
+    assert torch.equal(dx[at], pdx) and torch.isfinite(dx).all()
+    want = y.double().square().sum(0)                # dy = xh: squares, in chains of fewer than rows / 4 096 + 4 096 additions
+    assert ((dw.double() - want).abs() <= 2.0 ** -24 * (rows / 4096 + 4096) * want).all()
+
+
+def test_elements_beyond_32_bits():
+    """2^31 elements and more, of rows that end beside a group of four."""
+    import torch
+    import paper_2511_12056_amd as pda
+    rows, D = 2 * 697_300, 1541
+    assert rows * D > 1 << 31
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.empty(rows, D, device="cuda", dtype=torch.bfloat16)
+    for r in range(0, rows, 139_460):
+        x[r:r + 139_460].normal_(generator=g)
+    w = 1 + torch.randn(2, D, generator=g, device="cuda")
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    pda.layer_norm_fwd(x, w, None, y, mean, rstd, 1e-6)
+    dx, dw = torch.empty_like(x), torch.empty(2, D, device="cuda")
+    pda.layer_norm_bwd(y, x, w, mean, rstd, dx, dw, None)
+    for a, b in ((0, 3), (rows - 1000, rows)):
+        part, pw = x[a:b].clone(), w[0 if a == 0 else 1].clone()
+        py, pm, pr, pdx = torch.empty_like(part), torch.empty(b - a, device="cuda"), torch.empty(b - a, device="cuda"), torch.empty_like(part)
+        pda.layer_norm_fwd(part, pw, None, py, pm, pr, 1e-6)
+        pda.layer_norm_bwd(py, part, pw, pm, pr, pdx, None, None)
+        assert torch.equal(y[a:b], py) and torch.equal(mean[a:b], pm) and torch.equal(rstd[a:b], pr) and torch.equal(dx[a:b], pdx)
+    del dx
+    # dweight = sum of dy xh with dy = y: terms of one sign, each off by 3 * 2^-24 at most, in chains of fewer than rows / 512 + 512 additions
+    for i in (0, 1):
+        want = torch.zeros(D, device="cuda", dtype=torch.float64)
+        for r in range(i * rows // 2, (i + 1) * rows // 2, 69_730):
+            s = slice(r, r + 69_730)
+            want += (y[s].double() * (x[s].double() - mean[s, None].double()) * rstd[s, None].double()).sum(0)
+        assert ((dw[i].double() - want).abs() <= 2.0 ** -24 * (rows / 512 + 512) * want.abs()).all()
+
+
+def test_pack_gradient_beyond_32_bits():
+    import torch
+    import paper_2511_12056_amd as pda
+    S, H, d = 700_001, 24, 128
+    assert S * H * d > 1 << 31
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(1, S, H, d, generator=g, device="cuda")
+    dy = torch.empty(1, H, S, d, device="cuda", dtype=torch.bfloat16)
+    for h in range(H):
+        dy[:, h].normal_(generator=g)
+    dx = torch.full_like(x, float("nan"))
+    pda.pack_heads_bwd(dy, x, dx, True, 0.25)
+    for a, b in ((0, 9), (S // 2, S // 2 + 17), (S - 13, S)):
+        want = torch.empty(1, b - a, H, d, device="cuda")
+        pda.pack_heads_bwd(dy[:, :, a:b].contiguous(), x[:, a:b].contiguous(), want, True, 0.25)
+        assert torch.equal(dx[:, a:b], want)
+    assert not torch.isnan(dx).any()
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(4)
+    data, want = [], []
+    for rows, D in ((30_000, 640), (20_001, 1001)):
+        x, dy, w = (torch.randn(*s, generator=g, device="cuda") for s in ((rows, D), (rows, D), (D,)))
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        pda.layer_norm_fwd(x, w, None, y, mean, rstd)
+        data.append((dy, x, w, mean, rstd, pda.layer_norm_bwd_workspace(rows, D)))
+        want.append(pda.layer_norm_bwd(*data[-1][:5], torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)))
+    res = [[[torch.empty_like(t) for t in w] for _ in range(5)] for w in want]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(5):
+        for i in (0, 1):
+            pda.layer_norm_bwd(*data[i][:5], *res[i][rep], workspace=data[i][5], stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in (0, 1) for r in res[i] for a, b in zip(r, want[i]))
