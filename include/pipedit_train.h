@@ -44,8 +44,8 @@ extern "C" {
  *
  * Arithmetic: products of bf16 accumulated in fp32 on the matrix cores; probabilities, delta and ds in fp32, p and
  * ds rounded to bf16 only as operands of the products that sum them; gradients rounded once to bf16.
- * d must be 64 or 128, scale finite and >= 0; every tensor 16-byte aligned (lse 4).  dq, dk and dv must not overlap each
- * other or any input.  workspace: 256-byte aligned, workspace_bytes >= what pda_attn_bwd_workspace gives for the
+ * d must be 64 or 128, scale finite and >= 0; every tensor 16-byte aligned (lse 4).  dq, dk, dv and the workspace must not
+ * overlap each other or any input (inputs may share memory).  workspace: 256-byte aligned, workspace_bytes >= what pda_attn_bwd_workspace gives for the
  * same sizes on this device (with B*H == 0 or Sq == Skv == 0 nothing is done and nothing needed).
  */
 int pda_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type,
@@ -86,7 +86,7 @@ int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t
  * and a shift per sample).  Either may be NULL (1 and 0).  rows must be a multiple of groups.
  * x_type, y_type: PDA_F32 or PDA_BF16, any of the four pairs; y is rounded once.  mean and rstd [rows] fp32, for the backward
  * call; both may be NULL, not one alone.  y may be x itself if their types agree (the statistics then
- * describe what was overwritten).  Sums are fp32, the variance from the centred values.
+ * describe what was overwritten); otherwise nothing that is written may overlap anything else.  Sums are fp32, the variance from the centred values.
  * 1 <= D <= PDA_LAYER_NORM_MAX; eps finite and >= 0; x, y, weight and bias 16-byte aligned; rows == 0 is a no-op.
  */
 #define PDA_LAYER_NORM_MAX 8192
@@ -101,7 +101,7 @@ int pda_layer_norm_fwd(const void* x, int x_type, const float* weight, const flo
  *
  * dy has the type y_type, dx the type x_type (rounded once); mean and rstd are the forward call's.  dweight and dbias
  * [groups, D] fp32 are written, not added to; either may be NULL.  dx may be NULL (only the sums are wanted) and may be
- * x or dy itself if the types agree.  rows == 0 writes dweight = dbias = 0.  The sums over the rows are made in a fixed order: equal calls give equal bits.
+ * x or dy itself if the types agree; otherwise nothing that is written may overlap anything else.  rows == 0 writes dweight = dbias = 0.  The sums over the rows are made in a fixed order: equal calls give equal bits.
  * workspace: 16-byte aligned, at least what pda_layer_norm_bwd_workspace gives (NULL if that is 0, or if neither
  * dweight nor dbias is wanted).
  */

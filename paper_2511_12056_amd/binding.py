@@ -392,6 +392,15 @@ def _type_code(t, name):
     raise ValueError(f"{name}: expected fp32 or bf16, got {t.dtype}")
 
 
+def _on_current_device(*tensors):
+    """A kernel runs on the current device and would follow another device's addresses there."""
+    import torch
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"a tensor on device {t.get_device()}, the current device is {current}")
+
+
 def _workspace(nbytes: int, workspace, stream):
     """The given workspace, checked, or a new one from torch's allocator, on the stream of the call that is to use it."""
     import torch
@@ -438,6 +447,7 @@ def attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid_len: Op
     _expect(dq, bf16, (B, H, Sq, d), "dq")
     _expect(dk, bf16, (B, H, Skv, d), "dk")
     _expect(dv, bf16, (B, H, Skv, d), "dv")
+    _on_current_device(dout, q, k, v, out, lse, dq, dk, dv, workspace)
     n_v = Skv if kv_valid_len is None else int(kv_valid_len)
     if workspace is None:
         workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
@@ -467,6 +477,7 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
     st += [_view_strides(lse, 1, "lse"), _view_strides(dq, 2, "dq"), _view_strides(dk, 2, "dk")]
     if _view_strides(v, 2, "v") != st[2] or _view_strides(dv, 2, "dv") != st[6]:
         raise ValueError("k and v must share their strides, and dk and dv theirs")
+    _on_current_device(dout, q, k, v, out, lse, dq, dk, dv, workspace)
     n_v = Skv if kv_valid_len is None else int(kv_valid_len)
     if workspace is None:
         workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
@@ -512,6 +523,7 @@ def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, 
     for t, name in ((mean, "mean"), (rstd, "rstd")):
         if t is not None and (t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda):
             raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
+    _on_current_device(x, weight, bias, y, mean, rstd)
     _check(lib.pda_layer_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(bias), _ptr(y), _type_code(y, "y"), _ptr(mean), _ptr(rstd),
                                   rows, _norm_groups(D, (weight, "weight"), (bias, "bias")), D, float(eps), _stream_handle(stream)))
     return y, mean, rstd
@@ -544,6 +556,7 @@ def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace=None
         if t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda:
             raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
     groups = _norm_groups(D, (weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
+    _on_current_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
     if workspace is None:
         need = layer_norm_bwd_workspace_bytes(rows, D, groups) if dweight is not None or dbias is not None else 0
         workspace = _workspace(need, None, stream)
@@ -563,6 +576,7 @@ def pack_heads_bwd(dy, x, dx, unit_rms: bool, premul: float = 1.0, stream=None):
     if x is not None:
         _expect(x, torch.float32, (B, S, H, d), "x")
     _expect(dx, torch.float32, (B, S, H, d), "dx")
+    _on_current_device(dy, x, dx)
     _check(lib.pda_pack_heads_bwd(_ptr(dy), _ptr(x), _ptr(dx), B, S, H, d, 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
     return dx
 

@@ -1,6 +1,7 @@
 // C ABI of the training operators: argument validation and launches.
 #include <hip/hip_runtime.h>
 #include <cmath>
+#include <initializer_list>
 #include "../../include/pipedit_train.h"
 #include "attn_internal.h"
 #include "train_internal.h"
@@ -19,6 +20,18 @@ bool bad_type(int t) { return t != PDA_F32 && t != PDA_BF16; }
 bool overlap(const void* a, double na, const void* b, double nb) {
     const double x = (double)reinterpret_cast<uintptr_t>(a), y = (double)reinterpret_cast<uintptr_t>(b);
     return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+struct Range {
+    const void* p;           // null: not there
+    double bytes;
+    const char* name;
+};
+int check_apart(std::initializer_list<Range> written, std::initializer_list<Range> others) {
+    for (const Range& w : written)
+        for (const Range& x : others)
+            if (w.p && x.p && overlap(w.p, w.bytes, x.p, x.bytes)) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", w.name, x.name);
+    return PDA_OK;
 }
 
 int check_bwd_sizes(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_valid_len) {
@@ -46,21 +59,19 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
         if (!aligned(p, 16)) return report(PDA_ERR_UNSUPPORTED, "dout/q/k/v/out/dq/dk/dv must be 16-byte aligned");
     if (!aligned(lse, 4)) return report(PDA_ERR_UNSUPPORTED, "lse must be 4-byte aligned");
     const double rows_q = (double)B * H * (double)Sq, rows_k = (double)B * H * (double)Skv;
-    const struct { const void* p; double bytes; const char* name; } in[6] = {
-        {dout, rows_q * d * 2, "dout"}, {q, rows_q * d * 2, "q"}, {out, rows_q * d * (out_type == PDA_BF16 ? 2 : 4), "out"}, {lse, rows_q * 4, "lse"},
-        {k, rows_k * d * 2, "k"}, {v, rows_k * d * 2, "v"}};
-    const struct { const void* p; double bytes; const char* name; } res[3] = {{dq, rows_q * d * 2, "dq"}, {dk, rows_k * d * 2, "dk"}, {dv, rows_k * d * 2, "dv"}};
-    for (int i = 0; i < 3; ++i) {         // views may interleave: only their first elements are compared
-        const double n = compact ? res[i].bytes : (res[i].bytes > 0 ? 1 : 0);
-        for (const auto& x : in)
-            if (x.p && overlap(res[i].p, n, x.p, compact ? x.bytes : 1)) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", res[i].name, x.name);
-        for (int j = 0; j < i; ++j)
-            if (overlap(res[i].p, n, res[j].p, compact ? res[j].bytes : (res[j].bytes > 0 ? 1 : 0))) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", res[i].name, res[j].name);
-    }
+    auto size = [&](double bytes) { return compact ? bytes : (bytes > 0 ? 1 : 0); };       // views may interleave: only their first elements are compared
+    const Range rq{dq, size(rows_q * d * 2), "dq"}, rk{dk, size(rows_k * d * 2), "dk"}, rv{dv, size(rows_k * d * 2), "dv"};
+    const std::initializer_list<Range> in = {
+        {dout, size(rows_q * d * 2), "dout"}, {q, size(rows_q * d * 2), "q"}, {out, size(rows_q * d * (out_type == PDA_BF16 ? 2 : 4)), "out"},
+        {lse, size(rows_q * 4), "lse"}, {k, size(rows_k * d * 2), "k"}, {v, size(rows_k * d * 2), "v"}};
+    if ((rc = check_apart({rq, rk, rv}, in)) != PDA_OK) return rc;
+    if ((rc = check_apart({rk}, {rq})) != PDA_OK || (rc = check_apart({rv}, {rq, rk})) != PDA_OK) return rc;
     pda::AttnBwdParams p{};
     const int64_t stat_bytes = pda::bwd_stat_bytes((int64_t)B * H, Sq), given = workspace ? workspace_bytes : 0;
     if (given < stat_bytes) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, at least %lld needed", (long long)given, (long long)stat_bytes);
     if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
+    const Range ws{workspace, (double)given, "workspace"};
+    if ((rc = check_apart({ws}, in)) != PDA_OK || (rc = check_apart({ws}, {rq, rk, rv})) != PDA_OK) return rc;
     int n_cu = 0;
     hipError_t e = pda::device_cu_count(&n_cu);
     if (e != hipSuccess) return hip_error(e, "device query");
@@ -182,6 +193,10 @@ int pda_layer_norm_fwd(const void* x, int x_type, const float* weight, const flo
     if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, 16) || !aligned(bias, 16)) return report(PDA_ERR_UNSUPPORTED, "x/y/weight/bias must be 16-byte aligned");
     if (!aligned(mean, 4) || !aligned(rstd, 4)) return report(PDA_ERR_UNSUPPORTED, "mean/rstd must be 4-byte aligned");
     if ((rc = check_in_place(y, y_type, "y", x, x_type, "x", rows, D)) != PDA_OK) return rc;
+    const double param = (double)groups * D * 4, stat = (double)rows * 4;
+    const Range ry{y, row_bytes(rows, D, y_type), "y"}, rm{mean, stat, "mean"}, rr{rstd, stat, "rstd"}, rw{weight, param, "weight"}, rb{bias, param, "bias"};
+    if ((rc = check_apart({ry, rm, rr}, {rw, rb})) != PDA_OK) return rc;
+    if ((rc = check_apart({rm, rr}, {ry, {x, row_bytes(rows, D, x_type), "x"}})) != PDA_OK || (rc = check_apart({rm}, {rr})) != PDA_OK) return rc;
     pda::LayerNormParams p{};
     p.x = x; p.weight = weight; p.bias = bias; p.y = y; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.groups = groups; p.group_rows = rows / groups; p.D = D; p.eps = eps;
@@ -217,6 +232,10 @@ int pda_layer_norm_bwd(const void* dy, int y_type, const void* x, int x_type, co
         if (!aligned(mean, 4) || !aligned(rstd, 4)) return report(PDA_ERR_UNSUPPORTED, "mean/rstd must be 4-byte aligned");
         if (dx && (rc = check_in_place(dx, x_type, "dx", x, x_type, "x", rows, D)) != PDA_OK) return rc;
         if (dx && (rc = check_in_place(dx, x_type, "dx", dy, y_type, "dy", rows, D)) != PDA_OK) return rc;
+        const double param = (double)groups * D * 4, stat = (double)rows * 4;
+        const Range rx{x, row_bytes(rows, D, x_type), "x"}, ry{dy, row_bytes(rows, D, y_type), "dy"}, rd{dx, rx.bytes, "dx"}, rw{dweight, param, "dweight"}, rb{dbias, param, "dbias"};
+        const std::initializer_list<Range> in = {{weight, param, "weight"}, {mean, stat, "mean"}, {rstd, stat, "rstd"}};
+        if ((rc = check_apart({rd, rw, rb}, in)) != PDA_OK || (rc = check_apart({rw, rb}, {rx, ry, rd})) != PDA_OK || (rc = check_apart({rb}, {rw})) != PDA_OK) return rc;
         int n_cu = 0;
         const hipError_t e = pda::device_cu_count(&n_cu);
         if (e != hipSuccess) return hip_error(e, "device query");
@@ -224,6 +243,8 @@ int pda_layer_norm_bwd(const void* dy, int y_type, const void* x, int x_type, co
         if (need > 0 && (!workspace || workspace_bytes < need))
             return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", workspace ? (long long)workspace_bytes : 0LL, (long long)need);
         if (need > 0 && !aligned(workspace, 16)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 16-byte aligned");
+        const Range ws{need > 0 ? workspace : nullptr, (double)need, "workspace"};
+        if ((rc = check_apart({ws}, in)) != PDA_OK || (rc = check_apart({ws}, {rx, ry, rd, rw, rb})) != PDA_OK) return rc;
         p.group_rows = rows / groups;
         p.chunks = pda::ln_chunks(p.group_rows, groups, D, n_cu);
     }

@@ -169,3 +169,64 @@ def test_binding_checks_tensors(pda):
         pda.layer_norm_bwd(torch.zeros(4, 8), torch.zeros(4, 8), None, torch.zeros(4), torch.zeros(4), None, None, None)
     with pytest.raises(ValueError):
         pda.pack_heads_bwd(t, None, torch.zeros(1, 8, 1, 64), False)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(y=_addr(1)), "y overlaps weight"), (dict(b=_addr(3) + 1008), "y overlaps bias"), (dict(mean=_addr(0)), "mean overlaps x"),
+    (dict(rstd=_addr(3) + 1020), "rstd overlaps y"), (dict(rstd=_addr(4) + 28), "mean overlaps rstd"), (dict(mean=_addr(1) + 252), "mean overlaps weight"),
+])
+def test_layer_norm_fwd_refuses_results_over_other_tensors(pda, change, word):
+    assert _ln(pda, **change) == 1 and word in pda.last_error(), pda.last_error()
+
+
+@pytest.mark.parametrize("change,word", [         # 8 rows of 64: dy 1024 bytes, dx 2048, mean and rstd 32, the parameters 256
+    (dict(dw=_addr(2)), "dweight overlaps weight"), (dict(db=_addr(3) + 16), "dbias overlaps mean"), (dict(dw=_addr(0) + 1008), "dweight overlaps dy"),
+    (dict(db=_addr(5)), "dbias overlaps dx"), (dict(db=_addr(6) + 240), "dbias overlaps dweight"), (dict(dx=_addr(4) - 2032), "dx overlaps rstd"),
+])
+def test_layer_norm_bwd_refuses_results_over_other_tensors(pda, change, word):
+    assert _ln_bwd(pda, **change) == 1 and word in pda.last_error(), pda.last_error()
+
+
+def test_attn_bwd_refuses_a_workspace_over_a_tensor(pda):
+    for i in range(9):
+        assert _bwd(pda, ws=_addr(i), ws_bytes=1 << 20) == 1 and "workspace overlaps" in pda.last_error(), pda.last_error()
+
+
+class _Elsewhere:
+    """What the wrappers ask of a tensor, of one on device 1."""
+    is_cuda = True
+
+    def __init__(self, dtype, *shape):
+        import torch
+        self.dtype, self.shape = dtype, torch.Size(shape)
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return [int(self.shape[i + 1:].numel()) for i in range(len(self.shape))]
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return 1
+
+    def data_ptr(self):
+        raise AssertionError("its address was asked for")
+
+
+def test_tensors_of_another_device_are_refused(pda, monkeypatch):
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    bf16, fp32 = torch.bfloat16, torch.float32
+    q, lse = _Elsewhere(bf16, 1, 2, 8, 64), _Elsewhere(fp32, 1, 2, 8)
+    x, w, s = _Elsewhere(fp32, 8, 64), _Elsewhere(fp32, 64), _Elsewhere(fp32, 8)
+    for call in (lambda: pda.attn_bwd(q, q, q, q, q, lse, q, q, q, 1.0), lambda: pda.attn_bwd_strided(q, q, q, q, q, lse, q, q, q, 1.0),
+                 lambda: pda.layer_norm_fwd(x, w, w, x, s, s), lambda: pda.layer_norm_bwd(x, x, w, s, s, x, w, w),
+                 lambda: pda.pack_heads_bwd(q, None, _Elsewhere(fp32, 1, 8, 2, 64), False)):
+        with pytest.raises(ValueError, match="device 1, the current device is 0"):
+            call()
