@@ -267,3 +267,131 @@ def test_long_sequence_against_64_bits_on_the_gpu():
                 # three independent roundings of 2^-9 rms at most (operand, result, out in delta): below 2^-8 sqrt(3)
                 assert (x - w).norm() <= 2.0 ** -8 * 3 ** 0.5 * w.norm()
             assert all((x[0, h, n_v:] == 0).all() for x in got[1:])
+
+
+def _near_64_bits(got, dout, q, k, v, scale, n_v):
+    """One head: the gradients of the formulas in 64 bits on the GPU, within the roundings that pass through whole rows."""
+    import torch
+    Q, K, V, G = (x.double() for x in (q, k[:n_v], v[:n_v], dout))
+    p = torch.softmax(scale * torch.mm(Q, K.t()), dim=-1)
+    dp = torch.mm(G, V.t())
+    ds = p * (dp - (p * dp).sum(-1, keepdim=True))
+    for x, w in zip(got, (scale * torch.mm(ds, K), scale * torch.mm(ds.t(), Q), torch.mm(p.t(), G))):
+        # three independent roundings of 2^-9 rms at most (operand, result, out in delta): below 2^-8 sqrt(3)
+        assert (x[:w.shape[0]].double() - w).norm() <= 2.0 ** -8 * 3 ** 0.5 * w.norm()
+    assert all((x[n_v:] == 0).all() for x in got[1:])
+
+
+def _forward_call(B, H, Sq, Skv, d, n_v, seed):
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, k, v, dout = (torch.randn(B, H, n, d, generator=g, device="cuda").to(torch.bfloat16) for n in (Sq, Skv, Skv, Sq))
+    out, lse = torch.empty(B, H, Sq, d, device="cuda"), torch.empty(B, H, Sq, device="cuda")
+    pda.attn_fwd(q, k, v, out, lse, d ** -0.5, n_v)
+    return dout, q, k, v, out, lse
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("size", [
+    (1, 10, 9000, 600, 570),         # key blocks cut, query blocks whole
+    (1, 12, 3000, 3000, 2990),       # more blocks than compute units, the last query blocks cut
+    (2, 3, 400, 1500, 100),          # blocks of hidden keys only
+    (1, 1, 4100, 4100, 4033),        # one round, all blocks cut
+    (1, 40, 2049, 1025, 1025),       # blocks with one live row
+    (3, 30, 1600, 40, 33),           # many heads, two tiles of keys
+], ids=str)
+def test_forms_of_a_launch(size, d):
+    import torch
+    import paper_2511_12056_amd as pda
+    B, H, Sq, Skv, n_v = size
+    x = _forward_call(B, H, Sq, Skv, d, n_v, sum(size))
+    got = pda.attn_bwd(*x, *(torch.full_like(t, float("nan")) for t in x[1:4]), d ** -0.5, n_v)
+    for b, h in {(0, 0), (B - 1, H - 1), (B // 2, H // 3), (0, H // 2)}:
+        _near_64_bits([t[b, h] for t in got], *(t[b, h] for t in x[:4]), d ** -0.5, n_v)
+    assert all(torch.isfinite(t).all() for t in got)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_two_calls_at_once(d):
+    """Two streams, a workspace each, several calls on both."""
+    import torch
+    import paper_2511_12056_amd as pda
+    sizes = ((1, 4, 2500, 2500, d, 2400), (1, 2, 1111, 5000, d, 5000))
+    xs = [_forward_call(*s, seed=i) for i, s in enumerate(sizes)]
+    want = [[t.clone() for t in pda.attn_bwd(*x, *map(torch.empty_like, x[1:4]), d ** -0.5, s[5])] for x, s in zip(xs, sizes)]
+    ws = [pda.attn_bwd_workspace(*s) for s in sizes]
+    grads = [[[torch.empty_like(t) for t in x[1:4]] for _ in range(4)] for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(4):
+        for i in (0, 1):
+            pda.attn_bwd(*xs[i], *grads[i][rep], d ** -0.5, sizes[i][5], workspace=ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for rep in range(4):
+            assert all(torch.equal(a, b) for a, b in zip(grads[i][rep], want[i])), (i, rep)
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed one after the other on one stream; the workspace keeps nothing from call to call."""
+    import torch
+    import paper_2511_12056_amd as pda
+    sizes = ((1, 2, 1500, 1400, 64, 1390), (1, 3, 700, 900, 128, 900))
+    xs = [_forward_call(*s, seed=i) for i, s in enumerate(sizes)]
+    want = [[t.clone() for t in pda.attn_bwd(*x, *map(torch.empty_like, x[1:4]), s[4] ** -0.5, s[5])] for x, s in zip(xs, sizes)]
+    ws = torch.empty(max(pda.attn_bwd_workspace_bytes(*s) for s in sizes), dtype=torch.uint8, device="cuda")
+    grads = [[torch.empty_like(t) for t in x[1:4]] for x in xs]
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    torch.cuda.synchronize()
+    for g, x, to, s in zip(graphs, xs, grads, sizes):
+        with torch.cuda.graph(g):
+            pda.attn_bwd(*x, *to, s[4] ** -0.5, s[5], workspace=ws)
+    for rep in range(3):
+        for to in grads:
+            for t in to:
+                t.fill_(float("nan"))
+        ws.fill_(0xFF)                              # NaN in every float
+        for i in (rep % 2, 1 - rep % 2):
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(a, b) for a, b in zip(grads[i], want[i])), (rep, i)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_heads_that_share_keys(d):
+    """k and v of one head for all heads (stride 0): every head's own dk and dv, whose sums are the shared tensor's gradients."""
+    import torch
+    import paper_2511_12056_amd as pda
+    dout, q, k, v, out, lse = _forward_call(2, 3, 333, 210, d, 200, 5)
+    k, v = (t[:, :1].clone() for t in (k, v))
+    kk, vv = (t.expand(2, 3, 210, d).contiguous() for t in (k, v))
+    pda.attn_fwd(q, kk, vv, out, lse, d ** -0.5, 200)
+    want = pda.attn_bwd(dout, q, kk, vv, out, lse, *map(torch.empty_like, (q, kk, vv)), d ** -0.5, 200)
+    got = pda.attn_bwd_strided(dout, q, k.expand(2, 3, 210, d), v.expand(2, 3, 210, d), out, lse, *map(torch.empty_like, (q, kk, vv)), d ** -0.5, 200)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_offsets_beyond_32_bits(d):
+    """Heads 2^32 bytes and more apart, in one allocation for all tensors."""
+    import torch
+    import paper_2511_12056_amd as pda
+    S, n_v = 200, 190
+    x = _forward_call(1, 2, S, S, d, n_v, 6)
+    want = pda.attn_bwd(*x, *(torch.empty_like(t) for t in x[1:4]), d ** -0.5, n_v)
+    far = (1 << 31) + 64 * d                                     # elements
+    big = torch.empty(far + 16 * S * d, device="cuda", dtype=torch.bfloat16)
+
+    def at(i):
+        return torch.as_strided(big, (1, 2, S, d), (far, far, d, 1), i * S * d)
+    views = []
+    for i, t in enumerate(x[:4]):
+        views.append(at(i).copy_(t))
+    grads = [at(4 + i) for i in range(3)]
+    bigf = torch.empty(far + 3 * S * d, device="cuda")
+    out = torch.as_strided(bigf, (1, 2, S, d), (far, far, d, 1), 0).copy_(x[4])
+    lse = torch.as_strided(bigf, (1, 2, S), (far, far, 1), S * d).copy_(x[5])
+    pda.attn_bwd_strided(*views, out, lse, *grads, d ** -0.5, n_v)
+    assert all(torch.equal(a, b) for a, b in zip(grads, want))
