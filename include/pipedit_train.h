@@ -69,7 +69,7 @@ int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const v
                          int64_t kv_valid_len, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * Bytes of workspace of a pda_attn_bwd or pda_attn_bwd_strided call (host only; bytes is a HOST pointer): two floats
+ * Bytes of workspace of a pda_attn_bwd or pda_attn_bwd_strided call (host only; bytes is a HOST pointer): a counter, two floats
  * for every query row, and where the launch has few work items the partial gradients of its shares.
  * n_cu: compute units of the device (0 = ask the current device).
  */

@@ -23,12 +23,13 @@
 //     wavefronts share 64 resident rows (attn_bwd_pair_item): one has the scores, the probabilities and dV, the other dP, dS and dK or dQ.
 //     Without the phases, both wavefronts through their steps as they come, 24 x 9 600 3.80 instead of 3.40 ms.
 //   * d = 64: a wavefront has 32 resident rows to itself (attn_bwd_lone_item), so that the probabilities stay in its registers.  Pairs instead:
-//     24 x 9 600 2 146 us and now 2 058, 6 x 33 000 6 457 and 6 020, 24 x 4 797 on 4 701 559 and 545, 2 x 1 024 23.5 and 22.2.  (At d = 128 such wavefronts spill.)
+//     24 x 9 600 2 146 us and then 2 058, 6 x 33 000 6 457 and 6 020, 24 x 4 797 on 4 701 559 and 545, 2 x 1 024 23.5 and 22.2.  (At d = 128 such wavefronts spill.)
 // Rounding to bf16: P as the operand of dV and dS as the operand of dK and dQ, as in the forward call; the P in dS stays fp32 (rounded there too,
 // dq and dk are off by 0.0029 instead of 0.0024 of the largest value).
-// Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.8 ms
-// = 930 TFLOP/s (the seven products run at 1 300), 24 x 9 600 3.13 ms = 904, 1 x 9 600 157 us = 750, 24 x 16 384 on 570 461 us = 622; d = 64: 6 x 33 000
-// 6.02 ms = 695, 24 x 4 797 on 4 701 545 us = 635, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).
+// Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
+// = 956 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.07 ms = 923, 1 x 9 600 157 us = 750, 24 x 16 384 on 570
+// 449 us = 640; d = 64: 6 x 33 000 5.91 ms = 707, 24 x 4 797 on 4 701 538 us = 644, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
+// cores are busy 71 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 41 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"
@@ -56,6 +57,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
     const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     const int bh = blockIdx.y, b = bh / p.H, h = bh - b * p.H;
     if (row >= p.stat_rows) return;
+    if (row == 0 && bh == 0 && lane == 0) *p.counter = 0;      // for the kernel that follows
     float sum = 0.f;
     if (row < p.Sq) {
         const u32x4 g = *reinterpret_cast<const u32x4*>(p.dout + (int64_t)b * p.do_bs + (int64_t)h * p.do_hs + row * D + lane * 8);
@@ -94,7 +96,8 @@ constexpr int kBwdExchange = 64 * kBwdTile * 4;          // bytes of the probabi
 constexpr int bwd_tile_bytes(int d) { return kBwdTile * d * 2; }
 constexpr int bwd_stat_base(int d) { return kBwdRing * 2 * bwd_tile_bytes(d); }
 constexpr int bwd_p_base(int d) { return bwd_stat_base(d) + kBwdRing * 256; }
-constexpr int bwd_smem(int d) { return bwd_p_base(d) + 4 * kBwdExchange; }
+constexpr int bwd_next_base(int d) { return bwd_p_base(d) + 4 * kBwdExchange; }      // two places for the next item's number
+constexpr int bwd_smem(int d) { return bwd_next_base(d) + 16; }
 
 // 4 bytes per lane from global memory straight into LDS (see lds_dma16).
 __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsigned lds_addr) {
@@ -161,15 +164,16 @@ __device__ __forceinline__ bf16x8 read_tr(unsigned at) {
 //   2  first: probabilities of step t, into LDS for the other (vector)   second: sums of dK or dQ of step t - 1, dP of step t (matrix)
 // One block of resident rows against the streamed tiles [t0, t1).  part: where the sums go in fp32 if other work items have the
 // block's other tiles (dQ, or dK and behind it dV: kBwdRows * D floats each, in the order of the accumulator registers), else null.
-template <int D, bool KEYS>
-__device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
+// claim: called once by all wavefronts when none reads the tiles any more.
+template <int D, bool KEYS, typename F>
+__device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int wave, int bh, int64_t row0, int t0, int t1, float* part, F&& claim) {
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32;
     constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2);
     constexpr int CPW = TILE / 4096;                           // chunks of 1 KB of a tile that a fetching wavefront brings
     constexpr int PF = 3;                                      // operand fragments read ahead
     extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
     const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))bwd_smem_;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), pair = wave & 3;
+    const int pair = wave & 3;
     const int lane = opaque_lane(), li = lane & 31, lh = lane >> 5;
     const bool second = wave >= 4;
     const int b = bh / p.H, h = bh - b * p.H;
@@ -431,6 +435,7 @@ __device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int b
     }
 
     // ---- results
+    claim();
     if (!KEYS && !second) return;
     if (part) {
         f32x4* to = reinterpret_cast<f32x4*>(part + (KEYS && !second ? kBwdRows * D : 0)) + pair * (2 * NDB * 4 * 64) + opaque_lane();
@@ -465,16 +470,17 @@ __device__ __forceinline__ T* uniform(T* p) {
 // on a SIMD the second is half a step behind the first.
 constexpr int kLoneRing = 4;            // tile buffers per streamed tensor
 constexpr int lone_stat_base(int d) { return kLoneRing * 2 * bwd_tile_bytes(d); }
-constexpr int lone_smem(int d) { return lone_stat_base(d) + kLoneRing * 256; }
+constexpr int lone_next_base(int d) { return lone_stat_base(d) + kLoneRing * 256; }
+constexpr int lone_smem(int d) { return lone_next_base(d) + 16; }
 
-template <int D, bool KEYS>
-__device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
+template <int D, bool KEYS, typename F>
+__device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int wave, int bh, int64_t row0, int t0, int t1, float* part, F&& claim) {
     constexpr int G = D / 8, NKK = D / 16, NDB = D / 32, R = kLoneRing;
     constexpr int TILE = bwd_tile_bytes(D), RPC = 1024 / (D * 2), CPW = TILE / 4096;
     constexpr int NF = 8;                                      // operand fragments under way
     extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
     const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))bwd_smem_;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), quarter = wave & 3;
+    const int quarter = wave & 3;
     const int lane = opaque_lane(), li = lane & 31, lh = lane >> 5;
     const bool second = wave >= 4;                             // the wavefronts that run a phase behind
     const int b = bh / p.H, h = bh - b * p.H;
@@ -681,6 +687,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int b
     }
 
     // ---- results
+    claim();
     static_for<0, KEYS ? 2 : 1>([&](auto k) {
         constexpr int i = decltype(k)::value;
         if (part) {
@@ -699,43 +706,65 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int b
 
 template <int D>
 constexpr int item_smem() { return D == 128 ? bwd_smem(D) : lone_smem(D); }
-template <int D, bool KEYS>
-__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int bh, int64_t row0, int t0, int t1, float* part) {
-    if constexpr (D == 128) attn_bwd_pair_item<D, KEYS>(p, bh, row0, t0, t1, part);
-    else attn_bwd_lone_item<D, KEYS>(p, bh, row0, t0, t1, part);
+template <int D, bool KEYS, typename F>
+__device__ __forceinline__ void attn_bwd_item(const AttnBwdParams& p, int wave, int bh, int64_t row0, int t0, int t1, float* part, F&& claim) {
+    if constexpr (D == 128) attn_bwd_pair_item<D, KEYS>(p, wave, bh, row0, t0, t1, part, claim);
+    else attn_bwd_lone_item<D, KEYS>(p, wave, bh, row0, t0, t1, part, claim);
 }
 
+// A workgroup per compute unit takes items in order: item blockIdx.x, then what a counter gives it.  XCDs run at different speeds, the hardware deals a grid's
+// workgroups to them round robin, and a workgroup that goes on needs no new launch and starts on its next block while others still store.  A grid
+// of one workgroup an item instead, us: 3 x 67 576 18 896 and now 18 309, 24 x 9 600 3 139 and 3 066, 24 x 16 384 on 570 465 and 449; d = 64: 6 x 33 000
+// 6 050 and 5 913, 24 x 4 797 548 and 538.  (Each XCD with its own eighth of the items first, for its L2: 18 496, 3 084, 446, 5 892, 547.)
+// A launch with no more items than compute units has a workgroup for each and does not touch the counter.
 template <int D>
-__global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams p) {
-    const BwdPlan& w = p.plan;
-    int i = (int)blockIdx.x;
-    const int nk = w.key_blocks * w.key_parts;
-    if (i < nk) {
-        const int j = i / w.key_blocks, blk = i - j * w.key_blocks, bh = blk / w.key_per_head;
-        const int nt = (int)((p.Sq + kBwdTile - 1) / kBwdTile);
-        attn_bwd_item<D, true>(p, bh, (int64_t)(blk - bh * w.key_per_head) * kBwdRows, (int)((int64_t)nt * j / w.key_parts), (int)((int64_t)nt * (j + 1) / w.key_parts),
-                               w.key_parts > 1 ? p.parts + (int64_t)(blk * w.key_parts + j) * (2 * kBwdRows * D) : nullptr);
-        return;
-    }
-    i -= nk;
-    const int whole = w.query_blocks - w.query_cut, nq = whole + w.query_cut * w.query_parts;
-    if (i < nq) {
-        const int j = i < whole ? 0 : (i - whole) / w.query_cut, c = i - whole - j * w.query_cut;      // part j of cut block c
-        const int blk = i < whole ? i : whole + c, bh = blk / w.query_per_head, parts = i < whole ? 1 : w.query_parts;
-        const int nt = (int)((p.n_v + kBwdTile - 1) / kBwdTile);
-        attn_bwd_item<D, false>(p, bh, (int64_t)(blk - bh * w.query_per_head) * kBwdRows, (int)((int64_t)nt * j / parts), (int)((int64_t)nt * (j + 1) / parts),
-                                i < whole ? nullptr : p.parts + bwd_key_floats(w, D) + (int64_t)(c * w.query_parts + j) * (kBwdRows * D));
-        return;
-    }
-    // keys that nobody sees: zeros from the first row behind the last block of valid ones
-    i -= nq;
-    const int64_t from = (int64_t)w.key_per_head * kBwdRows, rows = p.Skv - from;
-    const int per_head = (int)((rows + kBwdRows - 1) / kBwdRows), bh = i / per_head, b = bh / p.H, h = bh - b * p.H;
-    const int64_t first = from + (int64_t)(i - bh * per_head) * kBwdRows, at = (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs + first * D;
-    const int n = (int)(p.Skv - first < kBwdRows ? p.Skv - first : kBwdRows) * (D / 8);
-    for (int x = threadIdx.x; x < n; x += 512) {
-        reinterpret_cast<u32x4*>(p.dk + at)[x] = u32x4{0, 0, 0, 0};
-        reinterpret_cast<u32x4*>(p.dv + at)[x] = u32x4{0, 0, 0, 0};
+__global__ __launch_bounds__(512, 2) void attn_bwd_kernel(const AttnBwdParams args) {
+    extern __shared__ __attribute__((aligned(256))) unsigned char bwd_smem_[];
+    using Args = const __attribute__((address_space(4))) AttnBwdParams*;
+    Args at = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    int item = (int)blockIdx.x, turn = 0;
+    for (;;) {
+        asm volatile("" : "+s"(at));                           // arguments are read where they are used, not carried through the items in registers
+        const AttnBwdParams& p = *(const AttnBwdParams*)at;
+        const BwdPlan& w = p.plan;
+        if (item >= p.items) break;
+        const int nk = w.key_blocks * w.key_parts, whole = w.query_blocks - w.query_cut, nq = whole + w.query_cut * w.query_parts;
+        int next = 0x7fffffff;
+        auto claim = [&]() __attribute__((always_inline)) {    // the next item: asked for by one lane, between two barriers of the items at the most
+            if (p.grid >= p.items) return;
+            volatile int* to = reinterpret_cast<int*>(bwd_smem_ + (D == 128 ? bwd_next_base(D) : lone_next_base(D))) + turn;
+            turn ^= 1;                                         // (a wavefront may still be reading the one before)
+            if (wave == 0 && opaque_lane() == 0) *to = p.grid + __hip_atomic_fetch_add(p.counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            next = __builtin_amdgcn_readfirstlane(*to);
+        };
+        int i = item;
+        if (i < nk) {
+            const int j = i / w.key_blocks, blk = i - j * w.key_blocks, bh = blk / w.key_per_head;
+            const int nt = (int)((p.Sq + kBwdTile - 1) / kBwdTile);
+            attn_bwd_item<D, true>(p, wave, bh, (int64_t)(blk - bh * w.key_per_head) * kBwdRows, (int)((int64_t)nt * j / w.key_parts), (int)((int64_t)nt * (j + 1) / w.key_parts),
+                                   w.key_parts > 1 ? p.parts + (int64_t)(blk * w.key_parts + j) * (2 * kBwdRows * D) : nullptr, claim);
+        } else if ((i -= nk) < nq) {
+            const int j = i < whole ? 0 : (i - whole) / w.query_cut, c = i - whole - j * w.query_cut;  // part j of cut block c
+            const int blk = i < whole ? i : whole + c, bh = blk / w.query_per_head, parts = i < whole ? 1 : w.query_parts;
+            const int nt = (int)((p.n_v + kBwdTile - 1) / kBwdTile);
+            attn_bwd_item<D, false>(p, wave, bh, (int64_t)(blk - bh * w.query_per_head) * kBwdRows, (int)((int64_t)nt * j / parts), (int)((int64_t)nt * (j + 1) / parts),
+                                    i < whole ? nullptr : p.parts + bwd_key_floats(w, D) + (int64_t)(c * w.query_parts + j) * (kBwdRows * D), claim);
+        } else {
+            // keys that nobody sees: zeros from the first row behind the last block of valid ones
+            claim();
+            i -= nq;
+            const int64_t from = (int64_t)w.key_per_head * kBwdRows, rows = p.Skv - from;
+            const int per_head = (int)((rows + kBwdRows - 1) / kBwdRows), bh = i / per_head, b = bh / p.H, h = bh - b * p.H;
+            const int64_t first = from + (int64_t)(i - bh * per_head) * kBwdRows, at = (int64_t)b * p.dkv_bs + (int64_t)h * p.dkv_hs + first * D;
+            const int n = (int)(p.Skv - first < kBwdRows ? p.Skv - first : kBwdRows) * (D / 8);
+            for (int x = wave * 64 + opaque_lane(); x < n; x += 512) {
+                reinterpret_cast<u32x4*>(p.dk + at)[x] = u32x4{0, 0, 0, 0};
+                reinterpret_cast<u32x4*>(p.dv + at)[x] = u32x4{0, 0, 0, 0};
+            }
+        }
+        item = next;
     }
 }
 
@@ -794,7 +823,7 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(const AttnBwdParams 
 }
 
 template <int D>
-static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
+static hipError_t launch_bwd(AttnBwdParams& p, hipStream_t st) {
     const int BH = p.B * p.H;
     if (p.Sq > 0) {
         constexpr int rows = 256 / (D / 8);
@@ -807,11 +836,13 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
     const BwdPlan& w = p.plan;
     const int64_t hidden = p.Skv > (int64_t)w.key_per_head * kBwdRows ? (p.Skv - (int64_t)w.key_per_head * kBwdRows + kBwdRows - 1) / kBwdRows * BH : 0;
     const int64_t items = (int64_t)w.key_blocks * w.key_parts + w.query_blocks + (int64_t)w.query_cut * (w.query_parts - 1) + hidden;
-    if (items > 0x7fffffff) return hipErrorInvalidValue;
+    if (items > 0x7fffffff - p.n_cu) return hipErrorInvalidValue;
+    p.items = (int)items;
+    p.grid = p.Sq > 0 && items > p.n_cu ? p.n_cu : p.items;
     static KernelSetup setup;
     hipError_t e = setup.ensure(reinterpret_cast<const void*>(attn_bwd_kernel<D>), item_smem<D>(), nullptr);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)items), dim3(512), item_smem<D>(), st, p);
+    hipLaunchKernelGGL(attn_bwd_kernel<D>, dim3((unsigned)p.grid), dim3(512), item_smem<D>(), st, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int64_t joins = (w.key_parts > 1 ? (int64_t)w.key_blocks * 2 : 0) + w.query_cut;
     if (joins == 0) return hipSuccess;
@@ -819,7 +850,7 @@ static hipError_t launch_bwd(const AttnBwdParams& p, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_attn_bwd(const AttnBwdParams& p, int d, hipStream_t st) {
+hipError_t launch_attn_bwd(AttnBwdParams p, int d, hipStream_t st) {
     return d == 128 ? launch_bwd<128>(p, st) : launch_bwd<64>(p, st);
 }
 

@@ -89,8 +89,10 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     p.dv = static_cast<__bf16*>(dv);
     p.Sq = Sq; p.Skv = Skv; p.n_v = n_v;
     p.stat_rows = pda::bwd_stat_rows(Sq);
-    p.stats = static_cast<float*>(workspace);
-    p.parts = p.stats + stat_bytes / 4;
+    p.counter = static_cast<int*>(workspace);
+    p.stats = static_cast<float*>(workspace) + pda::kBwdCounterBytes / 4;
+    p.parts = static_cast<float*>(workspace) + stat_bytes / 4;
+    p.n_cu = n_cu;
     p.do_bs = s.dout_batch; p.do_hs = s.dout_head;
     p.q_bs = s.q_batch; p.q_hs = s.q_head;
     p.kv_bs = s.kv_batch; p.kv_hs = s.kv_head;

@@ -135,11 +135,15 @@ struct AttnBwdParams {
     float scale, scale_log2e;
     float* parts;            // partial sums of cut blocks: the key blocks' (dk, dv of a part, part after part, block after block), the query blocks'
     BwdPlan plan;
+    int* counter;            // items taken beyond each workgroup's first; set to zero by the statistics' kernel
+    int items, grid, n_cu;   // work items, workgroups, compute units
 };
 inline int64_t bwd_stat_rows(int64_t Sq) { return (Sq + 63) / 64 * 64; }
-inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq) { return (BH * bwd_stat_rows(Sq) * 8 + 255) / 256 * 256; }
+// The counter, then the statistics.
+constexpr int64_t kBwdCounterBytes = 256;
+inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq) { return Sq == 0 ? 0 : kBwdCounterBytes + (BH * bwd_stat_rows(Sq) * 8 + 255) / 256 * 256; }
 inline int64_t bwd_workspace_bytes(const BwdPlan& w, int64_t BH, int64_t Sq, int d) { return bwd_stat_bytes(BH, Sq) + bwd_part_slots(w) * kBwdRows * d * 4; }
-hipError_t launch_attn_bwd(const AttnBwdParams& p, int d, hipStream_t st);
+hipError_t launch_attn_bwd(AttnBwdParams p, int d, hipStream_t st);
 
 // ---- layer norm (layer_norm.hip) ----------------------------------------------------------------
 struct LayerNormParams {
