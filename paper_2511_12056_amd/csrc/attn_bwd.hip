@@ -28,8 +28,8 @@
 // dq and dk are off by 0.0029 instead of 0.0024 of the largest value).
 // Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
 // = 956 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.07 ms = 923, 1 x 9 600 157 us = 750, 24 x 16 384 on 570
-// 449 us = 640; d = 64: 6 x 33 000 5.91 ms = 707, 24 x 4 797 on 4 701 538 us = 644, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
-// cores are busy 71 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 41 % in 24 x 4 797, d = 64; no bank conflicts.
+// 449 us = 640; d = 64: 6 x 33 000 5.67 ms = 737, 24 x 4 797 on 4 701 520 us = 666, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
+// cores are busy 71 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 46 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"
@@ -131,7 +131,7 @@ __device__ __forceinline__ void store_rows(__bf16* base, int64_t first, int64_t 
 }
 
 // Operand fragments of a streamed tile in LDS.  rows: 16 columns from 16 * KK on of 32 rows; tr: 16 rows from 16 * (IDX / (D / 32)) on, transposed, of the columns of
-// block IDX % (D / 32).  `at` is the lane's address in the tile (frag_rows_at, frag_tr_at); what moves it by a granule is XORed in where it is used.
+// block IDX % (D / 32) = db.  `at` is the lane's address in the tile (frag_rows_at, frag_tr_at); frag_block moves it by granules.
 template <int D>
 __device__ __forceinline__ unsigned frag_rows_at(int lane) { return (lane & 31) * (D * 2) + (((lane >> 5) ^ swz_kv<D>(lane & 31)) * 16); }
 template <int D>
@@ -148,11 +148,9 @@ __device__ __forceinline__ LDS_PTR(const unsigned char) frag_block(unsigned at) 
 template <int KK>
 __device__ __forceinline__ bf16x8 read_rows(unsigned at) { return *(LDS_PTR(const bf16x8))frag_block<KK * 32>(at); }
 template <int D, int IDX>
-__device__ __forceinline__ bf16x8 read_tr(unsigned at) {
-    constexpr int db = IDX % (D / 32), u = IDX / (D / 32);
+__device__ __forceinline__ bf16x8 read_tr(LDS_PTR(const unsigned char) x, LDS_PTR(const unsigned char) y) {      // frag_block<db * 64>, frag_block<(db * 64) ^ 32>
+    constexpr int u = IDX / (D / 32);
     static_assert(swz_kv<D>(8) == 2 && swz_kv<D>(0) == 0, "eight rows on, the granule differs in one bit");
-    LDS_PTR(const unsigned char) x = frag_block<db * 64>(at);
-    LDS_PTR(const unsigned char) y = frag_block<(db * 64) ^ 32>(at);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(x + u * 16 * (D * 2)));
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(y + (u * 16 + 8) * (D * 2)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -233,7 +231,9 @@ __device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int w
         frag[decltype(kk)::value % (PF + 1)] = read_rows<decltype(kk)::value>(rows_at + t % kBwdRing * 2 * TILE + tensor * TILE);
     };
     auto tr_frag = [&](int t, int tensor, auto idx) __attribute__((always_inline)) {
-        frag[decltype(idx)::value % (PF + 1)] = read_tr<D, decltype(idx)::value>(tr_at + t % kBwdRing * 2 * TILE + tensor * TILE);
+        constexpr int db = decltype(idx)::value % NDB;
+        const unsigned at = tr_at + t % kBwdRing * 2 * TILE + tensor * TILE;
+        frag[decltype(idx)::value % (PF + 1)] = read_tr<D, decltype(idx)::value>(frag_block<db * 64>(at), frag_block<(db * 64) ^ 32>(at));
     };
     // A pair's probabilities of a step: group a of block i, 16 bytes a lane.  Statistics of a tile's rows: four rows of group a.
     // (Addresses from a fresh lane index: they are not kept over the products.)
@@ -315,13 +315,14 @@ __device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int w
     if (!second) {
         const float c = p.scale_log2e;
         // -lse * log2 e of a step's rows, four at a time, into two fragments' registers as the last fragments go into products
-        auto read_l = [&](int t, int a) __attribute__((always_inline)) { if constexpr (KEYS) frag[a % 2] = __builtin_bit_cast(bf16x8, stat(stat_at(t), 0, a)); };
+        auto read_l = [&](unsigned at, int a) __attribute__((always_inline)) { if constexpr (KEYS) frag[a % 2] = __builtin_bit_cast(bf16x8, stat(at, 0, a)); };
         auto scores = [&](int t) __attribute__((always_inline)) {
-            products(t, 0, [&](auto n) __attribute__((always_inline)) { if constexpr (decltype(n)::value < 2) read_l(t, decltype(n)::value); });
+            const unsigned l_at = KEYS ? stat_at(t) : 0;
+            products(t, 0, [&](auto n) __attribute__((always_inline)) { if constexpr (decltype(n)::value < 2) read_l(l_at, decltype(n)::value); });
             barrier();
         };
         auto softmax = [&](int t) __attribute__((always_inline)) {
-            const unsigned to = exchange_at();
+            const unsigned to = exchange_at(), l_at = KEYS ? stat_at(t) : 0;
             const bool tail = !KEYS && (t + 1) * kBwdTile > n_str;
             // Eight groups of four values in place, each written and packed while the next one's exponentials are under way.
             static_for<0, 9>([&](auto j) {
@@ -336,7 +337,7 @@ __device__ __forceinline__ void attn_bwd_pair_item(const AttnBwdParams& p, int w
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[i][4 * a + e] = 8 * a + e >= hidden ? 0.f : s[i][4 * a + e];
                     }
-                    if constexpr (i == 1 && a < 2) read_l(t, a + 2);
+                    if constexpr (i == 1 && a < 2) read_l(l_at, a + 2);
                 }
                 if constexpr (n > 0) {
                     constexpr int a = (n - 1) / 2, i = (n - 1) % 2;
@@ -534,14 +535,19 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
         }
     };
 
-    // ---- operand fragments, number n of a matrix phase into frag[n % NF]
-    unsigned rows_at = lds0 + frag_rows_at<D>(lane), tr_at = lds0 + frag_tr_at<D>(lane);
+    // ---- operand fragments, number n of a matrix phase into frag[n % NF].  Their addresses in buffer 0 stay in registers, a phase adds its buffer to each: what a
+    // vector instruction costs here is seen in the time (a XOR for every read instead: 24 x 9 600 2 145 us and now 2 009).
     bf16x8 frag[NF];
-    auto rows_frag = [&](int t, int tensor, auto kk, auto n) __attribute__((always_inline)) {
-        frag[decltype(n)::value % NF] = read_rows<decltype(kk)::value>(rows_at + t % R * 2 * TILE + tensor * TILE);
+    unsigned rows_0[NKK], tr_0[NDB * 2], rows_at[NKK], tr_at[NDB * 2];
+    static_for<0, NKK>([&](auto k) { rows_0[decltype(k)::value] = (unsigned)(uintptr_t)frag_block<decltype(k)::value * 32>(lds0 + frag_rows_at<D>(lane)); });
+    static_for<0, NDB * 2>([&](auto k) { tr_0[decltype(k)::value] = (unsigned)(uintptr_t)frag_block<decltype(k)::value * 32>(lds0 + frag_tr_at<D>(lane)); });
+    auto rows_frag = [&](int tensor, auto kk, auto n) __attribute__((always_inline)) {
+        frag[decltype(n)::value % NF] = *(LDS_PTR(const bf16x8))((LDS_PTR(const unsigned char))(uintptr_t)rows_at[decltype(kk)::value] + tensor * TILE);
     };
-    auto tr_frag = [&](int t, int tensor, auto idx, auto n) __attribute__((always_inline)) {
-        frag[decltype(n)::value % NF] = read_tr<D, decltype(idx)::value>(tr_at + t % R * 2 * TILE + tensor * TILE);
+    auto tr_frag = [&](int tensor, auto idx, auto n) __attribute__((always_inline)) {
+        constexpr int db = decltype(idx)::value % NDB;
+        frag[decltype(n)::value % NF] = read_tr<D, decltype(idx)::value>((LDS_PTR(const unsigned char))(uintptr_t)tr_at[db * 2] + tensor * TILE,
+                                                                         (LDS_PTR(const unsigned char))(uintptr_t)tr_at[db * 2 + 1] + tensor * TILE);
     };
 
     // ---- resident rows
@@ -576,25 +582,37 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             for (int r = 0; r < 16; ++r) acc[i][db][r] = 0.f;
     const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     f32x16 s, dp;                                              // scores, then p; <dout, v>, then ds: as operands in groups 0 and 2
-    f32x4 st[2][4];                                            // -lse * log2 e and -delta of the step's rows
+    f32x4 st[4];                                               // -lse * log2 e of the step's rows
+    f32x16 delta = zero;                                       // -delta of the step's rows or of the resident row: where <dout, v> starts (added behind: 2 009 and now 1 968)
+    if constexpr (!KEYS)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) delta[e] = d_res;
 
     // Matrix phase: the sums of step t - 1 (SUMS), then the products of step t (PRODS).  Product n of the phase:
     constexpr int N_SUM = (KEYS ? 2 : 1) * 2 * NDB, N_PROD = 2 * NKK;
     auto matrix = [&](int t, auto has_sums, auto has_prods) __attribute__((always_inline)) {
         constexpr int N0 = decltype(has_sums)::value ? 0 : N_SUM, N1 = N_SUM + (decltype(has_prods)::value ? N_PROD : 0);
+        const unsigned st_at = KEYS && decltype(has_prods)::value ? lds0 + lone_stat_base(D) + t % R * 256 + (opaque_lane() >> 5) * 16 : 0;
         auto load = [&](auto j) __attribute__((always_inline)) {
             constexpr int n = decltype(j)::value;
             if constexpr (n < N_SUM) {
-                if constexpr (KEYS) tr_frag(t - 1, 1 - n % 2, std::integral_constant<int, n / 2>{}, j);       // dout for dV, q for dK
-                else tr_frag(t - 1, 0, j, j);
+                if constexpr (KEYS) tr_frag(1 - n % 2, std::integral_constant<int, n / 2>{}, j);       // dout for dV, q for dK
+                else tr_frag(0, j, j);
             } else if constexpr (n < N1) {
-                rows_frag(t, (n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM) / 2>{}, j);
-            } else if constexpr (KEYS && decltype(has_prods)::value && n < N1 + 8) {
-                constexpr int which = (n - N1) % 2, a = (n - N1) / 2;
-                const unsigned at = lds0 + lone_stat_base(D) + t % R * 256 + (opaque_lane() >> 5) * 16;
-                st[which][a] = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(at + which * 128 + 32 * a);
+                rows_frag((n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM) / 2>{}, j);
+            } else if constexpr (KEYS && decltype(has_prods)::value && n < N1 + 4) {
+                st[n - N1] = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(st_at + 32 * (n - N1));
             }
         };
+        static_for<0, NKK>([&](auto k) { rows_at[decltype(k)::value] = rows_0[decltype(k)::value] + t % R * 2 * TILE; });
+        static_for<0, NDB * 2>([&](auto k) { tr_at[decltype(k)::value] = tr_0[decltype(k)::value] + (t + R - 1) % R * 2 * TILE; });
+        if constexpr (KEYS && decltype(has_prods)::value)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const f32x4 x = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(st_at + 128 + 32 * a);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) delta[4 * a + e] = x[e];
+            }
         static_for<N0, N0 + NF - 1>([&](auto j) { load(j); });
         step();
         __builtin_amdgcn_s_setprio(1);
@@ -610,12 +628,10 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             } else {
                 constexpr int kk = (n - N_SUM) / 2;
                 if constexpr ((n - N_SUM) % 2 == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[0][kk], kk == 0 ? zero : s, 0, 0, 0);
-                else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[1][kk], kk == 0 ? zero : dp, 0, 0, 0);
+                else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[1][kk], kk == 0 ? delta : dp, 0, 0, 0);
             }
             step();
         });
-        static_for<N1 + NF - 1, N1 + 8>([&](auto j) { load(j); });
-        step();
         __builtin_amdgcn_s_setprio(0);
     };
     const float c = p.scale_log2e;
@@ -626,7 +642,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             constexpr int n = decltype(j)::value;
             if constexpr (n < 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[4 * n + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * n + e], c, KEYS ? st[0][n][e] : l_res));
+                for (int e = 0; e < 4; ++e) s[4 * n + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * n + e], c, KEYS ? st[n][e] : l_res));
                 if (tail) {
                     const int hidden = n_str - t * kBwdTile - (opaque_lane() >> 5) * 4;
 #pragma unroll
@@ -639,7 +655,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     x[e] = s[4 * a + e];
-                    y[e] = x[e] * (dp[4 * a + e] + (KEYS ? st[1][a][e] : d_res));
+                    y[e] = x[e] * dp[4 * a + e];
                 }
                 if constexpr (KEYS) {
                     s[at] = __uint_as_float(pack_bf16(x[0], x[1]));
@@ -669,7 +685,10 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
         if (second) arrived(2);
         barrier();
         for (int t = 1; t < nt; ++t) {
-            asm volatile("" : "+v"(rows_at), "+v"(tr_at));     // nothing formed from them is kept across steps
+#pragma unroll
+            for (int k = 0; k < NKK; ++k) asm volatile("" : "+v"(rows_0[k]));      // what is formed from them is not kept across steps
+#pragma unroll
+            for (int k = 0; k < 2 * NDB; ++k) asm volatile("" : "+v"(tr_0[k]));
             const int next = t + 1 + (second ? 1 : 0);
             if (KEYS && next < nt) issue(next);
             vector(t - 1);
