@@ -26,7 +26,8 @@ extern "C" {
  * from the log-sum-exp that the forward call has written; no score matrix is stored.  For every (b, h), with keys
  * j < kv_valid_len:
  *
- *     p_ij    = exp(scale * <q_i, k_j> - lse_i)                 0 in a row with lse_i = -inf (a row without keys)
+ *     p_ij    = exp(scale * <q_i, k_j> - lse_i)                 0 in a row with lse_i = -inf (a row without keys;
+ *                                                     its out is not used, its q and dout must be finite)
  *     delta_i = <dout_i, out_i>
  *     ds_ij   = p_ij * (<dout_i, v_j> - delta_i)
  *     dq_i = scale * sum_j ds_ij k_j,    dk_j = scale * sum_i ds_ij q_i,    dv_j = sum_i p_ij dout_i

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
         }
         float* to = p.stats + (bh * p.stat_rows + row / 32 * 32) * 2 + row % 32;
         to[0] = l;
-        to[32] = -sum;
+        to[32] = l == -INFINITY ? 0.f : -sum;                  // a row without keys: whatever stands in its out
     }
 }
 

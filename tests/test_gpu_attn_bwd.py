@@ -395,3 +395,55 @@ def test_offsets_beyond_32_bits(d):
     lse = torch.as_strided(bigf, (1, 2, S), (far, far, 1), S * d).copy_(x[5])
     pda.attn_bwd_strided(*views, out, lse, *grads, d ** -0.5, n_v)
     assert all(torch.equal(a, b) for a, b in zip(grads, want))
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_out_of_rows_without_keys_is_not_used(d):
+    import torch
+    p = Problem(12, 1, 2, 130, 200, d, 190)
+    p.lse[0, :, 5::7] = -float("inf")
+    want = [x.clone() for x in p.run()]
+    p.out[0, :, 5::14] = float("nan")
+    p.out[0, :, 12::14] = float("inf")
+    got = p.run()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and (got[0][0, :, 5::7] == 0).all()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,Sq,Skv,n_v", [(2, 40_001, 40_100, 0), (2, 5, 80_001, 3), (1, 0, 70_000, 0), (20_000, 1, 2, 1)])
+def test_more_items_than_compute_units_with_little_to_do(H, Sq, Skv, n_v, d):
+    """No keys, hidden keys only, no rows, one row and key a head."""
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(H)
+    q, k, v, dout = (torch.randn(1, H, n, d, generator=g, device="cuda").to(torch.bfloat16) for n in (Sq, Skv, Skv, Sq))
+    out, lse = torch.zeros(1, H, Sq, d, device="cuda"), torch.full((1, H, Sq), -float("inf"), device="cuda")
+    if n_v == 1:
+        out.copy_(v[:, :, :1])
+        lse.copy_((q.double() * k[:, :, :1].double()).sum(-1) * d ** -0.5)
+    elif n_v and Sq:
+        pda.attn_fwd(q, k, v, out, lse, d ** -0.5, n_v)
+    dq, dk, dv = pda.attn_bwd(dout, q, k, v, out, lse, *(torch.full_like(t, float("nan")) for t in (q, k, v)), d ** -0.5, n_v)
+    assert (dk[:, :, n_v:] == 0).all() and (dv[:, :, n_v:] == 0).all()
+    if n_v == 0:
+        assert (dq == 0).all()
+    elif n_v == 1:                                   # one key: p = 1; ds = 0 up to the fp32 rounding of <dout, v> and <dout, out>, d additions each
+        assert torch.equal(dv[:, :, :1], dout)
+        mag = (dout.double() * v[:, :, :1].double()).abs().sum(-1, keepdim=True)
+        for x, w in ((dq, k[:, :, :1]), (dk[:, :, :1], q)):
+            assert (x.double().abs() <= 2.0 ** -21 * d * mag * w.double().abs() * d ** -0.5).all()
+    else:
+        for h in range(H):
+            _near_64_bits([t[0, h] for t in (dq, dk, dv)], dout[0, h], q[0, h], k[0, h], v[0, h], d ** -0.5, n_v)
+
+
+def test_inputs_may_be_one_tensor():
+    import torch
+    import paper_2511_12056_amd as pda
+    for d in (64, 128):
+        x = torch.randn(1, 3, 700, d, generator=torch.Generator(device="cuda").manual_seed(d), device="cuda").to(torch.bfloat16)
+        out, lse = torch.empty_like(x), torch.empty(1, 3, 700, device="cuda")
+        pda.attn_fwd_bf16out(x, x, x, out, lse, d ** -0.5)
+        got = pda.attn_bwd(x, x, x, x, out, lse, *(torch.empty_like(x) for _ in range(3)), d ** -0.5)
+        want = pda.attn_bwd(*(x.clone() for _ in range(4)), out, lse, *(torch.empty_like(x) for _ in range(3)), d ** -0.5)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
