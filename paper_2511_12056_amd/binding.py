@@ -489,27 +489,30 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
     return dq, dk, dv
 
 
-def _norm_rows(x, name):
-    if x.dim() < 1 or not x.is_contiguous() or not x.is_cuda:
-        raise ValueError(f"{name}: expected a contiguous cuda tensor of at least one axis")
-    D = x.shape[-1]
-    return (x.numel() // D if D else 0), D
-
-
-def _norm_groups(D, *params):
-    """Groups of [D] or [groups, D] fp32 parameters (None: not wanted), which must agree."""
+def _norm_sizes(x, per_row, params):
+    """Rows, D and groups of a call.  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
+    (One function: a call on few rows is bound by host time.)"""
     import torch
-    groups = None
+    f32 = torch.float32
+    if x.dim() < 1 or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError("x: expected a contiguous cuda tensor of at least one axis")
+    D = x.shape[-1]
+    rows = x.numel() // D if D else 0
+    for t, name in per_row:
+        if t is not None and (t.dtype is not f32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
+    groups = 0
     for t, name in params:
         if t is None:
             continue
-        if t.dtype is not torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != D or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"{name}: expected contiguous cuda fp32 [{D}] or [groups, {D}], got {t.dtype} {tuple(t.shape)}")
-        n = t.shape[0] if t.dim() == 2 else 1
-        if groups not in (None, n):
+        shape = t.shape
+        n = 1 if len(shape) == 1 else shape[0] if len(shape) == 2 else -1
+        if n < 1 or t.dtype is not f32 or shape[-1] != D or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: expected contiguous cuda fp32 [{D}] or [groups, {D}], got {t.dtype} {tuple(shape)}")
+        if groups not in (0, n):
             raise ValueError(f"{name}: {n} groups, another parameter has {groups}")
         groups = n
-    return 1 if groups is None else groups
+    return rows, D, groups or 1
 
 
 def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, stream=None):
@@ -517,15 +520,11 @@ def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, 
 
     weight, bias: [D], or [groups, D] with one row for every rows/groups consecutive rows of x, or None.
     """
-    import torch
-    rows, D = _norm_rows(x, "x")
+    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (bias, "bias")))
     _expect(y, y.dtype, x.shape, "y")
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t is not None and (t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda):
-            raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
     _on_current_device(x, weight, bias, y, mean, rstd)
     _check(lib.pda_layer_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(bias), _ptr(y), _type_code(y, "y"), _ptr(mean), _ptr(rstd),
-                                  rows, _norm_groups(D, (weight, "weight"), (bias, "bias")), D, float(eps), _stream_handle(stream)))
+                                  rows, groups, D, float(eps), _stream_handle(stream)))
     return y, mean, rstd
 
 
@@ -547,15 +546,10 @@ def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace=None
 
     dx, dweight and dbias may be None; weight is None where the forward call had none.
     """
-    import torch
-    rows, D = _norm_rows(x, "x")
+    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias")))
     _expect(dy, dy.dtype, x.shape, "dy")
     if dx is not None:
         _expect(dx, x.dtype, x.shape, "dx")
-    for t, name in ((mean, "mean"), (rstd, "rstd")):
-        if t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
-    groups = _norm_groups(D, (weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
     _on_current_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
     if workspace is None:
         need = layer_norm_bwd_workspace_bytes(rows, D, groups) if dweight is not None or dbias is not None else 0

@@ -230,3 +230,18 @@ def test_tensors_of_another_device_are_refused(pda, monkeypatch):
                  lambda: pda.pack_heads_bwd(q, None, _Elsewhere(fp32, 1, 8, 2, 64), False)):
         with pytest.raises(ValueError, match="device 1, the current device is 0"):
             call()
+
+
+def test_layer_norm_parameters_that_do_not_fit(pda, monkeypatch):
+    import torch
+    f32 = torch.float32
+    x, y, s, w = _Elsewhere(f32, 8, 64), _Elsewhere(f32, 8, 64), _Elsewhere(f32, 8), _Elsewhere(f32, 64)
+    for bad in (_Elsewhere(f32, 0, 64), _Elsewhere(f32, 32), _Elsewhere(f32, 1, 1, 64), _Elsewhere(torch.bfloat16, 64), _Elsewhere(f32)):
+        with pytest.raises(ValueError, match="weight"):
+            pda.layer_norm_fwd(x, bad, None, y)
+    for call in (lambda: pda.layer_norm_fwd(x, _Elsewhere(f32, 2, 64), w, y), lambda: pda.layer_norm_bwd(y, x, _Elsewhere(f32, 2, 64), s, s, x, w, None)):
+        with pytest.raises(ValueError, match="1 groups, another parameter has 2"):
+            call()
+    for call in (lambda: pda.layer_norm_fwd(x, w, w, y, w, w), lambda: pda.layer_norm_fwd(x, w, w, y, s, _Elsewhere(torch.bfloat16, 8))):
+        with pytest.raises(ValueError, match="one entry per row"):
+            call()
