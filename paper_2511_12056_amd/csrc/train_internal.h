@@ -24,7 +24,7 @@ struct BwdPlan {
 constexpr int kBwdMaxParts = 16;
 // Steps of a block against n streamed rows.
 inline int64_t bwd_steps(int64_t n) { return (n + kBwdTile - 1) / kBwdTile; }
-// Time of an item in tenths of a query step (1 us at d = 128): a key step takes 1.2 of it, start and end of an item about six.
+// Time of an item in tenths of a query step (1.3 us at d = 128, 0.8 at 64): a key step takes 1.2 of it, start and end of an item about six.
 inline int64_t bwd_key_time(int64_t steps) { return steps * 12 + 60; }
 inline int64_t bwd_query_time(int64_t steps) { return steps * 10 + 60; }
 // Partial sums of kBwdRows rows and d columns that a plan writes and a second kernel adds: written and read at about 4 TB/s, and that
@@ -63,9 +63,11 @@ inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
 }
 // Cuts.  A launch of fewer blocks than compute units is cut so that its parts fill them in one round, key and query blocks into parts of
 // about equal time; one of more blocks has the blocks that start last cut where that ends it earlier, and its key blocks, which start
-// first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel.
-// us, uncut -> cut: d = 128: 1 x 9 600 343 -> 157, 12 x 3 000 240 -> 201, 24 x 2 048 184 -> 172, 24 x 16 384 on 570 628 -> 461, 24 x 9 600 3 329 -> 3 131,
-// 3 x 67 576 20 132 -> 18 822; d = 64: 2 x 1 024 39 -> 22, 1 x 9 600 294 -> 113, 24 x 4 797 569 -> 545, 6 x 33 000 6 891 -> 6 020.
+// first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel, 1 to 7 us
+// of host time in all.
+// us, uncut -> cut: d = 128: 1 x 9 600 343 -> 157, 12 x 3 000 240 -> 191, 24 x 2 048 184 -> 172, 24 x 16 384 on 570 628 -> 461, 24 x 9 600 3 329 -> 3 131,
+// 3 x 67 576 20 132 -> 18 822; d = 64: 2 x 1 024 39 -> 22, 1 x 9 600 294 -> 113, 24 x 4 797 569 -> 545, 6 x 33 000 6 891 -> 6 020 (all but
+// 12 x 3 000 before workgroups took their items from a counter).
 inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     BwdPlan w{};
     w.key_per_head = (int)((n_v + kBwdRows - 1) / kBwdRows);
@@ -105,9 +107,10 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     if (blocks > 64 * (int64_t)n_cu) return w;                 // nothing to gain at the end of so long a launch
     for (int k = 1; k <= max_k && (k == 1 || (int64_t)w.key_blocks * k <= 2 * (int64_t)n_cu); ++k) {
         if (k > 1) consider(k, 0, 1);
-        for (int r = 1; r <= 4; ++r) {
-            const int64_t cut = r * (int64_t)n_cu / 4;
-            for (int q = 2; q <= 4 && q <= max_q; ++q) consider(k, (int)(cut < w.query_blocks ? cut : w.query_blocks), q);
+        for (int r = k == 1 ? 1 : 4; r <= 16; r += r < 4 ? 1 : 4) {        // sixteenths of the compute units
+            const int64_t cut = r * (int64_t)n_cu / 16;
+            if (cut == 0) continue;
+            for (int q = 2; q <= (k == 1 && r <= 4 ? 8 : 4) && q <= max_q; ++q) consider(k, (int)(cut < w.query_blocks ? cut : w.query_blocks), q);
             if (cut >= w.query_blocks) break;
         }
     }
