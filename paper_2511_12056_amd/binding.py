@@ -392,13 +392,18 @@ def _type_code(t, name):
     raise ValueError(f"{name}: expected fp32 or bf16, got {t.dtype}")
 
 
+def _elsewhere(t):
+    import torch
+    return ValueError(f"a tensor on device {t.get_device()}, the current device is {torch.cuda.current_device()}")
+
+
 def _on_current_device(*tensors):
     """A kernel runs on the current device and would follow another device's addresses there."""
     import torch
     current = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != current:
-            raise ValueError(f"a tensor on device {t.get_device()}, the current device is {current}")
+            raise _elsewhere(t)
 
 
 def _workspace(nbytes: int, workspace, stream):
@@ -489,17 +494,26 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
     return dq, dk, dv
 
 
-def _norm_sizes(x, per_row, params):
-    """Rows, D and groups of a call.  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
+def _norm_sizes(x, per_row, params, others):
+    """Rows, D and groups of a call, and that all tensors are on the current device (others: of the shape of x, a workspace).  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
     (One function: a call on few rows is bound by host time.)"""
     import torch
-    f32 = torch.float32
-    if x.dim() < 1 or not x.is_contiguous() or not x.is_cuda:
+    f32, device = torch.float32, x.get_device()
+    if device < 0 or x.dim() < 1 or not x.is_contiguous():
         raise ValueError("x: expected a contiguous cuda tensor of at least one axis")
+    if device != torch.cuda.current_device():
+        raise _elsewhere(x)
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise _elsewhere(t)
     D = x.shape[-1]
     rows = x.numel() // D if D else 0
     for t, name in per_row:
-        if t is not None and (t.dtype is not f32 or t.numel() != rows or not t.is_contiguous() or not t.is_cuda):
+        if t is None:
+            continue
+        if t.get_device() != device:
+            raise _elsewhere(t)
+        if t.dtype is not f32 or t.numel() != rows or not t.is_contiguous():
             raise ValueError(f"{name}: expected contiguous cuda fp32 with one entry per row")
     groups = 0
     for t, name in params:
@@ -507,7 +521,9 @@ def _norm_sizes(x, per_row, params):
             continue
         shape = t.shape
         n = 1 if len(shape) == 1 else shape[0] if len(shape) == 2 else -1
-        if n < 1 or t.dtype is not f32 or shape[-1] != D or not t.is_contiguous() or not t.is_cuda:
+        if t.get_device() != device:
+            raise _elsewhere(t)
+        if n < 1 or t.dtype is not f32 or shape[-1] != D or not t.is_contiguous():
             raise ValueError(f"{name}: expected contiguous cuda fp32 [{D}] or [groups, {D}], got {t.dtype} {tuple(shape)}")
         if groups not in (0, n):
             raise ValueError(f"{name}: {n} groups, another parameter has {groups}")
@@ -520,9 +536,8 @@ def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, 
 
     weight, bias: [D], or [groups, D] with one row for every rows/groups consecutive rows of x, or None.
     """
-    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (bias, "bias")))
+    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (bias, "bias")), (y,))
     _expect(y, y.dtype, x.shape, "y")
-    _on_current_device(x, weight, bias, y, mean, rstd)
     _check(lib.pda_layer_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(bias), _ptr(y), _type_code(y, "y"), _ptr(mean), _ptr(rstd),
                                   rows, groups, D, float(eps), _stream_handle(stream)))
     return y, mean, rstd
@@ -546,11 +561,11 @@ def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace=None
 
     dx, dweight and dbias may be None; weight is None where the forward call had none.
     """
-    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias")))
+    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias")),
+                                  (dy, dx, workspace))
     _expect(dy, dy.dtype, x.shape, "dy")
     if dx is not None:
         _expect(dx, x.dtype, x.shape, "dx")
-    _on_current_device(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
     if workspace is None:
         need = layer_norm_bwd_workspace_bytes(rows, D, groups) if dweight is not None or dbias is not None else 0
         workspace = _workspace(need, None, stream)

@@ -195,6 +195,7 @@ def test_attn_bwd_refuses_a_workspace_over_a_tensor(pda):
 class _Elsewhere:
     """What the wrappers ask of a tensor, of one on device 1."""
     is_cuda = True
+    device = 1
 
     def __init__(self, dtype, *shape):
         import torch
@@ -213,7 +214,7 @@ class _Elsewhere:
         return self.shape.numel()
 
     def get_device(self):
-        return 1
+        return self.device
 
     def data_ptr(self):
         raise AssertionError("its address was asked for")
@@ -234,6 +235,7 @@ def test_tensors_of_another_device_are_refused(pda, monkeypatch):
 
 def test_layer_norm_parameters_that_do_not_fit(pda, monkeypatch):
     import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     f32 = torch.float32
     x, y, s, w = _Elsewhere(f32, 8, 64), _Elsewhere(f32, 8, 64), _Elsewhere(f32, 8), _Elsewhere(f32, 64)
     for bad in (_Elsewhere(f32, 0, 64), _Elsewhere(f32, 32), _Elsewhere(f32, 1, 1, 64), _Elsewhere(torch.bfloat16, 64), _Elsewhere(f32)):
