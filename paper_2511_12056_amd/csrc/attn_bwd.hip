@@ -29,7 +29,7 @@
 // Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
 // = 956 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.07 ms = 923, 1 x 9 600 157 us = 750, 24 x 16 384 on 570
 // 449 us = 640; d = 64: 6 x 33 000 5.67 ms = 737, 24 x 4 797 on 4 701 520 us = 666, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
-// cores are busy 71 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 46 % in 24 x 4 797, d = 64; no bank conflicts.
+// cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 46 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"
@@ -160,6 +160,10 @@ __device__ __forceinline__ bf16x8 read_tr(LDS_PTR(const unsigned char) x, LDS_PT
 // A step is two phases with a barrier behind each:
 //   1  first: sums of dV of step t - 1, scores of step t (matrix)     second: dS of step t - 1 (vector)
 //   2  first: probabilities of step t, into LDS for the other (vector)   second: sums of dK or dQ of step t - 1, dP of step t (matrix)
+// Phase 2 is the longer one: 64 multiply-adds and exponentials take 540 cycles beside matrix instructions, packing them 80, and writing them to LDS, four
+// wavefronts at once, 320.  (A single barrier a step and two buffers for the probabilities, each wavefront at its own pace: 24 x 9 600 3 043 us and 3 101, 12 x 3 000
+// 183 and 194.  Query items' tiles fetched by the first wavefronts, which wait in phase 1: no change.)  All launches run below the full clock: on zeros, which need
+// less power, 24 x 9 600 takes 2 362 us, 1 x 9 600 133 instead of 159.
 // One block of resident rows against the streamed tiles [t0, t1).  part: where the sums go in fp32 if other work items have the
 // block's other tiles (dQ, or dK and behind it dV: kBwdRows * D floats each, in the order of the accumulator registers), else null.
 // claim: called once by all wavefronts when none reads the tiles any more.
