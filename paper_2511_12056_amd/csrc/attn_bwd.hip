@@ -28,8 +28,8 @@
 // dq and dk are off by 0.0029 instead of 0.0024 of the largest value).
 // Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
 // = 956 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.07 ms = 923, 1 x 9 600 157 us = 750, 24 x 16 384 on 570
-// 449 us = 640; d = 64: 6 x 33 000 5.67 ms = 737, 24 x 4 797 on 4 701 520 us = 666, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
-// cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 46 % in 24 x 4 797, d = 64; no bank conflicts.
+// 449 us = 640; d = 64: 6 x 33 000 5.32 ms = 786, 24 x 4 797 on 4 701 481 us = 721, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
+// cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 53 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"
@@ -83,9 +83,18 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
             const float x = p.lse[(int64_t)b * p.l_bs + (int64_t)h * p.l_hs + row];
             l = x == -INFINITY ? -INFINITY : -x * kLog2e;
         }
-        float* to = p.stats + (bh * p.stat_rows + row / 32 * 32) * 2 + row % 32;
-        to[0] = l;
-        to[32] = l == -INFINITY ? 0.f : -sum;                  // a row without keys: whatever stands in its out
+        const float delta = l == -INFINITY ? 0.f : -sum;       // a row without keys: whatever stands in its out
+        if constexpr (D == 64) {
+            // both as sums of three bf16: operands of a product with ones (attn_bwd_lone_item).  l in units of the scores, finite in a row without keys.
+            l = l == -INFINITY ? -0x1p100f : l / p.scale_log2e;
+            auto rest = [](float x) { return x - __uint_as_float(pack_bf16(x, 0.f) << 16); };
+            const float l1 = rest(l), l2 = rest(l1), d1 = rest(delta), d2 = rest(d1);
+            *reinterpret_cast<u32x4*>(p.stats + (bh * p.stat_rows + row) * 4) = u32x4{pack_bf16(l, l1), pack_bf16(l2, delta), pack_bf16(d1, d2), 0u};
+        } else {
+            float* to = p.stats + (bh * p.stat_rows + row / 32 * 32) * 2 + row % 32;
+            to[0] = l;
+            to[32] = delta;
+        }
     }
 }
 
@@ -475,7 +484,7 @@ __device__ __forceinline__ T* uniform(T* p) {
 // on a SIMD the second is half a step behind the first.  (Matrix instructions at a higher priority: 24 x 9 600 1 873 instead of 1 855 us.)
 constexpr int kLoneRing = 4;            // tile buffers per streamed tensor
 constexpr int lone_stat_base(int d) { return kLoneRing * 2 * bwd_tile_bytes(d); }
-constexpr int lone_next_base(int d) { return lone_stat_base(d) + kLoneRing * 256; }
+constexpr int lone_next_base(int d) { return lone_stat_base(d) + kLoneRing * 512; }
 constexpr int lone_smem(int d) { return lone_next_base(d) + 16; }
 
 template <int D, bool KEYS, typename F>
@@ -493,7 +502,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
     const __bf16* dop = p.dout + (int64_t)b * p.do_bs + (int64_t)h * p.do_hs;
     const __bf16* kp = p.k + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
     const __bf16* vp = p.v + (int64_t)b * p.kv_bs + (int64_t)h * p.kv_hs;
-    const float* stats = p.stats + bh * p.stat_rows * 2 + (KEYS ? (int64_t)t0 * (2 * kBwdTile) : 0);
+    const float* stats = p.stats + bh * p.stat_rows * 4 + (KEYS ? (int64_t)t0 * (4 * kBwdTile) : 0);
     const int64_t n_res = KEYS ? p.n_v : p.Sq;
     const int n_all = (int)(KEYS ? p.Sq : p.n_v);
     const int n_str = (n_all < (int64_t)t1 * kBwdTile ? n_all : t1 * kBwdTile) - t0 * kBwdTile;        // streamed rows, counted from tile t0 on
@@ -526,13 +535,18 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
                 lds_dma16(src, (r < last ? r : last) * (D * 2) + (((l % G) ^ swz_kv<D>(r)) * 16), to + i * 4096);
             }
         }
-        if (with_stats) lds_dma4(uniform(stats + (int64_t)t * (2 * kBwdTile)), opaque_lane() * 4, __builtin_amdgcn_readfirstlane(lds0 + lone_stat_base(D) + t % R * 256));
+        if (with_stats) {
+            const float* st = uniform(stats + (int64_t)t * (4 * kBwdTile));
+            const unsigned st_to = __builtin_amdgcn_readfirstlane(lds0 + lone_stat_base(D) + t % R * 512), off = opaque_lane() * 4;
+            lds_dma4(st, off, st_to);
+            lds_dma4(st + 64, off, st_to + 256);
+        }
     };
     // what was fetched before tile t is there, tile t may be under way
     auto arrived = [&](int t) __attribute__((always_inline)) {
         step();
         if (t < nt) {
-            if (with_stats) wait_vmcnt<CPW + 1>();
+            if (with_stats) wait_vmcnt<CPW + 2>();
             else wait_vmcnt<CPW>();
         } else {
             wait_vmcnt<0>();
@@ -542,6 +556,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
     // ---- operand fragments, number n of a matrix phase into frag[n % NF].  Their addresses in buffer 0 stay in registers, a phase adds its buffer to each: what a
     // vector instruction costs here is seen in the time (a XOR for every read instead: 24 x 9 600 2 145 us and now 2 009).
     bf16x8 frag[NF];
+    const unsigned stat_0 = lds0 + lone_stat_base(D) + li * 16;
     unsigned rows_0[NKK], tr_0[NDB * 2], rows_at[NKK], tr_at[NDB * 2];
     static_for<0, NKK>([&](auto k) { rows_0[decltype(k)::value] = (unsigned)(uintptr_t)frag_block<decltype(k)::value * 32>(lds0 + frag_rows_at<D>(lane)); });
     static_for<0, NDB * 2>([&](auto k) { tr_0[decltype(k)::value] = (unsigned)(uintptr_t)frag_block<decltype(k)::value * 32>(lds0 + frag_tr_at<D>(lane)); });
@@ -566,8 +581,9 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             res[1][kk] = *reinterpret_cast<const bf16x8*>((KEYS ? vp : dop) + c * D + lh * 8 + kk * 16);
         }
         if constexpr (!KEYS) {
-            l_res = stats[(c / kBwdTile) * (2 * kBwdTile) + c % kBwdTile];
-            d_res = stats[(c / kBwdTile) * (2 * kBwdTile) + kBwdTile + c % kBwdTile];
+            const u32x4 x = *reinterpret_cast<const u32x4*>(stats + c * 4);
+            l_res = (bf16_lo(x[0]) + bf16_hi(x[0]) + bf16_lo(x[1])) * p.scale_log2e;
+            d_res = bf16_hi(x[1]) + bf16_lo(x[2]) + bf16_hi(x[2]);
         }
         __builtin_amdgcn_s_waitcnt(kWaitLoads);
         asm volatile("" : "+v"(l_res), "+v"(d_res));
@@ -586,37 +602,37 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             for (int r = 0; r < 16; ++r) acc[i][db][r] = 0.f;
     const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     f32x16 s, dp;                                              // scores, then p; <dout, v>, then ds: as operands in groups 0 and 2
-    f32x4 st[4];                                               // -lse * log2 e of the step's rows
-    f32x16 delta = zero;                                       // -delta of the step's rows or of the resident row: where <dout, v> starts (added behind: 2 009 and now 1 968)
-    if constexpr (!KEYS)
+    // What the accumulators of the products start with.  Query items: <dout, v> with -delta of the lane's row.  Key items, where rows are the accumulators'
+    // rows: a product of the statistics (k = 0 .. 2: l, 3 .. 5: -delta) and ones; read as fp32 values, four rows a lane and read, they took as much of the LDS as a
+    // tile does (24 x 9 600 1 869 us and now 1 838, 1 x 9 600 104.5 and 98.1).
+    f32x16 delta = zero;
+    bf16x8 ones[2], stat;
+    if constexpr (KEYS) {
+        const unsigned one = lh == 0 ? 0x3f80u : 0u, both = one << 16 | one;
+        ones[0] = __builtin_bit_cast(bf16x8, u32x4{both, one, 0u, 0u});
+        ones[1] = __builtin_bit_cast(bf16x8, u32x4{0u, one << 16, both, 0u});
+    } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) delta[e] = d_res;
+    }
 
     // Matrix phase: the sums of step t - 1 (SUMS), then the products of step t (PRODS).  Product n of the phase:
-    constexpr int N_SUM = (KEYS ? 2 : 1) * 2 * NDB, N_PROD = 2 * NKK;
+    constexpr int N_SUM = (KEYS ? 2 : 1) * 2 * NDB, N_PROD = 2 * NKK + (KEYS ? 2 : 0), STAT = KEYS ? 2 : 0;
     auto matrix = [&](int t, auto has_sums, auto has_prods) __attribute__((always_inline)) {
         constexpr int N0 = decltype(has_sums)::value ? 0 : N_SUM, N1 = N_SUM + (decltype(has_prods)::value ? N_PROD : 0);
-        const unsigned st_at = KEYS && decltype(has_prods)::value ? lds0 + lone_stat_base(D) + t % R * 256 + (opaque_lane() >> 5) * 16 : 0;
         auto load = [&](auto j) __attribute__((always_inline)) {
             constexpr int n = decltype(j)::value;
             if constexpr (n < N_SUM) {
                 if constexpr (KEYS) tr_frag(1 - n % 2, std::integral_constant<int, n / 2>{}, j);       // dout for dV, q for dK
                 else tr_frag(0, j, j);
+            } else if constexpr (n < N_SUM + STAT && n < N1) {
+                if constexpr (n == N_SUM) stat = *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)(stat_0 + t % R * 512);
             } else if constexpr (n < N1) {
-                rows_frag((n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM) / 2>{}, j);
-            } else if constexpr (KEYS && decltype(has_prods)::value && n < N1 + 4) {
-                st[n - N1] = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(st_at + 32 * (n - N1));
+                rows_frag((n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM - STAT) / 2>{}, j);
             }
         };
         static_for<0, NKK>([&](auto k) { rows_at[decltype(k)::value] = rows_0[decltype(k)::value] + t % R * 2 * TILE; });
         static_for<0, NDB * 2>([&](auto k) { tr_at[decltype(k)::value] = tr_0[decltype(k)::value] + (t + R - 1) % R * 2 * TILE; });
-        if constexpr (KEYS && decltype(has_prods)::value)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const f32x4 x = *(LDS_PTR(const f32x4))(LDS_PTR(const unsigned char))(uintptr_t)(st_at + 128 + 32 * a);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) delta[4 * a + e] = x[e];
-            }
         static_for<N0, N0 + NF - 1>([&](auto j) { load(j); });
         step();
         static_for<N0, N1>([&](auto j) {
@@ -629,9 +645,15 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
                 const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v, v, u, u + 1, u + 2, u + 3));
                 acc[dv][idx % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], x, acc[dv][idx % NDB], 0, 0, 0);
             } else {
-                constexpr int kk = (n - N_SUM) / 2;
-                if constexpr ((n - N_SUM) % 2 == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[0][kk], kk == 0 ? zero : s, 0, 0, 0);
-                else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[1][kk], kk == 0 ? delta : dp, 0, 0, 0);
+                constexpr int kk = (n - N_SUM - STAT) / 2;
+                if constexpr (n < N_SUM + STAT) {
+                    f32x16& x = n == N_SUM ? s : dp;
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stat, ones[n - N_SUM], zero, 0, 0, 0);
+                } else if constexpr ((n - N_SUM) % 2 == 0) {
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[0][kk], !KEYS && kk == 0 ? zero : s, 0, 0, 0);
+                } else {
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[1][kk], !KEYS && kk == 0 ? delta : dp, 0, 0, 0);
+                }
             }
             step();
         });
@@ -644,7 +666,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             constexpr int n = decltype(j)::value;
             if constexpr (n < 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[4 * n + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * n + e], c, KEYS ? st[n][e] : l_res));
+                for (int e = 0; e < 4; ++e) s[4 * n + e] = __builtin_amdgcn_exp2f(KEYS ? s[4 * n + e] * c : __builtin_fmaf(s[4 * n + e], c, l_res));
                 if (tail) {
                     const int hidden = n_str - t * kBwdTile - (opaque_lane() >> 5) * 4;
 #pragma unroll
@@ -846,6 +868,7 @@ __global__ __launch_bounds__(256) void attn_bwd_join_kernel(const AttnBwdParams 
 template <int D>
 static hipError_t launch_bwd(AttnBwdParams& p, hipStream_t st) {
     const int BH = p.B * p.H;
+    if (D == 64 && p.scale_log2e < 0x1p-64f) p.scale_log2e = 0x1p-64f;        // l is kept in units of the scores; below, every score counts for nothing
     if (p.Sq > 0) {
         constexpr int rows = 256 / (D / 8);
         const dim3 grid((unsigned)((p.stat_rows + rows - 1) / rows), (unsigned)BH);

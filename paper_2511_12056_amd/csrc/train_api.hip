@@ -67,7 +67,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     if ((rc = check_apart({rq, rk, rv}, in)) != PDA_OK) return rc;
     if ((rc = check_apart({rk}, {rq})) != PDA_OK || (rc = check_apart({rv}, {rq, rk})) != PDA_OK) return rc;
     pda::AttnBwdParams p{};
-    const int64_t stat_bytes = pda::bwd_stat_bytes((int64_t)B * H, Sq), given = workspace ? workspace_bytes : 0;
+    const int64_t stat_bytes = pda::bwd_stat_bytes((int64_t)B * H, Sq, d), given = workspace ? workspace_bytes : 0;
     if (given < stat_bytes) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, at least %lld needed", (long long)given, (long long)stat_bytes);
     if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
     const Range ws{workspace, (double)given, "workspace"};

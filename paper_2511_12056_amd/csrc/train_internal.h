@@ -128,8 +128,9 @@ struct AttnBwdParams {
     __bf16* dq;
     __bf16* dk;
     __bf16* dv;
-    float* stats;            // [B*H][stat_rows / 32][2][32]: -lse * log2(e) of 32 rows (-inf where a row has no keys and behind the last row),
-                             // -<dout, out> of the same rows (0 behind the last row)
+    float* stats;            // d = 128: [B*H][stat_rows / 32][2][32]: -lse * log2(e) of 32 rows (-inf where a row has no keys and behind the last row),
+                             // -<dout, out> of the same rows (0 there).  d = 64: [B*H][stat_rows][8] bf16, three whose sum is -lse / scale (-2^100 there),
+                             // three whose sum is -<dout, out>, two zeros
     int64_t Sq, Skv, n_v;    // query rows, key rows, valid keys
     int64_t stat_rows;       // bwd_stat_rows(Sq)
     int64_t do_bs, do_hs, q_bs, q_hs, kv_bs, kv_hs, o_bs, o_hs, l_bs, l_hs, dq_bs, dq_hs, dkv_bs, dkv_hs;
@@ -144,8 +145,8 @@ struct AttnBwdParams {
 inline int64_t bwd_stat_rows(int64_t Sq) { return (Sq + 63) / 64 * 64; }
 // The counter, then the statistics.
 constexpr int64_t kBwdCounterBytes = 256;
-inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq) { return Sq == 0 ? 0 : kBwdCounterBytes + (BH * bwd_stat_rows(Sq) * 8 + 255) / 256 * 256; }
-inline int64_t bwd_workspace_bytes(const BwdPlan& w, int64_t BH, int64_t Sq, int d) { return bwd_stat_bytes(BH, Sq) + bwd_part_slots(w) * kBwdRows * d * 4; }
+inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq, int d) { return Sq == 0 ? 0 : kBwdCounterBytes + (BH * bwd_stat_rows(Sq) * (d == 64 ? 16 : 8) + 255) / 256 * 256; }
+inline int64_t bwd_workspace_bytes(const BwdPlan& w, int64_t BH, int64_t Sq, int d) { return bwd_stat_bytes(BH, Sq, d) + bwd_part_slots(w) * kBwdRows * d * 4; }
 hipError_t launch_attn_bwd(AttnBwdParams p, int d, hipStream_t st);
 
 // ---- layer norm (layer_norm.hip) ----------------------------------------------------------------

@@ -78,7 +78,7 @@ def test_plans(plan):
         assert 1 <= kp <= 16 and 1 <= qp <= 16 and 0 <= qc <= qb and (qc > 0) == (qp > 1), case
         slots = (kb * kp * 2 if kp > 1 else 0) + qc * (qp if qc else 0)
         assert slots <= 4 * n_cu and (slots == 0) == (join == 0), case
-        stat = 256 + (BH * (-(-Sq // 64) * 64) * 8 + 255) // 256 * 256            # the counter, the statistics
+        stat = 256 + (BH * (-(-Sq // 64) * 64) * (16 if d == 64 else 8) + 255) // 256 * 256            # the counter, the statistics
         assert ws == stat + slots * 256 * d * 4, case
         assert end + join <= whole, case                                         # a cut is made where it is expected to pay
         if kb + qb <= n_cu:

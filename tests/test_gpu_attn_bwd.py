@@ -447,3 +447,36 @@ def test_inputs_may_be_one_tensor():
         got = pda.attn_bwd(x, x, x, x, out, lse, *(torch.empty_like(x) for _ in range(3)), d ** -0.5)
         want = pda.attn_bwd(*(x.clone() for _ in range(4)), out, lse, *(torch.empty_like(x) for _ in range(3)), d ** -0.5)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_log_sum_exps_far_off(d):
+    """Rows with lse = inf, or so large that no probability is left, give nothing; far from zero the probabilities keep their accuracy."""
+    import torch
+    p = Problem(13, 1, 2, 200, 260, d, 250)
+    want = [x.clone() for x in p.run()]
+    lse = p.lse.clone()
+    p.lse[0, 0, 3::5] = float("inf")
+    p.lse[0, 0, 4::5] = 1e6
+    got = p.run()
+    assert (got[0][0, 0, 3::5] == 0).all() and (got[0][0, 0, 4::5] == 0).all()
+    assert torch.equal(got[0][0, 0, 0::5], want[0][0, 0, 0::5]) and all(torch.equal(a[0, 1], b[0, 1]) for a, b in zip(got, want))
+    assert all(torch.isfinite(x).all() for x in got)
+    # one more column in q and k that adds the same to every score of a row: lse moves by up to 500, the probabilities stay
+    p.lse.copy_(lse)
+    p.q[..., d - 1] = torch.linspace(-16, 16, 200, device="cuda").to(torch.bfloat16)
+    p.k[..., d - 1] = 32.0 * (d ** 0.5 / 8)
+    q, k, v = (x.double() for x in (p.q, p.k[:, :, :250], p.v[:, :, :250]))
+    s = torch.matmul(q, k.transpose(-1, -2).contiguous()) * p.scale
+    p.lse.copy_(torch.logsumexp(s, -1))
+    p.out.copy_(torch.matmul(torch.softmax(s, -1), v))
+    assert p.lse.abs().max() > 50
+    got = p.run()
+    for h in (0, 1):
+        Q, K, V, G = q[0, h], k[0, h], v[0, h], p.dout[0, h].double()
+        pr = torch.softmax(s[0, h], -1)
+        dp = torch.mm(G, V.t().contiguous())
+        ds = pr * (dp - (pr * dp).sum(-1, keepdim=True))
+        # the bound of _near_64_bits, and 2^-22 |lse| for the exponents' rounding, which is far below it
+        for x, w in zip(got[1:], (p.scale * torch.mm(ds.t().contiguous(), Q), torch.mm(pr.t().contiguous(), G))):
+            assert (x[0, h, :250].double() - w).norm() <= 2.0 ** -8 * 3 ** 0.5 * w.norm()
