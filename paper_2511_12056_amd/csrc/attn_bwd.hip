@@ -521,7 +521,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
     // ---- loads of the streamed tiles: one tensor by either group, 1 KB chunks quarter, quarter + 4 .. of a tile (see attn_bwd_pair_item)
     const __bf16* from = (second ? (KEYS ? dop : vp) : (KEYS ? qp : kp)) + (int64_t)t0 * (kBwdTile * D);
     const unsigned whole = (quarter * RPC + lane / G) * (D * 2) + (((lane % G) ^ swz_kv<D>(quarter * RPC + lane / G)) * 16);
-    const bool with_stats = KEYS && wave == 4;
+    const bool with_stats = KEYS && (wave & 6) == 4;           // half of a tile's
     auto issue = [&](int t) __attribute__((always_inline)) {
         const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + t % R * 2 * TILE + (second ? TILE : 0) + quarter * 1024);
         const __bf16* src = uniform(from + (int64_t)t * (kBwdTile * D));
@@ -536,17 +536,14 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
             }
         }
         if (with_stats) {
-            const float* st = uniform(stats + (int64_t)t * (4 * kBwdTile));
-            const unsigned st_to = __builtin_amdgcn_readfirstlane(lds0 + lone_stat_base(D) + t % R * 512), off = opaque_lane() * 4;
-            lds_dma4(st, off, st_to);
-            lds_dma4(st + 64, off, st_to + 256);
+            lds_dma4(uniform(stats + (int64_t)t * (4 * kBwdTile) + quarter * 64), opaque_lane() * 4, __builtin_amdgcn_readfirstlane(lds0 + lone_stat_base(D) + t % R * 512 + quarter * 256));
         }
     };
     // what was fetched before tile t is there, tile t may be under way
     auto arrived = [&](int t) __attribute__((always_inline)) {
         step();
         if (t < nt) {
-            if (with_stats) wait_vmcnt<CPW + 2>();
+            if (with_stats) wait_vmcnt<CPW + 1>();
             else wait_vmcnt<CPW>();
         } else {
             wait_vmcnt<0>();
