@@ -28,7 +28,7 @@
 // dq and dk are off by 0.0029 instead of 0.0024 of the largest value).
 // Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
 // = 956 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.07 ms = 923, 1 x 9 600 157 us = 750, 24 x 16 384 on 570
-// 449 us = 640; d = 64: 6 x 33 000 5.32 ms = 786, 24 x 4 797 on 4 701 481 us = 721, 2 x 1 024 22 us = 60 (three launches, 16 steps in the longest).  The matrix
+// 449 us = 640; d = 64: 6 x 33 000 5.32 ms = 786, 24 x 4 797 on 4 701 481 us = 721, 2 x 1 024 22 us = 60 (three launches, parts of four steps).  The matrix
 // cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 53 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
         }
         const float delta = l == -INFINITY ? 0.f : -sum;       // a row without keys: whatever stands in its out
         if constexpr (D == 64) {
-            // both as sums of three bf16: operands of a product with ones (attn_bwd_lone_item).  l in units of the scores, finite in a row without keys.
+            // both as sums of three bf16 (24 bits, nothing is lost): operands of a product with ones (attn_bwd_lone_item).  l in units of the scores, finite in a row without keys.
             l = l == -INFINITY ? -0x1p100f : l / p.scale_log2e;
             auto rest = [](float x) { return x - __uint_as_float(pack_bf16(x, 0.f) << 16); };
             const float l1 = rest(l), l2 = rest(l1), d1 = rest(delta), d2 = rest(d1);
