@@ -6,8 +6,10 @@
 // each instead 119 056 x 1 536 191 -> 218 us.  Backward, a wavefront up to D = 512 only: there a thread also keeps the sums of its columns
 // over the rows, and four times the columns are four times the registers (60 000 x 2 048 bf16 394 -> 152 us with a workgroup a row).
 // A thread holds NV groups of four elements: 16 (fp32) or 8 bytes (bf16) an access, consecutive threads side by side.  Rows that are
-// not a multiple of four elements long start at any address, so there a thread takes single elements, consecutive threads side by
-// side again.
+// not a multiple of four elements long start at any address, and their accesses do too; the group that crosses the row's end is read element by element forward,
+// and backward, where the next row must not be waited for, together with the elements before it (single elements throughout instead, us, bf16: 30 000 x 1 541
+// forward 91 and now 49, backward 196 and 65; 20 000 x 4 999 backward 747 and 177; fp32 alone backward 111 and 121).  Forward, such rows of more than 1 024 elements
+// go to a workgroup (a wavefront would hold too many registers: 20 000 x 1 101 53 and 32).
 //
 // Backward, the sums over the rows (dweight, dbias): workgroup i of a group takes rows i, i + chunks, ..., so that all of them stream through
 // neighbouring rows (each through rows of its own: 5 to 25 % slower), and keeps its columns' sums in registers; they go to the workspace,
@@ -25,47 +27,72 @@ namespace pda {
 template <typename T, bool VEC, int TPR, int NV>
 struct RowIO {
     // element e of group i of thread t
-    static __device__ __forceinline__ int col(int i, int e, int t) { return VEC ? (i * TPR + t) * 4 + e : (i * 4 + e) * TPR + t; }
+    static __device__ __forceinline__ int col(int i, int e, int t) { return (i * TPR + t) * 4 + e; }
     // A thread's part of a row as it lies in memory, zeros behind the row's end.
-    using Group = std::conditional_t<!VEC || sizeof(T) == 4, f32x4, u32x2>;
+    using Group = std::conditional_t<sizeof(T) == 4, f32x4, u32x2>;
+    typedef Group Loose __attribute__((aligned(sizeof(T))));   // rows of any length start at any element
+    using Access = std::conditional_t<VEC, Group, Loose>;
+    // Elements by which group i of thread t ends behind the row's end; such a group is read from that many elements before it (rows of four elements at least).
+    static __device__ __forceinline__ int over(int c, int D) { return VEC || D < 4 || c + 4 <= D ? 0 : c + 4 - D; }
     static __device__ __forceinline__ void fetch(const T* row, int D, int t, Group (&g)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = col(i, 0, t);
-            if constexpr (VEC) {
-                g[i] = Group{};
-                if (c < D) g[i] = *reinterpret_cast<const Group*>(row + c);
-            } else {
+            g[i] = Group{};
+            if (c < D && (VEC || D >= 4)) g[i] = *reinterpret_cast<const Access*>(row + c - over(c, D));
+        }
+        if (!VEC && D < 4 && t == 0)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) g[i][e] = col(i, e, t) < D ? (float)row[col(i, e, t)] : 0.f;
+            for (int e = 0; e < 3; ++e)
+                if (e < D) {
+                    if constexpr (sizeof(T) == 4) g[0][e] = row[e];
+                    else g[0][e / 2] |= (unsigned)__builtin_bit_cast(unsigned short, row[e]) << (e % 2 * 16);
+                }
+    }
+    // What fetch has read, each element in its place (apart from it: this waits for the loads).
+    static __device__ __forceinline__ void settle(Group (&g)[NV], int D, int t) {
+        if constexpr (!VEC) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = col(i, 0, t), n = c < D ? over(c, D) : 0;
+                if constexpr (sizeof(T) == 4) {
+                    if (n & 1) g[i] = Group{g[i][1], g[i][2], g[i][3], 0.f};
+                    if (n & 2) g[i] = Group{g[i][2], g[i][3], 0.f, 0.f};
+                } else {
+                    g[i] = __builtin_bit_cast(Group, __builtin_bit_cast(uint64_t, g[i]) >> (16 * n));
+                }
             }
         }
     }
     static __device__ __forceinline__ float value(const Group (&g)[NV], int i, int e) {
-        if constexpr (std::is_same_v<Group, f32x4>) return g[i][e];
+        if constexpr (sizeof(T) == 4) return g[i][e];
         else return e % 2 ? bf16_hi(g[i][e / 2]) : bf16_lo(g[i][e / 2]);
     }
     static __device__ __forceinline__ void load(const T* row, int D, int t, float (&x)[NV][4]) {
-        Group g[NV];
-        fetch(row, D, t, g);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            const int c = col(i, 0, t);
+            Group g[1] = {Group{}};
+            if (c + (VEC ? 0 : 3) < D) g[0] = *reinterpret_cast<const Access*>(row + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[i][e] = value(g, i, e);
+            for (int e = 0; e < 4; ++e) x[i][e] = RowIO<T, VEC, TPR, 1>::value(g, 0, e);
+            if (!VEC && c < D && c + 3 >= D)                   // the row's last one to three elements
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (c + e < D) x[i][e] = (float)row[c + e];
+        }
     }
     static __device__ __forceinline__ void store(T* row, int D, int t, const float (&x)[NV][4]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if constexpr (VEC) {
-                const int c = col(i, 0, t);
-                if (c < D) {
-                    if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(f32x4{x[i][0], x[i][1], x[i][2], x[i][3]}, reinterpret_cast<f32x4*>(row + c));
-                    else __builtin_nontemporal_store(u32x2{pack_bf16(x[i][0], x[i][1]), pack_bf16(x[i][2], x[i][3])}, reinterpret_cast<u32x2*>(row + c));
-                }
-            } else {
+            const int c = col(i, 0, t);
+            if (c + (VEC ? 0 : 3) < D) {
+                if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(f32x4{x[i][0], x[i][1], x[i][2], x[i][3]}, reinterpret_cast<Access*>(row + c));
+                else __builtin_nontemporal_store(u32x2{pack_bf16(x[i][0], x[i][1]), pack_bf16(x[i][2], x[i][3])}, reinterpret_cast<Access*>(row + c));
+            } else if (!VEC && c < D) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col(i, e, t) < D) row[col(i, e, t)] = (T)x[i][e];
+                for (int e = 0; e < 3; ++e)
+                    if (c + e < D) row[c + e] = (T)x[i][e];
             }
         }
     }
@@ -147,6 +174,7 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_bwd_kernel(const L
     constexpr int RPW = ln_threads(TPR) / TPR;
     using X = RowIO<TX, VEC, TPR, NV>;
     using Y = RowIO<TY, VEC, TPR, NV>;
+    using W = RowIO<float, VEC, TPR, NV>;
     __shared__ float lds[4 * (TPR / 64)];
     int par = 0;
     __shared__ float joined[RPW > 1 ? RPW * NV * 4 * TPR : 1];
@@ -176,7 +204,17 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_bwd_kernel(const L
         const int64_t r = r0 + n;
         float x[NV][4], dy[NV][4], w[NV][4], a = 0.f, b = 0.f;
         const float mean = mean_n, rstd = rstd_n;
-        if (p.weight) RowIO<float, VEC, TPR, NV>::load(p.weight + g * D, D, t, w);
+        if (p.weight) {
+            typename W::Group wn[NV];
+            W::fetch(p.weight + g * D, D, t, wn);
+            W::settle(wn, D, t);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[i][e] = W::value(wn, i, e);
+        }
+        X::settle(xn, D, t);
+        Y::settle(yn, D, t);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -285,9 +323,12 @@ static hipError_t launch_ln(const LayerNormParams& p, hipStream_t st) {
     if (p.D <= 512) return launch_ln<BWD, TX, TY, VEC, 64, 2>(p, st);
     if constexpr (BWD) {
         if (p.D <= 1024) return launch_ln<BWD, TX, TY, VEC, 256, 1>(p, st);
-        if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 256, 2>(p, st);
     } else {
         if (p.D <= 1024) return launch_ln<BWD, TX, TY, VEC, 64, 4>(p, st);
+    }
+    if constexpr (BWD || !VEC) {
+        if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 256, 2>(p, st);
+    } else {
         if (p.D <= 1536) return launch_ln<BWD, TX, TY, VEC, 64, 6>(p, st);
         if (p.D <= 2048) return launch_ln<BWD, TX, TY, VEC, 64, 8>(p, st);
     }

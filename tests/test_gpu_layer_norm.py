@@ -312,3 +312,56 @@ def test_two_calls_at_once():
             pda.layer_norm_bwd(*data[i][:5], *res[i][rep], workspace=data[i][5], stream=streams[i])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for i in (0, 1) for r in res[i] for a, b in zip(r, want[i]))
+
+
+@pytest.mark.parametrize("xt", TYPES)
+@pytest.mark.parametrize("yt", TYPES)
+@pytest.mark.parametrize("rows,D,groups", [(4, 2, 1), (5, 3, 1), (9, 4, 3), (6, 5, 2), (8, 6, 1), (8, 7, 2), (40, 259, 2), (66, 510, 1), (35, 778, 1), (40, 1101, 2),
+                                           (23, 1541, 1), (30, 1903, 2), (14, 3001, 2), (9, 4999, 1), (5, 8190, 1)])
+def test_lengths_beside_a_group_of_four(rows, D, groups, xt, yt):
+    test_against_the_oracle(rows, D, groups, xt, yt)
+
+
+def test_in_place_beside_a_group_of_four():
+    """A row's last elements are read together with the ones before them."""
+    import torch
+    import paper_2511_12056_amd as pda
+    for D in (2, 3, 5, 6, 250, 511, 778, 1541, 3001, 4999, 8191):
+        for t in TYPES:
+            x, dy, w, b = _inputs(5, 600, D, 2, t, t)
+            y, mean, rstd = _forward(x, w, b, t)
+            z = x.clone()
+            pda.layer_norm_fwd(z, w, b, z)
+            assert torch.equal(z, y), (D, t)
+            dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+            pda.layer_norm_bwd(dy, x, w, mean, rstd, dx, dw, db)
+            for over_dy in (True, False):
+                a, g, dw2, db2 = x.clone(), dy.clone(), torch.empty_like(w), torch.empty_like(b)
+                pda.layer_norm_bwd(g, a, w, mean, rstd, g if over_dy else a, dw2, db2)
+                assert torch.equal(g if over_dy else a, dx) and torch.equal(dw2, dw) and torch.equal(db2, db), (D, t, over_dy)
+
+
+def test_lengths_beside_a_group_of_four_leave_their_surroundings():
+    """NaN in front of and behind the tensors is not read, what stands there is kept."""
+    import torch
+    import paper_2511_12056_amd as pda
+
+    def inside(x, fill):
+        big = torch.full((x.numel() + 256,), fill, device="cuda", dtype=x.dtype)
+        view = big[128:128 + x.numel()].view(x.shape)
+        view.copy_(x)
+        return big, view
+    for D in (3, 6, 509, 1541, 3001):
+        for t in TYPES:
+            x, dy, w, b = _inputs(6, 37, D, 1, t, t)
+            y, mean, rstd = _forward(x, w, b, t)
+            dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+            pda.layer_norm_bwd(dy, x, w, mean, rstd, dx, dw, db)
+            nan = [inside(v, float("nan"))[1] for v in (x, dy, w, b, mean, rstd)]
+            res = [inside(torch.zeros_like(v), 7.0) for v in (y, dx, dw, db)]
+            pda.layer_norm_fwd(nan[0], nan[2], nan[3], res[0][1])
+            pda.layer_norm_bwd(nan[1], nan[0], nan[2], nan[4], nan[5], *(v for _, v in res[1:]))
+            for (big, view), want in zip(res, (y, dx, dw, db)):
+                assert torch.equal(view, want), (D, t)
+                view.fill_(7.0)
+                assert (big == 7.0).all(), (D, t)
