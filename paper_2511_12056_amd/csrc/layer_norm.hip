@@ -1,8 +1,9 @@
 // Layer norm forward and backward over the last axis, bound by HBM: every element is read once, held in fp32 registers
 // across the sums over its row, and written once.
 //
-// A row belongs to TPR threads: a wavefront (sums over the row in registers, no barrier) or a whole workgroup (one barrier, the sums
-// of two rows alternate between two places in LDS).  Forward, a wavefront up to D = 2 048: rows x D fp32 -> bf16 with a workgroup
+// A row belongs to TPR threads: a wavefront, up to D = 64 and 128 a quarter and half of one (sums over the row in registers, no barrier), or a whole workgroup (one
+// barrier, the sums of two rows alternate between two places in LDS).  1 000 000 x 64, fp32 -> bf16, a wavefront each forward 219 us, a quarter 69, backward 228 and 125;
+// x 128 298 and 167, 275 and 247.  Forward, a wavefront up to D = 2 048: rows x D fp32 -> bf16 with a workgroup
 // each instead 119 056 x 1 536 191 -> 218 us.  Backward, a wavefront up to D = 512 only: there a thread also keeps the sums of its columns
 // over the rows, and four times the columns are four times the registers (60 000 x 2 048 bf16 394 -> 152 us with a workgroup a row).
 // A thread holds NV groups of four elements: 16 (fp32) or 8 bytes (bf16) an access, consecutive threads side by side.  Rows that are
@@ -101,8 +102,8 @@ struct RowIO {
 // Sum of (a, b) over the TPR threads of a row, in every one of them.
 template <int TPR>
 __device__ __forceinline__ void row_sum(float& a, float& b, float* lds) {
-    a = lane_sum<64>(a);
-    b = lane_sum<64>(b);
+    a = lane_sum<TPR < 64 ? TPR : 64>(a);
+    b = lane_sum<TPR < 64 ? TPR : 64>(b);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         const int w = threadIdx.x >> 6;
@@ -120,7 +121,7 @@ constexpr int ln_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 template <typename TX, typename TY, bool VEC, int TPR, int NV>
 __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_fwd_kernel(const LayerNormParams p) {
     constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
-    __shared__ float lds[4 * (TPR / 64)];
+    __shared__ float lds[TPR > 64 ? 4 * (TPR / 64) : 1];
     const int t = threadIdx.x % TPR, D = p.D;
     const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW + threadIdx.x / TPR;
     if (r >= p.rows) return;                                    // RPW > 1: no barrier follows
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(ln_threads(TPR)) void layer_norm_bwd_kernel(const L
     using X = RowIO<TX, VEC, TPR, NV>;
     using Y = RowIO<TY, VEC, TPR, NV>;
     using W = RowIO<float, VEC, TPR, NV>;
-    __shared__ float lds[4 * (TPR / 64)];
+    __shared__ float lds[TPR > 64 ? 4 * (TPR / 64) : 1];
     int par = 0;
     __shared__ float joined[RPW > 1 ? RPW * NV * 4 * TPR : 1];
     const int t = threadIdx.x % TPR, own = threadIdx.x / TPR, D = p.D;
@@ -319,6 +320,8 @@ static hipError_t launch_ln(const LayerNormParams& p, hipStream_t st) {
 
 template <bool BWD, typename TX, typename TY, bool VEC>
 static hipError_t launch_ln(const LayerNormParams& p, hipStream_t st) {
+    if (p.D <= 64) return launch_ln<BWD, TX, TY, VEC, 16, 1>(p, st);
+    if (p.D <= 128) return launch_ln<BWD, TX, TY, VEC, 32, 1>(p, st);
     if (p.D <= 256) return launch_ln<BWD, TX, TY, VEC, 64, 1>(p, st);
     if (p.D <= 512) return launch_ln<BWD, TX, TY, VEC, 64, 2>(p, st);
     if constexpr (BWD) {
