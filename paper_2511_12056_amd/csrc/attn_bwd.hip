@@ -85,11 +85,12 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
         }
         const float delta = l == -INFINITY ? 0.f : -sum;       // a row without keys: whatever stands in its out
         if constexpr (D == 64) {
-            // both as sums of three bf16 (24 bits, nothing is lost): operands of a product with ones (attn_bwd_lone_item).  l in units of the scores, finite in a row without keys.
+            // each as a sum of three bf16 (24 bits, nothing is lost), 8 bytes that are the operand of a product with ones (attn_bwd_lone_item).  l in units of
+            // the scores, finite in a row without keys.
             l = l == -INFINITY ? -0x1p100f : l / p.scale_log2e;
             auto rest = [](float x) { return x - __uint_as_float(pack_bf16(x, 0.f) << 16); };
             const float l1 = rest(l), l2 = rest(l1), d1 = rest(delta), d2 = rest(d1);
-            *reinterpret_cast<u32x4*>(p.stats + (bh * p.stat_rows + row) * 4) = u32x4{pack_bf16(l, l1), pack_bf16(l2, delta), pack_bf16(d1, d2), 0u};
+            *reinterpret_cast<u32x4*>(p.stats + (bh * p.stat_rows + row) * 4) = u32x4{pack_bf16(l, l1), pack_bf16(l2, 0.f), pack_bf16(delta, d1), pack_bf16(d2, 0.f)};
         } else {
             float* to = p.stats + (bh * p.stat_rows + row / 32 * 32) * 2 + row % 32;
             to[0] = l;
@@ -580,7 +581,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
         if constexpr (!KEYS) {
             const u32x4 x = *reinterpret_cast<const u32x4*>(stats + c * 4);
             l_res = (bf16_lo(x[0]) + bf16_hi(x[0]) + bf16_lo(x[1])) * p.scale_log2e;
-            d_res = bf16_hi(x[1]) + bf16_lo(x[2]) + bf16_hi(x[2]);
+            d_res = bf16_lo(x[2]) + bf16_hi(x[2]) + bf16_lo(x[3]);
         }
         __builtin_amdgcn_s_waitcnt(kWaitLoads);
         asm volatile("" : "+v"(l_res), "+v"(d_res));
@@ -600,14 +601,14 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
     const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     f32x16 s, dp;                                              // scores, then p; <dout, v>, then ds: as operands in groups 0 and 2
     // What the accumulators of the products start with.  Query items: <dout, v> with -delta of the lane's row.  Key items, where rows are the accumulators'
-    // rows: a product of the statistics (k = 0 .. 2: l, 3 .. 5: -delta) and ones; read as fp32 values, four rows a lane and read, they took as much of the LDS as a
-    // tile does (24 x 9 600 1 869 us and now 1 838, 1 x 9 600 104.5 and 98.1).
+    // rows: a product of the three parts of l, and one of those of -delta, with ones; read as fp32 values, four rows a lane and read, they took as much of the LDS as
+    // a tile does (24 x 9 600 1 869 us and now 1 838, 1 x 9 600 104.5 and 98.1).  Over k = 8, so that neither is in the other's product: a delta that is not
+    // finite would otherwise reach the scores, zero times NaN, and with them dv.
     f32x16 delta = zero;
-    bf16x8 ones[2], stat;
+    s16x4 ones, stat_l, stat_d;
     if constexpr (KEYS) {
-        const unsigned one = lh == 0 ? 0x3f80u : 0u, both = one << 16 | one;
-        ones[0] = __builtin_bit_cast(bf16x8, u32x4{both, one, 0u, 0u});
-        ones[1] = __builtin_bit_cast(bf16x8, u32x4{0u, one << 16, both, 0u});
+        const unsigned one = lh == 0 ? 0x3f80u : 0u;
+        ones = __builtin_bit_cast(s16x4, u32x2{one << 16 | one, one});
     } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) delta[e] = d_res;
@@ -623,7 +624,11 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
                 if constexpr (KEYS) tr_frag(1 - n % 2, std::integral_constant<int, n / 2>{}, j);       // dout for dV, q for dK
                 else tr_frag(0, j, j);
             } else if constexpr (n < N_SUM + STAT && n < N1) {
-                if constexpr (n == N_SUM) stat = *(LDS_PTR(const bf16x8))(LDS_PTR(const unsigned char))(uintptr_t)(stat_0 + t % R * 512);
+                if constexpr (n == N_SUM) {
+                    const u32x4 x = *(LDS_PTR(const u32x4))(LDS_PTR(const unsigned char))(uintptr_t)(stat_0 + t % R * 512);
+                    stat_l = __builtin_bit_cast(s16x4, u32x2{x[0], x[1]});
+                    stat_d = __builtin_bit_cast(s16x4, u32x2{x[2], x[3]});
+                }
             } else if constexpr (n < N1) {
                 rows_frag((n - N_SUM) % 2, std::integral_constant<int, (n - N_SUM - STAT) / 2>{}, j);
             }
@@ -645,7 +650,7 @@ __device__ __forceinline__ void attn_bwd_lone_item(const AttnBwdParams& p, int w
                 constexpr int kk = (n - N_SUM - STAT) / 2;
                 if constexpr (n < N_SUM + STAT) {
                     f32x16& x = n == N_SUM ? s : dp;
-                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(stat, ones[n - N_SUM], zero, 0, 0, 0);
+                    x = __builtin_amdgcn_mfma_f32_32x32x8bf16_1k(n == N_SUM ? stat_l : stat_d, ones, zero, 0, 0, 0);
                 } else if constexpr ((n - N_SUM) % 2 == 0) {
                     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[n % NF], res[0][kk], !KEYS && kk == 0 ? zero : s, 0, 0, 0);
                 } else {

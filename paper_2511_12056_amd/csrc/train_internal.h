@@ -129,8 +129,8 @@ struct AttnBwdParams {
     __bf16* dk;
     __bf16* dv;
     float* stats;            // d = 128: [B*H][stat_rows / 32][2][32]: -lse * log2(e) of 32 rows (-inf where a row has no keys and behind the last row),
-                             // -<dout, out> of the same rows (0 there).  d = 64: [B*H][stat_rows][8] bf16, three whose sum is -lse / scale (-2^100 there),
-                             // three whose sum is -<dout, out>, two zeros
+                             // -<dout, out> of the same rows (0 there).  d = 64: [B*H][stat_rows][8] bf16, three whose sum is -lse / scale (-2^100 there)
+                             // and a zero, three whose sum is -<dout, out> and a zero
     int64_t Sq, Skv, n_v;    // query rows, key rows, valid keys
     int64_t stat_rows;       // bwd_stat_rows(Sq)
     int64_t do_bs, do_hs, q_bs, q_hs, kv_bs, kv_hs, o_bs, o_hs, l_bs, l_hs, dq_bs, dq_hs, dkv_bs, dkv_hs;

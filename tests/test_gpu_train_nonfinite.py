@@ -1,0 +1,55 @@
+"""NaN and infinities in the training operators: they reach what the formulas put them in, all of it and nothing else."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _attention(d, H, S, n_v, seed):
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, k, v, dout = (torch.randn(1, H, S, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(4))
+    out, lse = torch.empty(1, H, S, d, device="cuda"), torch.empty(1, H, S, device="cuda")
+    pda.attn_fwd(q, k, v, out, lse, d ** -0.5, n_v)
+    return dout, q, k, v, out, lse
+
+
+def _gradients(x, d, n_v):
+    import torch
+    import paper_2511_12056_amd as pda
+    got = pda.attn_bwd(*x, *(torch.full_like(t, 7.0) for t in x[1:4]), d ** -0.5, n_v)
+    torch.cuda.synchronize()
+    return got
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,S,n_v", [(2, 700, 690), (30, 2500, 2410), (1, 40, 40)])      # cut blocks, whole ones, a tile and a part
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_delta_that_is_not_finite(value, H, S, n_v, d):
+    """An entry of out makes one row's delta NaN or infinite: dk of its head and the row's dq are lost, dv has no delta in it."""
+    import torch
+    x = _attention(d, H, S, n_v, S)
+    want = [t.clone() for t in _gradients(x, d, n_v)]
+    row = S // 3
+    x[4][0, -1, row, 5] = value
+    x[0][0, -1, row, 5] = 1.0
+    x[0][0, -1, row, 6] = -2.0
+    dv = _gradients((x[0], *x[1:4], torch.nan_to_num(x[4], 0.0, 0.0, 0.0), x[5]), d, n_v)[2].clone()
+    got = _gradients(x, d, n_v)
+    assert torch.equal(got[2], dv)                                         # dv: the bits of a call with another out
+    assert not torch.isfinite(got[0][0, -1, row]).any() and not torch.isfinite(got[1][0, -1, :n_v]).any()
+    rest = [r for r in range(S) if r != row]
+    assert torch.equal(got[0][0, -1, rest], want[0][0, -1, rest])
+    assert all(torch.equal(a[0, :-1], b[0, :-1]) for a, b in zip(got, want)) and (got[1][0, -1, n_v:] == 0).all()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_log_sum_exp_that_is_nan(d):
+    """The row's probabilities are NaN: its dq, and dk and dv of its head."""
+    import torch
+    x = _attention(d, 2, 300, 280, 1)
+    want = [t.clone() for t in _gradients(x, d, 280)]
+    x[5][0, 1, 77] = float("nan")
+    got = _gradients(x, d, 280)
+    assert torch.isnan(got[0][0, 1, 77]).all() and all(torch.isnan(t[0, 1, :280]).all() for t in got[1:])
+    assert all(torch.equal(a[0, 0], b[0, 0]) for a, b in zip(got, want)) and torch.equal(got[0][0, 1, :77], want[0][0, 1, :77])
