@@ -86,8 +86,9 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams
         const float delta = l == -INFINITY ? 0.f : -sum;       // a row without keys: whatever stands in its out
         if constexpr (D == 64) {
             // each as a sum of three bf16 (24 bits, nothing is lost), 8 bytes that are the operand of a product with ones (attn_bwd_lone_item).  l in units of
-            // the scores, finite in a row without keys.
-            l = l == -INFINITY ? -0x1p100f : l / p.scale_log2e;
+            // the scores, finite in a row without keys: no score comes near 2^100.
+            l /= p.scale_log2e;                                // may pass fp32's range
+            l = l < -0x1p100f ? -0x1p100f : l;                 // (NaN stays)
             auto rest = [](float x) { return x - __uint_as_float(pack_bf16(x, 0.f) << 16); };
             const float l1 = rest(l), l2 = rest(l1), d1 = rest(delta), d2 = rest(d1);
             *reinterpret_cast<u32x4*>(p.stats + (bh * p.stat_rows + row) * 4) = u32x4{pack_bf16(l, l1), pack_bf16(l2, 0.f), pack_bf16(delta, d1), pack_bf16(d2, 0.f)};

@@ -53,3 +53,20 @@ def test_log_sum_exp_that_is_nan(d):
     got = _gradients(x, d, 280)
     assert torch.isnan(got[0][0, 1, 77]).all() and all(torch.isnan(t[0, 1, :280]).all() for t in got[1:])
     assert all(torch.equal(a[0, 0], b[0, 0]) for a, b in zip(got, want)) and torch.equal(got[0][0, 1, :77], want[0][0, 1, :77])
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("scale", [0.125, 1e-6])
+def test_log_sum_exps_near_the_largest_float(scale, d):
+    """Rows whose log-sum-exp leaves no probability give nothing, however large it is (-lse log2 e, and it over the scale, pass fp32's range)."""
+    import torch
+    import paper_2511_12056_amd as pda
+    x = _attention(d, 2, 300, 280, 2)
+    call = lambda: [t.clone() for t in pda.attn_bwd(*x, *(torch.full_like(t, 7.0) for t in x[1:4]), scale, 280)]  # noqa: E731
+    x[5][0, :, 3::8] = float("inf")
+    want = call()
+    for value in (3.4e38, 2.3e38, 1e38, 1e33, 1e31, 1e7):
+        x[5][0, :, 3::8] = value
+        got = call()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), value
+        assert (got[0][0, :, 3::8] == 0).all()
