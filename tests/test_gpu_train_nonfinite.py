@@ -1,4 +1,5 @@
 """NaN and infinities in the training operators: they reach what the formulas put them in, all of it and nothing else."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +71,39 @@ def test_log_sum_exps_near_the_largest_float(scale, d):
         got = call()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), value
         assert (got[0][0, :, 3::8] == 0).all()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("where", ["x", "dy"])
+def test_pack_gradient_of_a_vector_with_nan(where, d):
+    """With unit_rms every element of the vector's gradient has <x, x> and <x, dy> in it; the other vectors keep their bits."""
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(d)
+    B, S, H = 2, 37, 3
+    x, dy = torch.randn(B, S, H, d, generator=g, device="cuda"), torch.randn(B, H, S, d, generator=g, device="cuda").to(torch.bfloat16)
+    x[0, 0, 0] = 0.0
+    want = pda.pack_heads_bwd(dy, x, torch.empty_like(x), True, 0.5).clone()
+    at = [(0, 3, 1), (1, 36, 2), (1, 0, 0)]
+    for i, (b, s, h) in enumerate(at):
+        if where == "x":
+            x[b, s, h, 7 * i] = float("nan")
+        else:
+            dy[b, h, s, 7 * i] = float("nan")
+    got = pda.pack_heads_bwd(dy, x, torch.full_like(x, 7.0), True, 0.5)
+    hit = np.zeros((B, S, H), dtype=bool)
+    for i in at:
+        hit[i] = True
+        assert torch.isnan(got[i]).all(), i
+    hit = torch.from_numpy(hit).cuda()
+    assert torch.equal(got[~hit], want[~hit]) and (got[0, 0, 0] == 0).all()
+
+
+def test_pack_gradient_of_an_infinite_element():
+    """An infinite element: x / rms(x) is NaN there, and so is the gradient."""
+    import torch
+    import paper_2511_12056_amd as pda
+    x, dy = torch.ones(1, 4, 2, 64, device="cuda"), torch.ones(1, 2, 4, 64, device="cuda", dtype=torch.bfloat16)
+    x[0, 2, 1, 9] = float("inf")
+    got = pda.pack_heads_bwd(dy, x, torch.empty_like(x), True)
+    assert torch.isnan(got[0, 2, 1, 9]) and torch.isfinite(got[0, :2]).all()
