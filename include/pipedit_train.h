@@ -47,7 +47,7 @@ extern "C" {
  * ds rounded to bf16 only as operands of the products that sum them; gradients rounded once to bf16.
  * d must be 64 or 128, scale finite and >= 0; every tensor 16-byte aligned (lse 4).  dq, dk, dv and the workspace must not
  * overlap each other or any input (inputs may share memory).  workspace: 256-byte aligned, workspace_bytes >= what pda_attn_bwd_workspace gives for the
- * same sizes on this device (with B*H == 0 or Sq == Skv == 0 nothing is done and nothing needed).
+ * same sizes and kv_valid_len, or for larger ones with PDA_ANY_LEN, on this device (with B*H == 0 or Sq == Skv == 0 nothing is done and nothing needed).
  */
 int pda_attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type,
                  const float* lse, void* dq, void* dk, void* dv,
@@ -73,7 +73,12 @@ int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const v
  * Bytes of workspace of a pda_attn_bwd or pda_attn_bwd_strided call (host only; bytes is a HOST pointer): a counter, two floats
  * for every query row, and where the launch has few work items the partial gradients of its shares.
  * n_cu: compute units of the device (0 = ask the current device).
+ *
+ * The need does not grow with the lengths: a shorter launch may be cut where a longer one is not.  kv_valid_len = PDA_ANY_LEN gives
+ * a size, of at most n_cu * d * 4 KB beside the statistics, that serves every call of the same d and of at most this B * H, Sq and
+ * Skv, with any kv_valid_len: for programs that keep one workspace for sequences or batches of several lengths.
  */
+#define PDA_ANY_LEN (-1)
 int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_valid_len, int n_cu, int64_t* bytes);
 
 /*

@@ -10,4 +10,4 @@ from .binding import (PdaError, attn_fwd, attn_fwd_base2, attn_fwd_bf16out, attn
                       plan_ragged_groups, probe_loop_rate, probe_mfma_rate, version, PDA_MAX_LOCAL_HEADS, PDA_MAX_PARTIALS, PDA_NOALLOC_MAX_SLOTS, PDA_SINK_HEAD_MAJOR,
                       PDA_SINK_TOKEN_ARRIVAL, PDA_SINK_TOKEN_FINAL)
 from .binding import (attn_bwd, attn_bwd_strided, attn_bwd_workspace, attn_bwd_workspace_bytes, layer_norm_bwd, layer_norm_bwd_workspace,  # noqa: F401
-                      layer_norm_bwd_workspace_bytes, layer_norm_fwd, pack_heads_bwd, PDA_BF16, PDA_F32, PDA_LAYER_NORM_MAX)
+                      layer_norm_bwd_workspace_bytes, layer_norm_fwd, pack_heads_bwd, PDA_ANY_LEN, PDA_BF16, PDA_F32, PDA_LAYER_NORM_MAX)

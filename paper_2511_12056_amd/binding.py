@@ -20,6 +20,7 @@ PDA_MAX_LOCAL_HEADS = 64
 PDA_SINK_HEAD_MAJOR, PDA_SINK_TOKEN_ARRIVAL, PDA_SINK_TOKEN_FINAL = 0, 1, 2
 PDA_F32, PDA_BF16 = 0, 1
 PDA_LAYER_NORM_MAX = 8192
+PDA_ANY_LEN = -1
 
 
 class AttnBwdStrides(C.Structure):
@@ -420,7 +421,8 @@ def _workspace(nbytes: int, workspace, stream):
 
 
 def attn_bwd_workspace_bytes(B: int, H: int, Sq: int, Skv: int, d: int, kv_valid_len: Optional[int] = None, n_cu: int = 0) -> int:
-    """pda_attn_bwd_workspace; n_cu = 0 asks the current device."""
+    """pda_attn_bwd_workspace; n_cu = 0 asks the current device.  kv_valid_len: None is Skv, PDA_ANY_LEN gives what serves every call of at
+    most these sizes (a call on fewer keys or rows may need more than one on all of them)."""
     n = C.c_int64(0)
     _check(lib.pda_attn_bwd_workspace(int(B), int(H), int(Sq), int(Skv), int(d), int(Skv if kv_valid_len is None else kv_valid_len),
                                       int(n_cu), C.byref(n)))
@@ -428,9 +430,10 @@ def attn_bwd_workspace_bytes(B: int, H: int, Sq: int, Skv: int, d: int, kv_valid
 
 
 def attn_bwd_workspace(B: int, H: int, Sq: int, Skv: int, d: int, kv_valid_len: Optional[int] = None):
-    """A workspace for attn_bwd calls of these sizes on the current device, for programs that keep it."""
+    """A workspace on the current device for programs that keep it: for attn_bwd calls of at most these sizes and any valid length, or with
+    kv_valid_len for calls of exactly these."""
     import torch
-    return torch.empty(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, kv_valid_len), dtype=torch.uint8, device="cuda")
+    return torch.empty(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, PDA_ANY_LEN if kv_valid_len is None else kv_valid_len), dtype=torch.uint8, device="cuda")
 
 
 def attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid_len: Optional[int] = None, workspace=None, stream=None):

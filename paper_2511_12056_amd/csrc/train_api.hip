@@ -77,7 +77,7 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     if (e != hipSuccess) return hip_error(e, "device query");
     p.plan = pda::plan_bwd(Sq, n_v, (int64_t)B * H, d, n_cu);
     const int64_t need = pda::bwd_workspace_bytes(p.plan, (int64_t)B * H, Sq, d);
-    if (given < need) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", (long long)given, (long long)need);
+    if (given < need) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed for kv_valid_len=%lld (PDA_ANY_LEN: a size for all lengths)", (long long)given, (long long)need, (long long)n_v);
     p.dout = static_cast<const __bf16*>(dout);
     p.q = static_cast<const __bf16*>(q);
     p.k = static_cast<const __bf16*>(k);
@@ -134,7 +134,8 @@ int check_in_place(const void* out, int out_type, const char* out_name, const vo
 extern "C" {
 
 int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_valid_len, int n_cu, int64_t* bytes) {
-    int rc = check_bwd_sizes(B, H, Sq, Skv, d, kv_valid_len);
+    const bool any = kv_valid_len == PDA_ANY_LEN;
+    int rc = check_bwd_sizes(B, H, Sq, Skv, d, any ? Skv : kv_valid_len);
     if (rc != PDA_OK) return rc;
     if (n_cu < 0) return report(PDA_ERR_INVALID_ARG, "n_cu=%d is negative", n_cu);
     if (!bytes) return report(PDA_ERR_INVALID_ARG, "null bytes");
@@ -146,7 +147,8 @@ int pda_attn_bwd_workspace(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t
         const hipError_t e = pda::device_cu_count(&n_cu);
         if (e != hipSuccess) return hip_error(e, "device query");
     }
-    *bytes = pda::bwd_workspace_bytes(pda::plan_bwd(Sq, kv_valid_len, (int64_t)B * H, d, n_cu), (int64_t)B * H, Sq, d);
+    const int64_t BH = (int64_t)B * H;
+    *bytes = any ? pda::bwd_workspace_bound(BH, Sq, Skv, d, n_cu) : pda::bwd_workspace_bytes(pda::plan_bwd(Sq, kv_valid_len, BH, d, n_cu), BH, Sq, d);
     return PDA_OK;
 }
 

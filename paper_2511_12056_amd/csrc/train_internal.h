@@ -147,6 +147,13 @@ inline int64_t bwd_stat_rows(int64_t Sq) { return (Sq + 63) / 64 * 64; }
 constexpr int64_t kBwdCounterBytes = 256;
 inline int64_t bwd_stat_bytes(int64_t BH, int64_t Sq, int d) { return Sq == 0 ? 0 : kBwdCounterBytes + (BH * bwd_stat_rows(Sq) * (d == 64 ? 16 : 8) + 255) / 256 * 256; }
 inline int64_t bwd_workspace_bytes(const BwdPlan& w, int64_t BH, int64_t Sq, int d) { return bwd_stat_bytes(BH, Sq, d) + bwd_part_slots(w) * kBwdRows * d * 4; }
+// Enough for every plan of at most these sizes: a plan has kBwdMaxParts parts a block and two steps a part at the least, 4 n_cu slots at the most.
+inline int64_t bwd_workspace_bound(int64_t BH, int64_t Sq, int64_t Skv, int d, int n_cu) {
+    const auto parts = [](int64_t n) { const int64_t p = bwd_steps(n) / 2; return p < 2 ? 0 : p < kBwdMaxParts ? p : kBwdMaxParts; };
+    const auto blocks = [BH](int64_t n) { return BH * ((n + kBwdRows - 1) / kBwdRows); };
+    const int64_t slots = blocks(Skv) * parts(Sq) * 2 + blocks(Sq) * parts(Skv), most = 4 * (int64_t)n_cu;
+    return bwd_stat_bytes(BH, Sq, d) + (slots < most ? slots : most) * kBwdRows * d * 4;
+}
 hipError_t launch_attn_bwd(AttnBwdParams p, int d, hipStream_t st);
 
 // ---- layer norm (layer_norm.hip) ----------------------------------------------------------------
