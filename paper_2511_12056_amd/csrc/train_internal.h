@@ -77,9 +77,13 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     w.key_parts = w.query_parts = 1;
     const int64_t sk = bwd_steps(Sq), sq = bwd_steps(n_v), blocks = (int64_t)w.key_blocks + w.query_blocks;
     if (w.key_blocks == 0 || w.query_blocks == 0) return w;
-    const int max_k = (int)(sk / 2 < kBwdMaxParts ? sk / 2 : kBwdMaxParts), max_q = (int)(sq / 2 < kBwdMaxParts ? sq / 2 : kBwdMaxParts);
+    // two steps a part at the least; one part is always a candidate, so that query blocks are cut where key blocks cannot be
+    const int max_k = (int)(sk < 4 ? 1 : sk / 2 < kBwdMaxParts ? sk / 2 : kBwdMaxParts), max_q = (int)(sq / 2 < kBwdMaxParts ? sq / 2 : kBwdMaxParts);
     BwdPlan best = w;
     int64_t best_time = bwd_end(w, Sq, n_v, n_cu);
+    // One tile of query rows and few keys: over before the host has issued another kernel (17 rows, one head, uncut and cut, us: d = 64 on 256 keys 13.7 and 16.3,
+    // 384 14.9 and 16.3, 448 16.2 and 16.3, 640 20.0 and 16.3; d = 128 on 256 keys 16.6 and 16.2, 640 28.1 and 17.4).
+    if (sk == 1 && best_time <= (d == 64 ? 190 : 120)) return w;
     auto consider = [&](int key_parts, int query_cut, int query_parts) {
         BwdPlan c = w;
         c.key_parts = key_parts;
@@ -99,6 +103,10 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
             const int64_t most = (n_cu - (int64_t)w.key_blocks * k) / w.query_blocks, even = (sq * 10 * k + sk * 12 - 1) / (sk * 12);
             const int64_t q = most < max_q ? most : max_q;
             consider(k, w.query_blocks, (int)q);
+            if (q > 1) {
+                const int64_t steps = (sq + q - 1) / q, least = (sq + steps - 1) / steps;      // the fewest parts that are as short
+                if (least < q) consider(k, w.query_blocks, (int)least);
+            }
             if (even < q) consider(k, w.query_blocks, (int)even);
             if (even - 1 < q) consider(k, w.query_blocks, (int)(even - 1));
         }

@@ -1,0 +1,36 @@
+"""Cuts of an attention gradient's launch with few query rows, and the runs that they make."""
+import pytest
+
+from tests.test_bwd_plan import plan  # noqa: F401
+
+
+def _time(p):
+    *_, end, whole, join, ws = p
+    return end + join
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("BH,n_v", [(1, 60_000), (3, 67_576), (24, 9_600), (1, 5_000), (2, 1_025)])
+def test_a_single_tile_of_query_rows_does_not_keep_the_query_blocks_whole(plan, BH, n_v, d):  # noqa: F811
+    """Key blocks against one tile cannot be cut; the query blocks, which stream every key, still can."""
+    rows = (1, 17, 31, 32, 33, 64)
+    plans = plan([(BH, Sq, n_v, d, 256) for Sq in rows])
+    for Sq, p in zip(rows, plans):
+        assert p[6] > 1 and p[5] == BH and (Sq > 32 or p[4] == 1), (Sq, p)
+    times = [_time(p) for p in plans]
+    assert times == sorted(times), times                     # fewer rows take no longer
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("size", [(1, 2, 17, 5000, 4990), (1, 1, 1, 3000, 3000), (2, 3, 32, 2100, 2055)], ids=str)
+def test_few_rows_against_many_keys(size, d):
+    import torch
+    import paper_2511_12056_amd as pda
+    from tests.test_gpu_attn_bwd import _forward_call, _near_64_bits
+    B, H, Sq, Skv, n_v = size
+    x = _forward_call(B, H, Sq, Skv, d, n_v, sum(size))
+    got = pda.attn_bwd(*x, *(torch.full_like(t, float("nan")) for t in x[1:4]), d ** -0.5, n_v)
+    for b in range(B):
+        for h in range(H):
+            _near_64_bits([t[b, h] for t in got], *(t[b, h] for t in x[:4]), d ** -0.5, n_v)
