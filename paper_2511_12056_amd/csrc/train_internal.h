@@ -118,8 +118,9 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
         for (int r = k == 1 ? 1 : 4; r <= 16; r += r < 4 ? 1 : 4) {        // sixteenths of the compute units
             const int64_t cut = r * (int64_t)n_cu / 16;
             if (cut == 0) continue;
-            for (int q = 2; q <= (k == 1 && r <= 4 ? 8 : 4) && q <= max_q; ++q) consider(k, (int)(cut < w.query_blocks ? cut : w.query_blocks), q);
-            if (cut >= w.query_blocks) break;
+            const bool all = cut >= w.query_blocks;            // few query blocks: each part of them counts
+            for (int q = 2; q <= (all ? kBwdMaxParts : k == 1 && r <= 4 ? 8 : 4) && q <= max_q; ++q) consider(k, all ? w.query_blocks : (int)cut, q);
+            if (all) break;
         }
     }
     return best;

@@ -21,9 +21,23 @@ def test_a_single_tile_of_query_rows_does_not_keep_the_query_blocks_whole(plan, 
     assert times == sorted(times), times                     # fewer rows take no longer
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("BH,Sq", [(1, 256), (1, 100), (2, 200), (8, 64), (3, 300)])
+def test_one_block_more_than_compute_units(plan, BH, Sq, d):  # noqa: F811
+    """A few query blocks end the launch on either side of as many blocks as compute units: the cuts do not become coarser there."""
+    query_blocks = BH * -(-Sq // 256)
+    fit = (256 - query_blocks) // BH                          # key blocks a head that still make one round
+    below, above = plan([(BH, Sq, fit * 256, d, 256), (BH, Sq, fit * 256 + 1, d, 256)])
+    assert below[2] + below[3] <= 256 < above[2] + above[3]
+    slots = 4 * 256 // query_blocks                           # what the partial sums allow
+    assert above[5] == query_blocks and above[6] > min(8, slots - 1), above
+    keys = -(-Sq // 32) * 12 + 60                             # the key blocks are a second round now
+    assert _time(above) <= _time(below) + keys, (below, above)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [128, 64])
-@pytest.mark.parametrize("size", [(1, 2, 17, 5000, 4990), (1, 1, 1, 3000, 3000), (2, 3, 32, 2100, 2055)], ids=str)
+@pytest.mark.parametrize("size", [(1, 2, 17, 5000, 4990), (1, 1, 1, 3000, 3000), (2, 3, 32, 2100, 2055), (1, 1, 256, 67_576, 67_500)], ids=str)
 def test_few_rows_against_many_keys(size, d):
     import torch
     import paper_2511_12056_amd as pda
