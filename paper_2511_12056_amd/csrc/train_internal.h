@@ -42,11 +42,29 @@ inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
     int64_t end = 0;
     for (const auto& j : jobs) {
         for (int64_t left = j.n; left > 0;) {
-            int g = 0;
-            for (int i = 1; i < groups; ++i)
-                if (f[i].at < f[g].at) g = i;
-            const int64_t n = f[g].units < left ? f[g].units : left, at = f[g].at + j.time;
-            left -= n;
+            int g = 0, last = 0;
+            for (int i = 1; i < groups; ++i) {
+                g = f[i].at < f[g].at ? i : g;
+                last = f[i].at > f[last].at ? i : last;
+            }
+            if (left >= n_cu && f[last].at - f[g].at <= j.time) {      // whole rounds: each unit takes one item, and all are as far apart as before
+                const int64_t rounds = left / n_cu;
+                for (int i = 0; i < groups; ++i) f[i].at += rounds * j.time;
+                if (f[last].at > end) end = f[last].at;
+                left -= rounds * n_cu;
+                continue;
+            }
+            const int64_t n = f[g].units < left ? f[g].units : left;
+            int64_t rounds = 1;                                // of the first group alone, up to the next one's time
+            if (n == f[g].units) {
+                int64_t next = f[last].at;
+                for (int i = 0; i < groups; ++i)
+                    if (i != g && f[i].at < next) next = f[i].at;
+                const int64_t reach = (next - f[g].at + j.time - 1) / j.time, most = left / n;
+                if (reach > 1) rounds = reach < most ? reach : most;
+            }
+            const int64_t at = f[g].at + rounds * j.time;
+            left -= n * rounds;
             if (at > end) end = at;
             int same = 0;
             while (same < groups && f[same].at != at) ++same;
@@ -63,8 +81,8 @@ inline int64_t bwd_end(const BwdPlan& w, int64_t Sq, int64_t n_v, int n_cu) {
 }
 // Cuts.  A launch of fewer blocks than compute units is cut so that its parts fill them in one round, key and query blocks into parts of
 // about equal time; one of more blocks has the blocks that start last cut where that ends it earlier, and its key blocks, which start
-// first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel, 1 to 7 us
-// of host time in all.
+// first, where there are few of them against many rows.  Candidates are compared by bwd_end and the time of the second kernel: 0.1 to
+// 4 us of host time in all, up to 16 where there are many query blocks against few keys.
 // us, uncut -> cut: d = 128: 1 x 9 600 343 -> 157, 12 x 3 000 240 -> 191, 24 x 2 048 184 -> 172, 24 x 16 384 on 570 628 -> 461, 24 x 9 600 3 329 -> 3 131,
 // 3 x 67 576 20 132 -> 18 822; d = 64: 2 x 1 024 39 -> 22, 1 x 9 600 294 -> 113, 24 x 4 797 569 -> 545, 6 x 33 000 6 891 -> 6 020 (all but
 // 12 x 3 000 before workgroups took their items from a counter).
@@ -76,7 +94,7 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     w.query_blocks = (int)(BH * w.query_per_head);
     w.key_parts = w.query_parts = 1;
     const int64_t sk = bwd_steps(Sq), sq = bwd_steps(n_v), blocks = (int64_t)w.key_blocks + w.query_blocks;
-    if (w.key_blocks == 0 || w.query_blocks == 0) return w;
+    if (w.key_blocks == 0 || w.query_blocks == 0 || blocks > 64 * (int64_t)n_cu) return w;      // (nothing to gain at the end of so long a launch)
     // two steps a part at the least; one part is always a candidate, so that query blocks are cut where key blocks cannot be
     const int max_k = (int)(sk < 4 ? 1 : sk / 2 < kBwdMaxParts ? sk / 2 : kBwdMaxParts), max_q = (int)(sq / 2 < kBwdMaxParts ? sq / 2 : kBwdMaxParts);
     BwdPlan best = w;
@@ -112,7 +130,6 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
         }
         return best;
     }
-    if (blocks > 64 * (int64_t)n_cu) return w;                 // nothing to gain at the end of so long a launch
     for (int k = 1; k <= max_k && (k == 1 || (int64_t)w.key_blocks * k <= 2 * (int64_t)n_cu); ++k) {
         if (k > 1) consider(k, 0, 1);
         for (int r = k == 1 ? 1 : 4; r <= 16; r += r < 4 ? 1 : 4) {        // sixteenths of the compute units

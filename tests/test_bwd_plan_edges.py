@@ -1,7 +1,32 @@
 """Cuts of an attention gradient's launch with few query rows, and the runs that they make."""
+import os
+import subprocess
+
 import pytest
 
-from tests.test_bwd_plan import plan  # noqa: F401
+from tests.test_bwd_plan import CLANG, CSRC, plan  # noqa: F401
+
+CLOCK = r"""
+#include "attn_internal.h"
+#include "train_internal.h"
+#include <chrono>
+#include <stdio.h>
+int main() {
+    long long Sq, n_v;
+    int BH;
+    while (scanf("%d %lld %lld", &BH, &Sq, &n_v) == 3) {
+        double best = 1e9;
+        volatile int sink = 0;
+        for (int rep = 0; rep < 200; ++rep) {
+            const auto a = std::chrono::steady_clock::now();
+            sink = sink + pda::plan_bwd(Sq, n_v, BH, 128, 256).key_parts;
+            const double t = std::chrono::duration<double>(std::chrono::steady_clock::now() - a).count();
+            best = t < best ? t : best;
+        }
+        printf("%.3f\n", best * 1e6);
+    }
+}
+"""
 
 
 def _time(p):
@@ -33,6 +58,21 @@ def test_one_block_more_than_compute_units(plan, BH, Sq, d):  # noqa: F811
     assert above[5] == query_blocks and above[6] > min(8, slots - 1), above
     keys = -(-Sq // 32) * 12 + 60                             # the key blocks are a second round now
     assert _time(above) <= _time(below) + keys, (below, above)
+
+
+def test_planning_takes_microseconds(tmp_path):
+    """Every call plans: a long launch is not simulated item by item, and one that is never cut not at all (these took 15 to 90 us; the limit is
+    some four times what they take now)."""
+    if not os.path.exists(CLANG):
+        pytest.skip("no ROCm clang++ here")
+    src, exe = tmp_path / "clock.cpp", tmp_path / "clock"
+    src.write_text(CLOCK)
+    subprocess.run([CLANG, "-std=c++17", "-O2", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", CSRC, str(src), "-o", str(exe)], check=True, timeout=120)
+    cases = {(60_000, 8_192, 8_192): 2, (17, 119_056, 119_056): 10, (24, 67_576, 67_576): 10, (25, 120_472, 226): 30}
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True, check=True, timeout=60).stdout.split()
+    assert len(out) == len(cases)
+    for (c, most), us in zip(cases.items(), out):
+        assert float(us) <= most, (c, us)
 
 
 @pytest.mark.gpu
