@@ -205,15 +205,17 @@ hipError_t launch_layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_b
 
 // Workgroups of a group of rows in the backward kernel: as many as a compute unit holds at once (by their registers; more would leave
 // the last round partly empty: 119 056 x 1 536 on 1 024 workgroups 334 us, on 1 280 346, on 2 048 380; 100 000 x 1 024 on 1 024 163, on 2 048 131;
-// 4 797 x 4 096 bf16 on 1 024 33.5, on 512 26.5; 4 797 x 8 192 on 1 024 63.9, on 512 49.2, on 256 42.4), each with four rows at least.  Where a wavefront has
+// 4 797 x 4 096 bf16 on 1 024 33.5, on 512 26.5; 4 797 x 8 192 on 1 024 63.9, on 512 49.2, on 256 42.4), each with four rows at least, or
+// up to D = 128 with the eight or 16 that it takes at once.  Where a wavefront has
 // rows of its own, up to D = 512, six for each of them if all compute units then have a workgroup: 9 600 x 256 with four in all 15.2 us, with 24 10.0; 1 000 x 512
 // 8.0 and 10.0.
 inline int64_t ln_chunks(int64_t group_rows, int64_t groups, int D, int n_cu) {
     const int64_t per_cu = D <= 256 ? 8 : D <= 512 ? 4 : D <= 1024 ? 8 : D <= 2048 ? 4 : D <= 4096 ? 2 : 1;
     const int64_t resident = per_cu * n_cu, want = resident / groups > 1 ? resident / groups : 1;
-    int64_t most = (group_rows + 3) / 4;
+    const int64_t least = D <= 64 ? 16 : D <= 128 ? 8 : 4;     // rows of a workgroup: what it holds at once up to D = 512
+    int64_t most = (group_rows + least - 1) / least;
     if (D <= 512) {
-        const int64_t rows = D <= 64 ? 96 : D <= 128 ? 48 : 24, each = (n_cu + groups - 1) / groups, full = (group_rows + rows - 1) / rows, few = each > full ? each : full;
+        const int64_t each = (n_cu + groups - 1) / groups, full = (group_rows + 6 * least - 1) / (6 * least), few = each > full ? each : full;
         if (few < most) most = few;
     }
     return want < most ? want : most;
