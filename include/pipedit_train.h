@@ -58,7 +58,7 @@ int pda_attn_bwd(const void* dout, const void* q, const void* k, const void* v, 
  * pda_attn_bwd on views, as pda_attn_fwd_strided: batch and head strides in ELEMENTS, rows compact (d elements
  * apart): head groups of larger tensors, query ranges, key chunks.  k and v share their strides, dk and dv theirs.
  * Strides of bf16 tensors must be multiples of 8, of an fp32 out multiples of 4, none negative; heads and
- * batches of dq, dk and dv, which are written, must not overlap.
+ * batches of dq, dk and dv, which are written, must not overlap (either axis may be the outer one).
  */
 typedef struct {
     int64_t dout_batch, dout_head, q_batch, q_head, kv_batch, kv_head, out_batch, out_head, lse_batch, lse_head;

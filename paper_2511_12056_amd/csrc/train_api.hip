@@ -44,6 +44,21 @@ int check_bwd_sizes(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_val
     return PDA_OK;
 }
 
+// The blocks of n elements at b * batch + h * head must not share any, whichever of the two axes is the outer one.
+int check_blocks(int B, int H, int64_t batch, int64_t head, int64_t n, const char* name) {
+    if (n == 0) return PDA_OK;
+    if (H > 1 && head < n) return report(PDA_ERR_INVALID_ARG, "heads of %s overlap (head stride too small)", name);
+    for (int64_t i = 1; i < B; ++i) {                          // block (0, h) against (i, 0); differences with h on the other side are larger
+        const int64_t x = i * batch;
+        if (x >= (H - 1) * head + n) break;
+        int64_t h = H > 1 ? x / head : 0;                      // the nearest ones
+        h = h < H - 1 ? h : H - 1;
+        if (x - h * head < n || (h + 1 < H && (h + 1) * head - x < n))
+            return report(PDA_ERR_INVALID_ARG, "batches of %s overlap (batch stride %lld, head stride %lld)", name, (long long)batch, (long long)head);
+    }
+    return PDA_OK;
+}
+
 int attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type, const float* lse,
              void* dq, void* dk, void* dv, int B, int H, int64_t Sq, int64_t Skv, int d, const pda_attn_bwd_strides& s, bool compact,
              float scale, int64_t n_v, void* workspace, int64_t workspace_bytes, void* stream) {
@@ -178,11 +193,7 @@ int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const v
     if ((s.dout_batch | s.dout_head | s.q_batch | s.q_head | s.kv_batch | s.kv_head | s.dq_batch | s.dq_head | s.dkv_batch | s.dkv_head) % 8 != 0)
         return report(PDA_ERR_UNSUPPORTED, "strides of bf16 tensors must be multiples of 8 elements");
     if ((s.out_batch | s.out_head) % (out_type == PDA_BF16 ? 8 : 4) != 0) return report(PDA_ERR_UNSUPPORTED, "out strides must be multiples of 16 bytes");
-    const struct { int64_t batch, head, extent; const char* name; } res[2] = {{s.dq_batch, s.dq_head, Sq * d, "dq"}, {s.dkv_batch, s.dkv_head, Skv * d, "dk/dv"}};
-    for (const auto& x : res) {
-        if (H > 1 && x.head < x.extent) return report(PDA_ERR_INVALID_ARG, "heads of %s overlap (head stride too small)", x.name);
-        if (B > 1 && x.batch < (int64_t)(H - 1) * x.head + x.extent) return report(PDA_ERR_INVALID_ARG, "batches of %s overlap (batch stride too small)", x.name);
-    }
+    if ((rc = check_blocks(B, H, s.dq_batch, s.dq_head, Sq * d, "dq")) != PDA_OK || (rc = check_blocks(B, H, s.dkv_batch, s.dkv_head, Skv * d, "dk/dv")) != PDA_OK) return rc;
     return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, false, scale, kv_valid_len, workspace, workspace_bytes, stream);
 }
 
