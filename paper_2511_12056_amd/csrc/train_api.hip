@@ -44,6 +44,47 @@ int check_bwd_sizes(int B, int H, int64_t Sq, int64_t Skv, int d, int64_t kv_val
     return PDA_OK;
 }
 
+// B x H blocks of `bytes` bytes, `batch` and `head` bytes apart.
+struct View {
+    const void* p;           // null: not there
+    int64_t bytes, B, H, batch, head;
+    const char* name;
+    int64_t span() const { return (B - 1) * batch + (H - 1) * head + bytes; }
+};
+View view(const void* p, int64_t n, int size, int B, int H, int64_t batch, int64_t head, const char* name) {
+    View v{p, n * size, B, H, batch * size, head * size, name};
+    if (v.head == v.bytes || H == 1) v = View{p, v.bytes * H, B, 1, v.batch, 0, name};       // one piece a batch, or one in all
+    if (v.H == 1 && v.batch == v.bytes) v = View{p, v.bytes * B, 1, 1, 0, 0, name};
+    return v;
+}
+// Do two views share a byte?  Every block of one against the blocks of the other that its place leaves.
+bool overlap(const View& x, const View& y) {
+    if (!x.p || !y.p || x.bytes == 0 || y.bytes == 0) return false;
+    const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(x.p) - reinterpret_cast<uintptr_t>(y.p));
+    if (from >= y.span() || from + x.span() <= 0) return false;
+    const bool heads_out = y.head > y.batch;                   // the outer axis of y is the one of the larger stride
+    const int64_t n1 = heads_out ? y.H : y.B, s1 = heads_out ? y.head : y.batch, n2 = heads_out ? y.B : y.H, s2 = heads_out ? y.batch : y.head;
+    const int64_t span2 = (n2 - 1) * s2 + y.bytes;
+    // first of the places i * s whose `len` bytes end behind `at`
+    const auto first = [](int64_t at, int64_t len, int64_t s) -> int64_t { return at < len ? 0 : s == 0 ? INT64_MAX : (at - len) / s + 1; };
+    for (int64_t b = 0; b < x.B; ++b)
+        for (int64_t h = 0; h < x.H; ++h) {
+            const int64_t at = from + b * x.batch + h * x.head, end = at + x.bytes;
+            for (int64_t i = first(at, span2, s1); i < n1 && i * s1 < end; ++i) {
+                const int64_t j = first(at - i * s1, y.bytes, s2);
+                if (j < n2 && j * s2 < end - i * s1) return true;
+                if (s1 == 0) break;
+            }
+        }
+    return false;
+}
+int check_apart(std::initializer_list<View> written, std::initializer_list<View> others) {
+    for (const View& w : written)
+        for (const View& x : others)
+            if (overlap(w, x)) return report(PDA_ERR_INVALID_ARG, "%s overlaps %s", w.name, x.name);
+    return PDA_OK;
+}
+
 // The blocks of n elements at b * batch + h * head must not share any, whichever of the two axes is the outer one.
 int check_blocks(int B, int H, int64_t batch, int64_t head, int64_t n, const char* name) {
     if (n == 0) return PDA_OK;
@@ -60,7 +101,7 @@ int check_blocks(int B, int H, int64_t batch, int64_t head, int64_t n, const cha
 }
 
 int attn_bwd(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type, const float* lse,
-             void* dq, void* dk, void* dv, int B, int H, int64_t Sq, int64_t Skv, int d, const pda_attn_bwd_strides& s, bool compact,
+             void* dq, void* dk, void* dv, int B, int H, int64_t Sq, int64_t Skv, int d, const pda_attn_bwd_strides& s,
              float scale, int64_t n_v, void* workspace, int64_t workspace_bytes, void* stream) {
     int rc = check_bwd_sizes(B, H, Sq, Skv, d, n_v);
     if (rc != PDA_OK) return rc;
@@ -73,19 +114,20 @@ int attn_bwd(const void* dout, const void* q, const void* k, const void* v, cons
     for (const void* p : {dout, q, k, v, out, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
         if (!aligned(p, 16)) return report(PDA_ERR_UNSUPPORTED, "dout/q/k/v/out/dq/dk/dv must be 16-byte aligned");
     if (!aligned(lse, 4)) return report(PDA_ERR_UNSUPPORTED, "lse must be 4-byte aligned");
-    const double rows_q = (double)B * H * (double)Sq, rows_k = (double)B * H * (double)Skv;
-    auto size = [&](double bytes) { return compact ? bytes : (bytes > 0 ? 1 : 0); };       // views may interleave: only their first elements are compared
-    const Range rq{dq, size(rows_q * d * 2), "dq"}, rk{dk, size(rows_k * d * 2), "dk"}, rv{dv, size(rows_k * d * 2), "dv"};
-    const std::initializer_list<Range> in = {
-        {dout, size(rows_q * d * 2), "dout"}, {q, size(rows_q * d * 2), "q"}, {out, size(rows_q * d * (out_type == PDA_BF16 ? 2 : 4)), "out"},
-        {lse, size(rows_q * 4), "lse"}, {k, size(rows_k * d * 2), "k"}, {v, size(rows_k * d * 2), "v"}};
+    const int64_t nq = Sq * d, nk = Skv * d;
+    const View rq = view(dq, nq, 2, B, H, s.dq_batch, s.dq_head, "dq"), rk = view(dk, nk, 2, B, H, s.dkv_batch, s.dkv_head, "dk"),
+               rv = view(dv, nk, 2, B, H, s.dkv_batch, s.dkv_head, "dv");
+    const std::initializer_list<View> in = {
+        view(dout, nq, 2, B, H, s.dout_batch, s.dout_head, "dout"), view(q, nq, 2, B, H, s.q_batch, s.q_head, "q"),
+        view(out, nq, out_type == PDA_BF16 ? 2 : 4, B, H, s.out_batch, s.out_head, "out"), view(lse, Sq, 4, B, H, s.lse_batch, s.lse_head, "lse"),
+        view(k, nk, 2, B, H, s.kv_batch, s.kv_head, "k"), view(v, nk, 2, B, H, s.kv_batch, s.kv_head, "v")};
     if ((rc = check_apart({rq, rk, rv}, in)) != PDA_OK) return rc;
     if ((rc = check_apart({rk}, {rq})) != PDA_OK || (rc = check_apart({rv}, {rq, rk})) != PDA_OK) return rc;
     pda::AttnBwdParams p{};
     const int64_t stat_bytes = pda::bwd_stat_bytes((int64_t)B * H, Sq, d), given = workspace ? workspace_bytes : 0;
     if (given < stat_bytes) return report(PDA_ERR_INVALID_ARG, "workspace of %lld bytes, at least %lld needed", (long long)given, (long long)stat_bytes);
     if (!aligned(workspace, 256)) return report(PDA_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
-    const Range ws{workspace, (double)given, "workspace"};
+    const View ws = view(workspace, given < (int64_t)1 << 60 ? given : (int64_t)1 << 60, 1, 1, 1, 0, 0, "workspace");     // (sums of addresses stay in 64 bits)
     if ((rc = check_apart({ws}, in)) != PDA_OK || (rc = check_apart({ws}, {rq, rk, rv})) != PDA_OK) return rc;
     int n_cu = 0;
     hipError_t e = pda::device_cu_count(&n_cu);
@@ -175,7 +217,7 @@ int pda_attn_bwd(const void* dout, const void* q, const void* k, const void* v, 
     if (rc != PDA_OK) return rc;
     const int64_t qh = Sq * d, kh = Skv * d, qb = H * qh, kb = H * kh;
     const pda_attn_bwd_strides s{qb, qh, qb, qh, kb, kh, qb, qh, H * Sq, Sq, qb, qh, kb, kh};
-    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, true, scale, kv_valid_len, workspace, workspace_bytes, stream);
+    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, scale, kv_valid_len, workspace, workspace_bytes, stream);
 }
 
 int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const void* v, const void* out, int out_type,
@@ -194,7 +236,7 @@ int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const v
         return report(PDA_ERR_UNSUPPORTED, "strides of bf16 tensors must be multiples of 8 elements");
     if ((s.out_batch | s.out_head) % (out_type == PDA_BF16 ? 8 : 4) != 0) return report(PDA_ERR_UNSUPPORTED, "out strides must be multiples of 16 bytes");
     if ((rc = check_blocks(B, H, s.dq_batch, s.dq_head, Sq * d, "dq")) != PDA_OK || (rc = check_blocks(B, H, s.dkv_batch, s.dkv_head, Skv * d, "dk/dv")) != PDA_OK) return rc;
-    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, false, scale, kv_valid_len, workspace, workspace_bytes, stream);
+    return attn_bwd(dout, q, k, v, out, out_type, lse, dq, dk, dv, B, H, Sq, Skv, d, s, scale, kv_valid_len, workspace, workspace_bytes, stream);
 }
 
 int pda_layer_norm_fwd(const void* x, int x_type, const float* weight, const float* bias, void* y, int y_type,
