@@ -54,7 +54,7 @@ template <int D, bool OUT16>
 __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(const AttnBwdParams p) {
     constexpr int LPR = D / 8;
     const int lane = threadIdx.x % LPR;
-    const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const int64_t row = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * (256 / LPR) + threadIdx.x / LPR;
     const int bh = blockIdx.y, b = bh / p.H, h = bh - b * p.H;
     if (row >= p.stat_rows) return;
     if (row == 0 && bh == 0 && lane == 0) *p.counter = 0;      // for the kernel that follows
@@ -874,7 +874,8 @@ static hipError_t launch_bwd(AttnBwdParams& p, hipStream_t st) {
     if (D == 64 && p.scale_log2e < 0x1p-64f) p.scale_log2e = 0x1p-64f;        // l is kept in units of the scores; below, every score counts for nothing
     if (p.Sq > 0) {
         constexpr int rows = 256 / (D / 8);
-        const dim3 grid((unsigned)((p.stat_rows + rows - 1) / rows), (unsigned)BH);
+        const int64_t n = (p.stat_rows + rows - 1) / rows, x = n < 1 << 21 ? n : 1 << 21;       // a launch has fewer than 2^32 threads along x, and is cut short without an error beyond
+        const dim3 grid((unsigned)x, (unsigned)BH, (unsigned)((n + x - 1) / x));
         if (p.out_bf16) hipLaunchKernelGGL((attn_bwd_stats_kernel<D, true>), grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL((attn_bwd_stats_kernel<D, false>), grid, dim3(256), 0, st, p);
         const hipError_t e = hipGetLastError();
