@@ -398,10 +398,18 @@ def _elsewhere(t):
     return ValueError(f"a tensor on device {t.get_device()}, the current device is {torch.cuda.current_device()}")
 
 
-def _on_current_device(*tensors):
+def _stream_of(current: int, stream):
+    """A kernel on another device's stream would run there, and so would a workspace that is taken on it."""
+    device = getattr(stream, "device", None)                    # (anything with a cuda_stream is a stream here)
+    if device is not None and device.index != current:
+        raise ValueError(f"a stream of device {device.index}, the current device is {current}")
+
+
+def _on_current_device(stream, *tensors):
     """A kernel runs on the current device and would follow another device's addresses there."""
     import torch
     current = torch.cuda.current_device()
+    _stream_of(current, stream)
     for t in tensors:
         if t is not None and t.get_device() != current:
             raise _elsewhere(t)
@@ -455,7 +463,7 @@ def attn_bwd(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid_len: Op
     _expect(dq, bf16, (B, H, Sq, d), "dq")
     _expect(dk, bf16, (B, H, Skv, d), "dk")
     _expect(dv, bf16, (B, H, Skv, d), "dv")
-    _on_current_device(dout, q, k, v, out, lse, dq, dk, dv, workspace)
+    _on_current_device(stream, dout, q, k, v, out, lse, dq, dk, dv, workspace)
     n_v = Skv if kv_valid_len is None else int(kv_valid_len)
     if workspace is None:
         workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
@@ -485,7 +493,7 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
     st += [_view_strides(lse, 1, "lse"), _view_strides(dq, 2, "dq"), _view_strides(dk, 2, "dk")]
     if _view_strides(v, 2, "v") != st[2] or _view_strides(dv, 2, "dv") != st[6]:
         raise ValueError("k and v must share their strides, and dk and dv theirs")
-    _on_current_device(dout, q, k, v, out, lse, dq, dk, dv, workspace)
+    _on_current_device(stream, dout, q, k, v, out, lse, dq, dk, dv, workspace)
     n_v = Skv if kv_valid_len is None else int(kv_valid_len)
     if workspace is None:
         workspace = _workspace(attn_bwd_workspace_bytes(B, H, Sq, Skv, d, n_v), None, stream)
@@ -497,8 +505,8 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
     return dq, dk, dv
 
 
-def _norm_sizes(x, per_row, params, others):
-    """Rows, D and groups of a call, and that all tensors are on the current device (others: of the shape of x, a workspace).  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
+def _norm_sizes(stream, x, per_row, params, others):
+    """Rows, D and groups of a call, and that all tensors and the stream are of the current device (others: of the shape of x, a workspace).  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
     (One function: a call on few rows is bound by host time.)"""
     import torch
     f32, device = torch.float32, x.get_device()
@@ -506,6 +514,7 @@ def _norm_sizes(x, per_row, params, others):
         raise ValueError("x: expected a contiguous cuda tensor of at least one axis")
     if device != torch.cuda.current_device():
         raise _elsewhere(x)
+    _stream_of(device, stream)
     for t in others:
         if t is not None and t.get_device() != device:
             raise _elsewhere(t)
@@ -539,7 +548,7 @@ def layer_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, 
 
     weight, bias: [D], or [groups, D] with one row for every rows/groups consecutive rows of x, or None.
     """
-    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (bias, "bias")), (y,))
+    rows, D, groups = _norm_sizes(stream, x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (bias, "bias")), (y,))
     _expect(y, y.dtype, x.shape, "y")
     _check(lib.pda_layer_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(weight), _ptr(bias), _ptr(y), _type_code(y, "y"), _ptr(mean), _ptr(rstd),
                                   rows, groups, D, float(eps), _stream_handle(stream)))
@@ -564,7 +573,7 @@ def layer_norm_bwd(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace=None
 
     dx, dweight and dbias may be None; weight is None where the forward call had none.
     """
-    rows, D, groups = _norm_sizes(x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias")),
+    rows, D, groups = _norm_sizes(stream, x, ((mean, "mean"), (rstd, "rstd")), ((weight, "weight"), (dweight, "dweight"), (dbias, "dbias")),
                                   (dy, dx, workspace))
     _expect(dy, dy.dtype, x.shape, "dy")
     if dx is not None:
@@ -588,7 +597,7 @@ def pack_heads_bwd(dy, x, dx, unit_rms: bool, premul: float = 1.0, stream=None):
     if x is not None:
         _expect(x, torch.float32, (B, S, H, d), "x")
     _expect(dx, torch.float32, (B, S, H, d), "dx")
-    _on_current_device(dy, x, dx)
+    _on_current_device(stream, dy, x, dx)
     _check(lib.pda_pack_heads_bwd(_ptr(dy), _ptr(x), _ptr(dx), B, S, H, d, 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
     return dx
 
