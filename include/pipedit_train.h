@@ -41,7 +41,8 @@ extern "C" {
  * The gradient of pda_attn_fwd_base2 is this call with scale = ln 2 (0.69314718f; the scores are then used as
  * they are).  Shares of the keys (key chunks whose partial results went through pda_attn_merge): each share's call
  * with the MERGED out and lse gives its exact dk and dv, and the sum of the shares' dq is dq.  Shares of the
- * queries: dq per share, and dk and dv are the sums.
+ * queries: dq per share, and dk and dv are the sums.  Each share's gradients are rounded to bf16, so a sum over shares, which the
+ * caller makes (in fp32), holds a rounding of every share where one call holds one.
  *
  * Arithmetic: products of bf16 accumulated in fp32 on the matrix cores; probabilities, delta and ds in fp32, p and
  * ds rounded to bf16 only as operands of the products that sum them; gradients rounded once to bf16.
@@ -70,8 +71,9 @@ int pda_attn_bwd_strided(const void* dout, const void* q, const void* k, const v
                          int64_t kv_valid_len, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * Bytes of workspace of a pda_attn_bwd or pda_attn_bwd_strided call (host only; bytes is a HOST pointer): a counter, two floats
- * for every query row, and where the launch has few work items the partial gradients of its shares.
+ * Bytes of workspace of a pda_attn_bwd or pda_attn_bwd_strided call (host only; bytes is a HOST pointer): 256 bytes for a
+ * counter; for every query row, rounded up to 64 a head, 8 bytes of statistics (d = 128) or 16 (d = 64); and where the launch does not
+ * fill the device evenly the partial gradients of its shares.
  * n_cu: compute units of the device (0 = ask the current device).
  *
  * The need does not grow with the lengths: a shorter launch may be cut where a longer one is not.  kv_valid_len = PDA_ANY_LEN gives
