@@ -94,7 +94,10 @@ inline BwdPlan plan_bwd(int64_t Sq, int64_t n_v, int64_t BH, int d, int n_cu) {
     w.query_blocks = (int)(BH * w.query_per_head);
     w.key_parts = w.query_parts = 1;
     const int64_t sk = bwd_steps(Sq), sq = bwd_steps(n_v), blocks = (int64_t)w.key_blocks + w.query_blocks;
-    if (w.key_blocks == 0 || w.query_blocks == 0 || blocks > 64 * (int64_t)n_cu) return w;      // (nothing to gain at the end of so long a launch)
+    if (w.key_blocks == 0 || w.query_blocks == 0) return w;
+    const int64_t key_time = bwd_key_time(sk), query_time = bwd_query_time(sq), longest = key_time > query_time ? key_time : query_time;
+    // so long a launch has nothing to gain at its end, unless that is a few blocks against the long side among many against the short one
+    if (blocks > 64 * (int64_t)n_cu && longest * 16 * n_cu <= w.key_blocks * key_time + w.query_blocks * query_time) return w;
     // two steps a part at the least; one part is always a candidate, so that query blocks are cut where key blocks cannot be
     const int max_k = (int)(sk < 4 ? 1 : sk / 2 < kBwdMaxParts ? sk / 2 : kBwdMaxParts), max_q = (int)(sq / 2 < kBwdMaxParts ? sq / 2 : kBwdMaxParts);
     BwdPlan best = w;

@@ -60,15 +60,32 @@ def test_one_block_more_than_compute_units(plan, BH, Sq, d):  # noqa: F811
     assert _time(above) <= _time(below) + keys, (below, above)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("BH,Sq,n_v", [(24, 32, 180_000), (24, 180_000, 226), (1, 17, 4_300_000), (96, 200, 45_000), (2, 2_200_000, 64)])
+def test_a_few_long_blocks_among_very_many_short_ones(plan, BH, Sq, n_v, d):  # noqa: F811
+    """However many blocks a launch has, the ones that stream the long side do not end it alone: with the long blocks in as many parts as there are places for, a
+    launch in which each item goes to the unit that is free first ends within its work over the units and its longest item, and the kernel that adds the parts follows."""
+    p, = plan([(BH, Sq, n_v, d, 256)])
+    kb, qb, (sk, sq) = p[2], p[3], (-(-Sq // 32), -(-n_v // 32))
+    long_keys = sk > sq
+    parts = min(16, 4 * 256 // (2 * kb if long_keys else qb))
+    parts = min(parts, 2 * 256 // kb) if long_keys else parts             # key blocks: at most two parts a unit in all
+    steps = -(-max(sk, sq) // parts)
+    key, query = (12 * (steps if long_keys else sk) + 60), (10 * (sq if long_keys else steps) + 60)
+    work = kb * (parts if long_keys else 1) * key + qb * (1 if long_keys else parts) * query
+    most = work // 256 + max(key, query) + 30 + 4 * 256 * d // 200
+    assert kb + qb > 64 * 256 and _time(p) <= most < p[8], (p, most)
+
+
 def test_planning_takes_microseconds(tmp_path):
-    """Every call plans: a long launch is not simulated item by item, and one that is never cut not at all (these took 15 to 90 us; the limit is
+    """Every call plans: a long launch is not simulated item by item, and one that is never cut not at all (these took 15 to 90 us: the limits are
     some four times what they take now)."""
     if not os.path.exists(CLANG):
         pytest.skip("no ROCm clang++ here")
     src, exe = tmp_path / "clock.cpp", tmp_path / "clock"
     src.write_text(CLOCK)
     subprocess.run([CLANG, "-std=c++17", "-O2", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", CSRC, str(src), "-o", str(exe)], check=True, timeout=120)
-    cases = {(60_000, 8_192, 8_192): 2, (17, 119_056, 119_056): 10, (24, 67_576, 67_576): 10, (25, 120_472, 226): 30}
+    cases = {(60_000, 8_192, 8_192): 2, (17, 119_056, 119_056): 10, (24, 67_576, 67_576): 10, (25, 120_472, 226): 60}
     out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True, check=True, timeout=60).stdout.split()
     assert len(out) == len(cases)
     for (c, most), us in zip(cases.items(), out):
