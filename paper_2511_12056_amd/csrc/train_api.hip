@@ -87,7 +87,7 @@ int check_apart(std::initializer_list<View> written, std::initializer_list<View>
 
 // The blocks of n elements at b * batch + h * head must not share any, whichever of the two axes is the outer one.
 int check_blocks(int B, int H, int64_t batch, int64_t head, int64_t n, const char* name) {
-    if (n == 0) return PDA_OK;
+    if (n == 0 || B == 0 || H == 0) return PDA_OK;
     if (H > 1 && head < n) return report(PDA_ERR_INVALID_ARG, "heads of %s overlap (head stride too small)", name);
     for (int64_t i = 1; i < B; ++i) {                          // block (0, h) against (i, 0); differences with h on the other side are larger
         const int64_t x = i * batch;

@@ -111,6 +111,11 @@ def test_results_against_the_other_tensors(pda, seed):  # noqa: F811
             assert "at least" in pda.last_error(), pda.last_error()
 
 
+@pytest.mark.parametrize("B,H", [(2, 0), (0, 2), (3, 0)])
+def test_no_heads_or_batches_share_nothing(pda, B, H):  # noqa: F811
+    assert _bwd(pda, strides=_strides(pda, dq_batch=0, dq_head=0, dkv_batch=0, dkv_head=0), B=B, H=H) == 0, pda.last_error()
+
+
 def test_a_workspace_of_any_size_is_compared(pda):  # noqa: F811
     for size in ((1 << 63) - 1, 1 << 62):
         assert _bwd(pda, ws=256, ws_bytes=size) == 1 and "workspace overlaps dout" in pda.last_error(), pda.last_error()
