@@ -179,7 +179,8 @@ __global__ __launch_bounds__(256) void pack_heads_bwd_kernel(const uint2* __rest
         const float ss = lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w);
         const float dot = lane_sum<LPV>(a.x * g.x + a.y * g.y + a.z * g.z + a.w * g.w);
         // dx = premul r (dy - x <x, dy> / <x, x>); only a zero vector counts as one, NaN goes into the whole vector
-        const float r = ss == 0.f ? 0.f : premul / sqrtf(ss * (1.0f / (4 * LPV)));
+        const float r = ss == 0.f ? 0.f : ss < 0x1p-100f ? premul * sqrtf(4 * LPV) / sqrtf(ss)     // (their mean would lose bits, or be 0)
+                                        : premul / sqrtf(ss * (1.0f / (4 * LPV)));
         const float f = ss == 0.f ? 0.f : -dot / ss;
         g.x = r * __builtin_fmaf(a.x, f, g.x);
         g.y = r * __builtin_fmaf(a.y, f, g.y);

@@ -107,3 +107,26 @@ def test_pack_gradient_of_an_infinite_element():
     x[0, 2, 1, 9] = float("inf")
     got = pda.pack_heads_bwd(dy, x, torch.empty_like(x), True)
     assert torch.isnan(got[0, 2, 1, 9]) and torch.isfinite(got[0, :2]).all()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("value", [1e-21, 3e-22, 2e-22, 1.5e-22, 1e-22, 5e-23, 1e-23, 1e-30])
+def test_pack_gradient_of_a_vector_whose_squares_nearly_vanish(value, d):
+    """One element whose square, or its mean over the vector, is at the end of fp32's range: the gradient is that of the formula, or 0 where the square is."""
+    import torch
+    import paper_2511_12056_amd as pda
+    x, dy = torch.zeros(1, 3, 1, d, device="cuda"), torch.ones(1, 1, 3, d, device="cuda", dtype=torch.bfloat16)
+    x[0, :, 0, 5] = value
+    dy[..., 9] = -2.0
+    got = pda.pack_heads_bwd(dy, x, torch.full_like(x, 7.0), True)
+    assert torch.isfinite(got).all()
+    x2 = float(x[0, 0, 0, 5].double()) ** 2
+    if x2 < 2.0 ** -150:
+        assert (got == 0).all()
+        return
+    # the square is rounded to whole units of 2^-149: off by e = 2^-150 / x^2 < 1 relatively, to half and twice its value at the most.  r = 1 / sqrt(..) is off by
+    # less than 1.5 e (1 / sqrt(1 - e) - 1 <= e up to e = 0.6, 0.42 beyond it), the element itself, r (1 - x^2 / square), by r times 2 e; 2^-20 for the other roundings
+    r, e = d ** 0.5 / x2 ** 0.5, 2.0 ** -150 / x2
+    want = r * dy.double().transpose(1, 2)
+    want[..., 5] = 0
+    assert ((got.double() - want).abs() <= 2 * r * (1.5 * e + 2.0 ** -20)).all(), (got[0, 0, 0, :10], want[0, 0, 0, :10])
