@@ -128,7 +128,7 @@ int pda_layer_norm_bwd_workspace(int64_t rows, int64_t groups, int D, int n_cu, 
  * a zero vector (the squares lose bits below some 1e-19), one whose squares pass fp32's range (some 1e19) has the gradient 0.  A NaN in the vector or its dy makes all of its dx NaN.
  *
  * x is the pack's input and is read with unit_rms only (NULL without).  dx may be x itself.  The rounding of the pack
- * counts as the identity.  d, alignment and sizes as pda_pack_heads.
+ * counts as the identity.  d, alignment and sizes as pda_pack_heads, H < 2^24.
  */
 int pda_pack_heads_bwd(const void* dy, const float* x, float* dx, int B, int64_t S, int H, int d, int unit_rms,
                        float premul, void* stream);

@@ -317,6 +317,7 @@ int pda_pack_heads_bwd(const void* dy, const float* x, float* dx, int B, int64_t
     if (B < 0 || H < 0 || S < 0) return report(PDA_ERR_INVALID_ARG, "negative size (B=%d H=%d S=%lld)", B, H, (long long)S);
     if (d != 64 && d != 128) return report(PDA_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", d);
     if ((double)B * H * (double)S * d >= 1099511627776.0) return report(PDA_ERR_UNSUPPORTED, "B*H*S*d overflows 2^40 elements");
+    if (H >= 1 << 24) return report(PDA_ERR_UNSUPPORTED, "H=%d heads (fewer than 2^24 supported)", H);       // 256 threads each along one axis
     if (B == 0 || H == 0 || S == 0) return PDA_OK;
     if (!dy || !dx || (unit_rms && !x)) return report(PDA_ERR_INVALID_ARG, "null dy/dx, or x with unit_rms");
     if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(dx, 16)) return report(PDA_ERR_UNSUPPORTED, "dy, x and dx must be 16-byte aligned");
