@@ -29,7 +29,7 @@
 // Measured, whole call (floating-point operations of the five products that are the least, 10 Sq n_v d, per second): d = 128: 3 x 67 576 on 67 476 18.3 ms
 // = 954 TFLOP/s (the seven products run at 1 340, as fast as a large library product), 24 x 9 600 3.04 ms = 930, 1 x 9 600 160 us = 736, 24 x 16 384 on 570
 // 484 us = 593 (a sixth of its products are of rows behind the last key); d = 64: 6 x 33 000 5.29 ms = 791, 24 x 4 797 on 4 701 492 us = 704, 2 x 1 024 18.6 us = 72
-// (three launches, parts of four steps).  Boxes differ by up to 5 %.  The matrix cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 53 % in 24 x 4 797, d = 64; no bank conflicts.
+// (three launches, parts of four steps).  Cards differ by up to 5 %.  The matrix cores are busy 72 % of the time in 24 x 9 600, 61 % in 24 x 16 384 on 570 and 53 % in 24 x 4 797, d = 64; no bank conflicts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "attn_internal.h"

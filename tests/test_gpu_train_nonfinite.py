@@ -130,3 +130,28 @@ def test_pack_gradient_of_a_vector_whose_squares_nearly_vanish(value, d):
     want = r * dy.double().transpose(1, 2)
     want[..., 5] = 0
     assert ((got.double() - want).abs() <= 2 * r * (1.5 * e + 2.0 ** -20)).all(), (got[0, 0, 0, :10], want[0, 0, 0, :10])
+
+
+@pytest.mark.parametrize("D", [3, 30, 64, 100, 128, 300, 640, 1001, 1536, 3001])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_layer_norm_of_a_row_that_is_not_finite(value, D):
+    """It loses its own results, and in the backward pass its group's sums; rows beside it, which may share a wavefront, keep their bits."""
+    import torch
+    import paper_2511_12056_amd as pda
+    g = torch.Generator(device="cuda").manual_seed(D)
+    rows, groups, bad = 66, 2, 13
+    x, dy = (torch.randn(rows, D, generator=g, device="cuda") for _ in range(2))
+    w, b = 1 + torch.randn(groups, D, generator=g, device="cuda"), torch.randn(groups, D, generator=g, device="cuda")
+
+    def both():
+        y, mean, rstd = pda.layer_norm_fwd(x, w, b, torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"))
+        dx, dw, db = pda.layer_norm_bwd(dy, x, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(b))
+        return y, mean, rstd, dx, dw, db
+    want = [t.clone() for t in both()]
+    x[bad, D // 2] = value
+    y, mean, rstd, dx, dw, db = both()
+    others = [r for r in range(rows) if r != bad]
+    for a, c in zip((y, mean, rstd, dx), want):
+        assert torch.equal(a[others], c[others])
+    assert torch.isnan(y[bad]).all() and torch.isnan(dx[bad]).all() and not torch.isfinite(mean[bad]) and torch.isnan(dw[0]).all()
+    assert torch.equal(dw[1], want[4][1]) and torch.equal(db, want[5])
