@@ -7,7 +7,7 @@ A case is a dict with an "op" and the sizes of that operator:
     rms_fwd   rows, D, groups (rows that share a weight), x and res types ("none": no residual), y type ("e4m3": 8 bits with scales)
     rms_bwd   rows, D, groups, dy and h types, dres (whether the residual stream has a gradient of its own)
     quant     rows, cols, x type, fp8 type, block (rows of a block: 1 or 128), order ("rows", "cols" or "both")
-    matmul    M, N, K, a ("e4m3" or "e5m2"), block (rows of a block of b), bias, out type
+    matmul    M, N, K, a ("e4m3" or "e5m2"), block (rows of a block of b), bias; the result is bf16
     rope, rope_bwd   B, S, H, d, rot (columns that turn), layout, axes (1, or 3 with a gh x gw grid a frame), x type, fused (x is the first third
               of a fused projection), unit_rms, factor (of the context's extension), first (the first position)
 
@@ -44,13 +44,13 @@ def listed():
         # the gradient of a projection's result: by rows for the gradient of its input, by columns for the gradient of its weight
         {"name": "quant_720p", "op": "quant", "rows": 119056, "cols": 1536, "x": "bf16", "fp8": "e5m2", "block": 1, "order": "both"},
         # one token through a fused projection: the weight's bytes
-        {"name": "matmul_one_token", "op": "matmul", "M": 1, "N": 4608, "K": 1536, "a": "e4m3", "block": 128, "bias": True, "out": "bf16"},
+        {"name": "matmul_one_token", "op": "matmul", "M": 1, "N": 4608, "K": 1536, "a": "e4m3", "block": 128, "bias": True},
         # 256 text tokens from an encoder of another width
-        {"name": "matmul_text", "op": "matmul", "M": 256, "N": 1536, "K": 4096, "a": "e4m3", "block": 128, "bias": True, "out": "bf16"},
+        {"name": "matmul_text", "op": "matmul", "M": 256, "N": 1536, "K": 4096, "a": "e4m3", "block": 128, "bias": True},
         # the fused projection of a 720p clip's tokens to queries, keys and values
-        {"name": "matmul_720p", "op": "matmul", "M": 119056, "N": 4608, "K": 1536, "a": "e4m3", "block": 128, "bias": True, "out": "bf16"},
+        {"name": "matmul_720p", "op": "matmul", "M": 119056, "N": 4608, "K": 1536, "a": "e4m3", "block": 128, "bias": True},
         # the gradient of that projection's weight: a sum over all tokens
-        {"name": "matmul_weight_grad", "op": "matmul", "M": 4608, "N": 1536, "K": 119056, "a": "e5m2", "block": 1, "bias": False, "out": "fp32"},
+        {"name": "matmul_weight_grad", "op": "matmul", "M": 4608, "N": 1536, "K": 119056, "a": "e5m2", "block": 1, "bias": False},
         # single tokens of a batch at far positions, in a context extended four times
         {"name": "rope_token", "op": "rope", "B": 8, "S": 1, "H": 12, "d": 128, "rot": 64, "layout": "half", "axes": 1, "gh": 1, "gw": 1, "x": "bf16",
          "fused": True, "unit_rms": False, "factor": 4.0, "first": 119055},
@@ -89,8 +89,7 @@ def draw(rng):
             long = rng.random() < 0.25
             tokens = _log_int(rng, 1, 119056)
             case = {"op": op, "M": width if long else tokens, "N": rng.choice([64 * rng.randint(2, 64), _log_int(rng, 30, 8192)]), "K": tokens if long else width,
-                    "a": rng.choice(["e4m3", "e4m3", "e5m2"]), "block": 1 if long else rng.choice([1, 128, 128]), "bias": rng.random() < 0.5,
-                    "out": rng.choice(["bf16", "bf16", "fp32"])}
+                    "a": rng.choice(["e4m3", "e4m3", "e5m2"]), "block": 1 if long else rng.choice([1, 128, 128]), "bias": rng.random() < 0.5}
             if work(case)["flops"] <= LARGEST_FLOPS / 2:
                 return case
         else:
@@ -200,7 +199,7 @@ def prepare(case, seed):
         st["a"], st["a_scales"] = _quantise(uneven(M, K), case["a"], 1)
         st["b"], st["b_scales"] = _quantise(normal(N, K) * K ** -0.5, "e4m3", case["block"])
         st["bias"] = normal(N) if case["bias"] else None
-        st["out"] = torch.empty(M, N, device=dev, dtype=TYPES[case["out"]])
+        st["out"] = torch.empty(M, N, device=dev, dtype=torch.bfloat16)
     else:
         B, S, H, d = case["B"], case["S"], case["H"], case["d"]
         def tokens():                                   # token-major heads, alone or beside two others as a fused projection leaves them
@@ -314,7 +313,7 @@ def run(st):
     if op == "matmul":
         a, b = _values(st["a"], st["a_scales"], 1), _values(st["b"], st["b_scales"], case["block"])
         out = torch.matmul(a, b.t())
-        return (out if st["bias"] is None else out + st["bias"]).to(TYPES[case["out"]])
+        return (out if st["bias"] is None else out + st["bias"]).to(torch.bfloat16)
     cos, sin = (t.float() for t in _turns(st))
     if op == "rope":
         x = st["x"].float()
@@ -440,7 +439,7 @@ def work(case):
         return {"bytes": rows * cols * SIZE[case["x"]] + out + out // 128, "flops": 3 * rows * cols}
     if op == "matmul":
         M, N, K = case["M"], case["N"], _up(case["K"], 128)
-        return {"bytes": (M + N) * K + M * K // 128 + N * K // 128 // case["block"] + M * N * SIZE[case["out"]] + (4 * N if case["bias"] else 0),
+        return {"bytes": (M + N) * K + M * K // 128 + N * K // 128 // case["block"] + M * N * 2 + (4 * N if case["bias"] else 0),
                 "flops": 2.0 * M * N * case["K"]}
     n = case["B"] * case["S"] * case["H"] * case["d"]
     reads = SIZE[case["x"]] if op == "rope" or case["unit_rms"] else 0
