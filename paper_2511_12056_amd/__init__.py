@@ -11,3 +11,6 @@ from .binding import (PdaError, attn_fwd, attn_fwd_base2, attn_fwd_bf16out, attn
                       PDA_SINK_TOKEN_ARRIVAL, PDA_SINK_TOKEN_FINAL)
 from .binding import (attn_bwd, attn_bwd_strided, attn_bwd_workspace, attn_bwd_workspace_bytes, layer_norm_bwd, layer_norm_bwd_workspace,  # noqa: F401
                       layer_norm_bwd_workspace_bytes, layer_norm_fwd, pack_heads_bwd, PDA_ANY_LEN, PDA_BF16, PDA_F32, PDA_LAYER_NORM_MAX)
+from .binding import (fp8_empty, fp8_matmul, fp8_matmul_workspace, fp8_matmul_workspace_bytes, fp8_quant, pack_heads_rope, pack_heads_rope_bwd,  # noqa: F401
+                      rms_norm_bwd, rms_norm_bwd_workspace, rms_norm_bwd_workspace_bytes, rms_norm_fwd, Rope, rope_frequencies,
+                      PDA_E4M3, PDA_E5M2, PDA_ROPE_MAX_AXES)

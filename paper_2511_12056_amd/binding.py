@@ -18,14 +18,23 @@ PDA_NOALLOC_MAX_SLOTS = 576
 PDA_MAX_KEY_RANGES = 16
 PDA_MAX_LOCAL_HEADS = 64
 PDA_SINK_HEAD_MAJOR, PDA_SINK_TOKEN_ARRIVAL, PDA_SINK_TOKEN_FINAL = 0, 1, 2
-PDA_F32, PDA_BF16 = 0, 1
+PDA_F32, PDA_BF16, PDA_E4M3, PDA_E5M2 = 0, 1, 2, 3
 PDA_LAYER_NORM_MAX = 8192
 PDA_ANY_LEN = -1
+PDA_ROPE_MAX_AXES = 4
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "blend": 3}
 
 
 class AttnBwdStrides(C.Structure):
     """pda_attn_bwd_strides: batch and head strides in elements."""
     _fields_ = [(n + "_" + a, C.c_int64) for n in ("dout", "q", "kv", "out", "lse", "dq", "dkv") for a in ("batch", "head")]
+
+
+class RopeStruct(C.Structure):
+    """pda_rope."""
+    _fields_ = [("rot", C.c_int), ("layout", C.c_int), ("axes", C.c_int), ("axis_pairs", C.c_int * PDA_ROPE_MAX_AXES),
+                ("freqs", C.POINTER(C.c_double)), ("positions", C.c_void_p), ("pos_batch", C.c_int64), ("first", C.c_int64)]
 
 
 class PdaError(RuntimeError):
@@ -99,6 +108,24 @@ def _load() -> C.CDLL:
     lib.pda_layer_norm_bwd_workspace.restype = i32
     lib.pda_pack_heads_bwd.argtypes = [vp, fp, fp, i32, i64, i32, i32, i32, f32, vp]
     lib.pda_pack_heads_bwd.restype = i32
+    lib.pda_fp8_quant.argtypes = [vp, i32, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    lib.pda_fp8_quant.restype = i32
+    lib.pda_fp8_matmul.argtypes = [vp, i32, vp, vp, vp, i32, fp, vp, i64, i64, i64, i64, vp, i64, vp]
+    lib.pda_fp8_matmul.restype = i32
+    lib.pda_fp8_matmul_workspace.argtypes = [i64, i64, i64, i32, C.POINTER(i64)]
+    lib.pda_fp8_matmul_workspace.restype = i32
+    lib.pda_rms_norm_fwd.argtypes = [vp, i32, vp, i32, fp, vp, vp, i32, vp, fp, i64, i64, i32, f32, vp]
+    lib.pda_rms_norm_fwd.restype = i32
+    lib.pda_rms_norm_bwd.argtypes = [vp, i32, vp, i32, fp, fp, vp, vp, fp, i64, i64, i32, vp, i64, vp]
+    lib.pda_rms_norm_bwd.restype = i32
+    lib.pda_rms_norm_bwd_workspace.argtypes = [i64, i64, i32, i32, C.POINTER(i64)]
+    lib.pda_rms_norm_bwd_workspace.restype = i32
+    lib.pda_pack_heads_rope.argtypes = [vp, i32, i64, i64, vp, i64, i64, i32, i64, i32, i32, C.POINTER(RopeStruct), i32, f32, vp]
+    lib.pda_pack_heads_rope.restype = i32
+    lib.pda_pack_heads_rope_bwd.argtypes = [vp, i64, i64, vp, i32, i64, i64, vp, i64, i64, i32, i64, i32, i32, C.POINTER(RopeStruct), i32, f32, vp]
+    lib.pda_pack_heads_rope_bwd.restype = i32
+    lib.pda_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, C.POINTER(f64), C.POINTER(f64)]
+    lib.pda_rope_frequencies.restype = i32
     lib.pda_last_error.argtypes = []
     lib.pda_last_error.restype = C.c_char_p
     lib.pda_version.argtypes = []
@@ -599,6 +626,261 @@ def pack_heads_bwd(dy, x, dx, unit_rms: bool, premul: float = 1.0, stream=None):
     _expect(dx, torch.float32, (B, S, H, d), "dx")
     _on_current_device(stream, dy, x, dx)
     _check(lib.pda_pack_heads_bwd(_ptr(dy), _ptr(x), _ptr(dx), B, S, H, d, 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
+    return dx
+
+
+# ---- projections: RMS norm, 8-bit matrices and their product, rotary positions (include/pipedit_proj.h) -------
+
+def _fp8_code(t, name):
+    import torch
+    if t.dtype is torch.float8_e4m3fn:
+        return PDA_E4M3
+    if t.dtype is torch.float8_e5m2:
+        return PDA_E5M2
+    raise ValueError(f"{name}: expected float8_e4m3fn or float8_e5m2, got {t.dtype}")
+
+
+def _up(n: int, m: int) -> int:
+    return (n + m - 1) // m * m
+
+
+def _expect_fp8(q, scales, rows: int, cols: int, block_rows: int, name: str):
+    """q [rows, cols padded to 128] and its scales [blocks of rows, blocks of columns padded to 4]."""
+    import torch
+    _fp8_code(q, name)
+    shape = (rows, _up(cols, 128))
+    if tuple(q.shape) != shape or not q.is_contiguous() or not q.is_cuda:
+        raise ValueError(f"{name}: expected contiguous cuda {shape}, got {tuple(q.shape)} contiguous={q.is_contiguous()} cuda={q.is_cuda}")
+    shape = (_up(rows, block_rows) // block_rows, _up(_up(cols, 128) // 128, 4))
+    if scales is None or scales.dtype is not torch.float8_e8m0fnu or tuple(scales.shape) != shape or not scales.is_contiguous() or not scales.is_cuda:
+        raise ValueError(f"{name}_scales: expected contiguous cuda float8_e8m0fnu {shape}, got " +
+                         ("None" if scales is None else f"{scales.dtype} {tuple(scales.shape)} contiguous={scales.is_contiguous()} cuda={scales.is_cuda}"))
+
+
+def fp8_empty(rows: int, cols: int, block_rows: int = 1, dtype=None):
+    """(q, scales) for an 8-bit matrix [rows, cols] on the current device, not filled; dtype: torch.float8_e4m3fn (default) or torch.float8_e5m2."""
+    import torch
+    q = torch.empty(rows, _up(cols, 128), dtype=torch.float8_e4m3fn if dtype is None else dtype, device="cuda")
+    return q, torch.empty(_up(rows, block_rows) // block_rows, _up(_up(cols, 128) // 128, 4), dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+
+
+def fp8_quant(x, q=None, q_scales=None, qt=None, qt_scales=None, block_rows: int = 1, stream=None):
+    """pda_fp8_quant: x [rows, cols] fp32 or bf16 (rows may lie apart) -> q, q_scales and/or qt, qt_scales (of the transposed matrix), as fp8_empty makes them.
+
+    block_rows: 1 (a scale per row and 128 columns of what is written) or 128 (per 128 x 128, the same in both orders).
+    """
+    if x.dim() != 2 or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"x: expected a cuda matrix with compact rows, got {tuple(x.shape)} stride {x.stride()}")
+    rows, cols = x.shape
+    if q is None and qt is None:
+        raise ValueError("neither q nor qt: nothing to compute")
+    if block_rows not in (1, 128):
+        raise ValueError(f"block_rows: expected 1 or 128, got {block_rows}")
+    if q is not None:
+        _expect_fp8(q, q_scales, rows, cols, block_rows, "q")
+    if qt is not None:
+        _expect_fp8(qt, qt_scales, cols, rows, block_rows, "qt")
+        if q is not None and q.dtype is not qt.dtype:
+            raise ValueError("q and qt: expected one type")
+    if (q is None and q_scales is not None) or (qt is None and qt_scales is not None):
+        raise ValueError("scales without their values")
+    _on_current_device(stream, x, q, q_scales, qt, qt_scales)
+    _check(lib.pda_fp8_quant(_ptr(x), _type_code(x, "x"), rows, cols, max(x.stride(0), cols) if rows > 1 else cols, _fp8_code(q if q is not None else qt, "q"), block_rows,
+                             _ptr(q), _ptr(q_scales), _ptr(qt), _ptr(qt_scales), _stream_handle(stream)))
+    return q, q_scales, qt, qt_scales
+
+
+def fp8_matmul_workspace_bytes(M: int, N: int, K: int, n_cu: int = 0) -> int:
+    """pda_fp8_matmul_workspace (K is rounded up to 128); n_cu = 0 asks the current device."""
+    n = C.c_int64(0)
+    _check(lib.pda_fp8_matmul_workspace(int(M), int(N), _up(int(K), 128), int(n_cu), C.byref(n)))
+    return n.value
+
+
+def fp8_matmul_workspace(M: int, N: int, K: int):
+    """A workspace for fp8_matmul calls of these sizes on the current device, for programs that keep it."""
+    import torch
+    return torch.empty(fp8_matmul_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+
+
+def fp8_matmul(a, a_scales, b, b_scales, out, bias=None, workspace=None, stream=None):
+    """pda_fp8_matmul: a [M, K] (blocks of one row), b [N, K] (blocks of one row or of 128, as its scales say) -> out [M, N] bf16 = a b^T + bias [N] fp32.
+
+    K is the padded length of the rows.  out may be a view whose rows lie apart.
+    """
+    import torch
+    if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[1] or a.shape[1] % 128:
+        raise ValueError(f"a, b: expected [M, K] and [N, K] with rows padded to 128, got {tuple(a.shape)} and {tuple(b.shape)}")
+    M, K = a.shape
+    N = b.shape[0]
+    block = 1 if b_scales is not None and b_scales.dim() == 2 and b_scales.shape[0] == N else 128
+    _expect_fp8(a, a_scales, M, K, 1, "a")
+    _expect_fp8(b, b_scales, N, K, block, "b")
+    if b.dtype is not torch.float8_e4m3fn:
+        raise ValueError(f"b: expected float8_e4m3fn, got {b.dtype}")
+    if out.dtype is not torch.bfloat16 or tuple(out.shape) != (M, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N):
+        raise ValueError(f"out: expected cuda bf16 {(M, N)} with compact rows, got {out.dtype} {tuple(out.shape)} stride {out.stride()}")
+    if bias is not None:
+        _expect(bias, torch.float32, (N,), "bias")
+    _on_current_device(stream, a, a_scales, b, b_scales, out, bias, workspace)
+    if workspace is None:
+        workspace = _workspace(fp8_matmul_workspace_bytes(M, N, K), None, stream)
+    else:
+        _workspace(0, workspace, stream)
+    _check(lib.pda_fp8_matmul(_ptr(a), _fp8_code(a, "a"), _ptr(a_scales), _ptr(b), _ptr(b_scales), block, _ptr(bias), _ptr(out), M, N, K,
+                              out.stride(0) if M > 1 else N, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream)))
+    return out
+
+
+def rms_norm_fwd(x, weight, y, res=None, h=None, y_scales=None, rstd=None, eps: float = 1e-6, stream=None):
+    """pda_rms_norm_fwd: h = res + x (res and h of one type, both or neither), y = the norm of h times weight; x [..., D].
+
+    weight: [D], or [groups, D] with one row for every rows/groups consecutive rows, or None.  y: fp32 or bf16 of the shape of x, or
+    float8_e4m3fn [rows, D padded to 128] with y_scales (fp8_empty(rows, D)).  rstd [rows] fp32, for rms_norm_bwd, or None.
+    """
+    import torch
+    rows, D, groups = _norm_sizes(stream, x, ((rstd, "rstd"),), ((weight, "weight"),), (res, h, y, y_scales))
+    if (res is None) != (h is None):
+        raise ValueError("res and h go together")
+    if res is not None:
+        _expect(res, res.dtype, x.shape, "res")
+        _expect(h, res.dtype, x.shape, "h")
+    if y.dtype is torch.float8_e4m3fn:
+        _expect_fp8(y, y_scales, rows, D, 1, "y")
+        code = PDA_E4M3
+    else:
+        _expect(y, y.dtype, x.shape, "y")
+        code = _type_code(y, "y")
+        if y_scales is not None:
+            raise ValueError("y_scales go with an 8-bit y")
+    _check(lib.pda_rms_norm_fwd(_ptr(x), _type_code(x, "x"), _ptr(res), 0 if res is None else _type_code(res, "res"), _ptr(weight), _ptr(h), _ptr(y), code,
+                                _ptr(y_scales), _ptr(rstd), rows, groups, D, float(eps), _stream_handle(stream)))
+    return h, y, y_scales, rstd
+
+
+def rms_norm_bwd_workspace_bytes(rows: int, D: int, groups: int = 1, n_cu: int = 0) -> int:
+    """pda_rms_norm_bwd_workspace; n_cu = 0 asks the current device."""
+    n = C.c_int64(0)
+    _check(lib.pda_rms_norm_bwd_workspace(int(rows), int(groups), int(D), int(n_cu), C.byref(n)))
+    return n.value
+
+
+def rms_norm_bwd_workspace(rows: int, D: int, groups: int = 1):
+    """A workspace for rms_norm_bwd calls of these sizes on the current device, for programs that keep it."""
+    import torch
+    return torch.empty(rms_norm_bwd_workspace_bytes(rows, D, groups), dtype=torch.uint8, device="cuda")
+
+
+def rms_norm_bwd(dy, h, weight, rstd, dh, dweight, dres=None, workspace=None, stream=None):
+    """pda_rms_norm_bwd: dy (fp32 or bf16), h, weight, rstd of the forward call, dres (the gradient that reaches h past the norm, or None)
+    -> dh like h, the gradient of res and x, and dweight [D] or [groups, D]; dh or dweight may be None.
+    """
+    rows, D, groups = _norm_sizes(stream, h, ((rstd, "rstd"),), ((weight, "weight"), (dweight, "dweight")), (dy, dres, dh, workspace))
+    _expect(dy, dy.dtype, h.shape, "dy")
+    for t, name in ((dres, "dres"), (dh, "dh")):
+        if t is not None:
+            _expect(t, h.dtype, h.shape, name)
+    if workspace is None:
+        workspace = _workspace(rms_norm_bwd_workspace_bytes(rows, D, groups) if dweight is not None else 0, None, stream)
+    else:
+        _workspace(0, workspace, stream)
+    _check(lib.pda_rms_norm_bwd(_ptr(dy), _type_code(dy, "dy"), _ptr(h), _type_code(h, "h"), _ptr(weight), _ptr(rstd), _ptr(dres), _ptr(dh), _ptr(dweight),
+                                rows, groups, D, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream)))
+    return dh, dweight
+
+
+def rope_frequencies(n: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original: float = 4096, slow_turns: float = 1.0,
+                     fast_turns: float = 32.0):
+    """pda_rope_frequencies: (n radians a position, what queries and keys are multiplied by).  scaling: plain, linear, base or blend."""
+    out, magnitude = (C.c_double * max(int(n), 1))(), C.c_double(0)
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: expected one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
+    _check(lib.pda_rope_frequencies(int(n), float(base), ROPE_SCALINGS[scaling], float(factor), float(original), float(slow_turns), float(fast_turns),
+                                    out, C.byref(magnitude)))
+    return list(out), magnitude.value
+
+
+class Rope:
+    """What turns: freqs (radians a position, one for each pair of columns), the layout of the pairs (interleaved or half) and how many of them
+    turn with each axis of a position (default: all with one).  No frequencies: nothing turns.  Made once, used by every call."""
+
+    def __init__(self, freqs, layout: str = "interleaved", axis_pairs: Optional[Sequence[int]] = None):
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError(f"layout: expected one of {sorted(ROPE_LAYOUTS)}, got {layout!r}")
+        freqs = [float(f) for f in freqs]
+        pairs = [len(freqs)] if axis_pairs is None else [int(n) for n in axis_pairs]
+        if not 1 <= len(pairs) <= PDA_ROPE_MAX_AXES or any(n < 0 for n in pairs) or sum(pairs) != len(freqs):
+            raise ValueError(f"axis_pairs: expected up to {PDA_ROPE_MAX_AXES} counts that sum to {len(freqs)}, got {pairs}")
+        if len(freqs) % 4 or len(freqs) > 64:
+            raise ValueError(f"freqs: expected a multiple of 4 of them, at most 64, got {len(freqs)}")
+        self.rot, self.layout, self.axes = 2 * len(freqs), layout, len(pairs)
+        self._freqs = (C.c_double * max(len(freqs), 1))(*freqs)
+        self._pairs = (C.c_int * PDA_ROPE_MAX_AXES)(*pairs)
+
+    def at(self, positions, first: int, B: int, S: int) -> RopeStruct:
+        """The description for one call (positions, checked, must outlive it)."""
+        import torch
+        pos_batch = 0
+        if positions is not None:
+            if first:
+                raise ValueError("positions and first: expected one of them")
+            shape = tuple(positions.shape)
+            if positions.dtype is not torch.int32 or not positions.is_cuda or not positions.is_contiguous() or \
+                    shape not in ((S, self.axes), (B, S, self.axes), (1, S, self.axes)):
+                raise ValueError(f"positions: expected contiguous cuda int32 {(S, self.axes)} or {(B, S, self.axes)}, got {positions.dtype} {shape}")
+            pos_batch = S * self.axes if len(shape) == 3 and shape[0] == B else 0
+        return RopeStruct(self.rot, ROPE_LAYOUTS[self.layout], self.axes, self._pairs, C.cast(self._freqs, C.POINTER(C.c_double)), _ptr(positions), pos_batch, int(first))
+
+
+def _token_strides(t, B, S, H, d, name):
+    """(batch stride, token stride) of a [B,S,H,d] view whose tokens are compact."""
+    st = t.stride()
+    if tuple(t.shape) != (B, S, H, d) or not t.is_cuda or (d > 1 and st[3] != 1) or (H > 1 and st[2] != d):
+        raise ValueError(f"{name}: expected cuda {(B, S, H, d)} with compact tokens, got {tuple(t.shape)} stride {st}")
+    return (int(st[0]) if B > 1 else 0), (int(st[1]) if S > 1 else 0)
+
+
+def _head_strides(t, B, H, S, d, name):
+    """(batch stride, head stride) of a bf16 [B,H,S,d] view whose heads are compact."""
+    import torch
+    if t.dtype is not torch.bfloat16 or tuple(t.shape) != (B, H, S, d):
+        raise ValueError(f"{name}: expected bf16 {(B, H, S, d)}, got {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if not t.is_cuda or st[3] != 1 or (S > 1 and st[2] != d):
+        raise ValueError(f"{name}: rows must be compact on the GPU (stride {st})")
+    return (int(st[0]) if B > 1 else 0), (int(st[1]) if H > 1 else 0)
+
+
+def pack_heads_rope(x, y, rope: Rope, positions=None, first: int = 0, unit_rms: bool = False, premul: float = 1.0, stream=None):
+    """pda_pack_heads_rope: x [B,S,H,d] fp32 or bf16 (a view with compact tokens, e.g. a third of a fused projection) -> y [B,H,S,d] bf16 (a view
+    with compact heads, e.g. a part of a longer sequence), normalised as by pack_heads and turned by rope.
+
+    positions: int32 [S, axes] or [B, S, axes]; None: token s is at first + s.
+    """
+    B, S, H, d = x.shape
+    xs = _token_strides(x, B, S, H, d, "x")
+    ys = _head_strides(y, B, H, S, d, "y")
+    _on_current_device(stream, x, y, positions)
+    _check(lib.pda_pack_heads_rope(_ptr(x), _type_code(x, "x"), *xs, _ptr(y), *ys, B, S, H, d, C.byref(rope.at(positions, first, B, S)),
+                                   1 if unit_rms else 0, float(premul), _stream_handle(stream)))
+    return y
+
+
+def pack_heads_rope_bwd(dy, x, dx, rope: Rope, positions=None, first: int = 0, unit_rms: bool = False, premul: float = 1.0, stream=None):
+    """pda_pack_heads_rope_bwd: dy [B,H,S,d] bf16, the pack's x (None without unit_rms) -> dx [B,S,H,d] of x's type; views as for pack_heads_rope."""
+    B, S, H, d = dx.shape
+    ds = _token_strides(dx, B, S, H, d, "dx")
+    gs = _head_strides(dy, B, H, S, d, "dy")
+    xs = (0, 0)
+    if unit_rms:
+        if x is None:
+            raise ValueError("x: needed with unit_rms")
+        if x.dtype is not dx.dtype:
+            raise ValueError(f"x and dx: expected one type, got {x.dtype} and {dx.dtype}")
+        xs = _token_strides(x, B, S, H, d, "x")
+    _on_current_device(stream, dy, x, dx, positions)
+    _check(lib.pda_pack_heads_rope_bwd(_ptr(dy), *gs, _ptr(x) if unit_rms else None, _type_code(dx, "dx"), *xs, _ptr(dx), *ds, B, S, H, d,
+                                       C.byref(rope.at(positions, first, B, S)), 1 if unit_rms else 0, float(premul), _stream_handle(stream)))
     return dx
 
 

@@ -1,0 +1,288 @@
+// Root-mean-square norm, forward (with the residual's addition in front and 8-bit results behind) and backward, bound by HBM: every element is
+// read once, held in fp32 registers across the sum over its row, and written once.  Threads of a row, accesses and the backward pass's sums over
+// rows as in layer_norm.hip, where the reasons stand.
+//
+// Forward, the types of x, the residual and y are branches that all threads take alike (36 combinations of them would otherwise be as many kernels
+// a row length); an access by groups of four keeps a block of 128 columns in 32 consecutive lanes, whose largest magnitude five lane permutations find.
+#include <hip/hip_runtime.h>
+#include "attn_internal.h"
+#include "fp8_device.h"
+#include "proj_internal.h"
+#include "row_io.h"
+
+namespace pda {
+
+template <bool VEC, int TPR, int NV>
+__device__ __forceinline__ void load_row(const void* p, int type, int64_t at, int D, int t, float (&x)[NV][4]) {
+    if (type == PDA_BF16) RowIO<__bf16, VEC, TPR, NV>::load(static_cast<const __bf16*>(p) + at, D, t, x);
+    else RowIO<float, VEC, TPR, NV>::load(static_cast<const float*>(p) + at, D, t, x);
+}
+template <bool VEC, int TPR, int NV>
+__device__ __forceinline__ void store_row(void* p, int type, int64_t at, int D, int t, const float (&x)[NV][4]) {
+    if (type == PDA_BF16) RowIO<__bf16, VEC, TPR, NV>::store(static_cast<__bf16*>(p) + at, D, t, x);
+    else RowIO<float, VEC, TPR, NV>::store(static_cast<float*>(p) + at, D, t, x);
+}
+
+template <bool VEC, int TPR, int NV>
+__global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const RmsNormParams p) {
+    constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
+    __shared__ float lds[TPR > 64 ? 2 * (TPR / 64) : 1];
+    const int t = threadIdx.x % TPR, D = p.D;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW + threadIdx.x / TPR;
+    if (r >= p.rows) return;                                    // RPW > 1: no barrier follows
+    float h[NV][4], ss = 0.f, zero = 0.f;
+    load_row<VEC, TPR, NV>(p.x, p.x_type, r * D, D, t, h);
+    if (p.res) {
+        float a[NV][4];
+        load_row<VEC, TPR, NV>(p.res, p.h_type, r * D, D, t, a);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[i][e] += a[i][e];
+        if (p.h_type == PDA_BF16)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][e] = (float)(__bf16)h[i][e];      // the stream as it is stored is what is normalised
+        store_row<VEC, TPR, NV>(p.h, p.h_type, r * D, D, t, h);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ss = __builtin_fmaf(h[i][e], h[i][e], ss);
+    row_sum<TPR>(ss, zero, lds);
+    const float rstd = 1.0f / sqrtf(ss / (float)D + p.eps);
+    const int64_t g = p.groups == 1 ? 0 : (unsigned)r / (unsigned)p.group_rows;       // rows < 2^31
+    if (p.weight) {
+        float w[NV][4];
+        RowIO<float, VEC, TPR, NV>::load(p.weight + g * D, D, t, w);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[i][e] *= rstd * w[i][e];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[i][e] *= rstd;
+    }
+    if (p.y_type == PDA_E4M3) {
+        if constexpr (TPR >= 32) {
+            const int64_t cols = fp8_cols(D), scale_cols = fp8_scale_cols(D);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + t) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][e] = c + e < D ? h[i][e] : 0.f;       // (0 times a NaN or an infinity above)
+                float top = fmaxf(fmaxf(finite_magnitude(h[i][0]), finite_magnitude(h[i][1])), fmaxf(finite_magnitude(h[i][2]), finite_magnitude(h[i][3])));
+                top = lane_max<32>(top);
+                const unsigned byte = scale_byte<false>(top);
+                const float f = inverse_scale(byte);
+                if (c < cols) {                                 // (a block of lanes alike)
+                    const unsigned q = pack_fp8<false>(h[i][0] * f, h[i][1] * f, h[i][2] * f, h[i][3] * f);
+                    __builtin_nontemporal_store(q, reinterpret_cast<unsigned*>(static_cast<unsigned char*>(p.y) + r * cols + c));
+                    if (t % 32 == 0) p.y_scales[r * scale_cols + c / 128] = (uint8_t)byte;
+                }
+            }
+        }
+    } else {
+        store_row<VEC, TPR, NV>(p.y, p.y_type, r * D, D, t, h);
+    }
+    if (t == 0 && p.rstd) p.rstd[r] = rstd;
+}
+
+template <typename TY, typename TH, bool VEC, int TPR, int NV>
+__global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_bwd_kernel(const RmsNormParams p) {
+    constexpr int RPW = ln_threads(TPR) / TPR;
+    using X = RowIO<TH, VEC, TPR, NV>;
+    using Y = RowIO<TY, VEC, TPR, NV>;
+    using W = RowIO<float, VEC, TPR, NV>;
+    __shared__ float lds[TPR > 64 ? 4 * (TPR / 64) : 1];
+    int par = 0;
+    __shared__ float joined[RPW > 1 ? RPW * NV * 4 * TPR : 1];
+    const int t = threadIdx.x % TPR, own = threadIdx.x / TPR, D = p.D;
+    const int64_t g = blockIdx.y;
+    const float inv_d = 1.0f / (float)D;
+    float sw[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sw[i][e] = 0.f;
+    const int64_t step = RPW * p.chunks, r0 = g * p.group_rows;
+    const TH* hp = static_cast<const TH*>(p.h);
+    const TY* yp = static_cast<const TY*>(p.x);
+    const TH* rp = static_cast<const TH*>(p.res);
+    int64_t n = (int64_t)blockIdx.x * RPW + own;
+    typename X::Group hn[NV], rn[NV];
+    typename Y::Group yn[NV];
+    float rstd_n = 0.f;
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+        X::fetch(hp + r * D, D, t, hn);
+        Y::fetch(yp + r * D, D, t, yn);
+        if (rp) X::fetch(rp + r * D, D, t, rn);
+        rstd_n = p.rstd[r];
+    };
+    if (n < p.group_rows) fetch(r0 + n);
+    for (; n < p.group_rows; n += step) {                      // RPW == 1: all threads of the workgroup alike
+        const int64_t r = r0 + n;
+        float hh[NV][4], dy[NV][4], dr[NV][4], w[NV][4], a = 0.f, b = 0.f;
+        const float rstd = rstd_n;
+        if (p.weight) {
+            typename W::Group wn[NV];
+            W::fetch(p.weight + g * D, D, t, wn);
+            W::settle(wn, D, t);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[i][e] = W::value(wn, i, e);
+        }
+        X::settle(hn, D, t);
+        Y::settle(yn, D, t);
+        if (rp) X::settle(rn, D, t);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                hh[i][e] = X::value(hn, i, e) * rstd;           // columns behind D: zeros
+                dy[i][e] = Y::value(yn, i, e);
+                dr[i][e] = rp ? X::value(rn, i, e) : 0.f;
+            }
+        if (n + step < p.group_rows) fetch(r + step);           // the next row travels under this one's arithmetic
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sw[i][e] = __builtin_fmaf(dy[i][e], hh[i][e], sw[i][e]);
+                if (p.weight) dy[i][e] *= w[i][e];
+                b = __builtin_fmaf(dy[i][e], hh[i][e], b);
+            }
+        if (p.y) {
+            row_sum<TPR>(a, b, lds + par);
+            par ^= 2 * (TPR / 64);
+            b *= inv_d;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) hh[i][e] = __builtin_fmaf(rstd, dy[i][e] - hh[i][e] * b, dr[i][e]);
+            X::store(static_cast<TH*>(p.y) + r * D, D, t, hh);
+        }
+    }
+    if (!p.dweight) return;
+    // the sums of the workgroup's rows: its own place in the workspace, or the result if it is alone in the group
+    if constexpr (RPW > 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) joined[(own * NV * 4 + i * 4 + e) * TPR + t] = sw[i][e];
+        __syncthreads();
+        if (own != 0) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int o = 1; o < RPW; ++o) sw[i][e] += joined[(o * NV * 4 + i * 4 + e) * TPR + t];
+    }
+    W::store(p.chunks == 1 ? p.dweight + g * D : p.part + (g * p.chunks + blockIdx.x) * D, D, t, sw);
+}
+
+// 32 columns a workgroup, 32 threads a column, each with every 32nd of the chunks.
+__global__ __launch_bounds__(1024) void rms_norm_join_kernel(const RmsNormParams p) {
+    __shared__ float lds[32][33];
+    const int c = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    const int64_t g = blockIdx.y;
+    float s = 0.f;
+    if (col < p.D) {
+        const float* src = p.part + g * p.chunks * p.D + col;
+        for (int64_t k = w; k < p.chunks; k += 32 * 16) {      // sixteen loads in flight
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = k + 32 * i < p.chunks ? src[(k + 32 * i) * p.D] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += x[i];
+        }
+    }
+    lds[w][c] = s;
+    __syncthreads();
+    if (w == 0 && col < p.D) {
+#pragma unroll
+        for (int i = 1; i < 32; ++i) s += lds[i][c];
+        p.dweight[g * p.D + col] = s;
+    }
+}
+
+// rows == 0: no sums
+__global__ __launch_bounds__(256) void rms_norm_zero_kernel(float* a, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) a[i] = 0.f;
+}
+
+template <bool VEC, int TPR, int NV>
+static hipError_t launch_fwd(const RmsNormParams& p, hipStream_t st) {
+    constexpr int rpw = ln_threads(TPR) / TPR;
+    const int64_t n = (p.rows + rpw - 1) / rpw, x = n < 1 << 21 ? n : 1 << 21;           // a launch has fewer than 2^32 threads along x
+    hipLaunchKernelGGL((rms_norm_fwd_kernel<VEC, TPR, NV>), dim3((unsigned)x, (unsigned)((n + x - 1) / x)), dim3(ln_threads(TPR)), 0, st, p);
+    return hipGetLastError();
+}
+
+template <bool VEC>
+static hipError_t launch_fwd(const RmsNormParams& p, hipStream_t st) {
+    const int D = p.y_type == PDA_E4M3 ? (int)fp8_cols(p.D) : p.D;      // the padded columns are written too
+    if (D <= 64) return launch_fwd<VEC, 16, 1>(p, st);
+    if (D <= 128) return launch_fwd<VEC, 32, 1>(p, st);
+    if (D <= 256) return launch_fwd<VEC, 64, 1>(p, st);
+    if (D <= 512) return launch_fwd<VEC, 64, 2>(p, st);
+    if (D <= 1024) return launch_fwd<VEC, 64, 4>(p, st);
+    if constexpr (VEC) {
+        if (D <= 1536) return launch_fwd<VEC, 64, 6>(p, st);
+        if (D <= 2048) return launch_fwd<VEC, 64, 8>(p, st);
+    } else {
+        if (D <= 2048) return launch_fwd<VEC, 256, 2>(p, st);
+    }
+    if (D <= 4096) return launch_fwd<VEC, 512, 2>(p, st);
+    return launch_fwd<VEC, 512, 4>(p, st);                     // up to PDA_LAYER_NORM_MAX = 8192
+}
+
+hipError_t launch_rms_norm_fwd(const RmsNormParams& p, hipStream_t st) {
+    return p.D % 4 == 0 ? launch_fwd<true>(p, st) : launch_fwd<false>(p, st);
+}
+
+template <typename TY, typename TH, bool VEC, int TPR, int NV>
+static hipError_t launch_bwd(const RmsNormParams& p, hipStream_t st) {
+    hipLaunchKernelGGL((rms_norm_bwd_kernel<TY, TH, VEC, TPR, NV>), dim3((unsigned)p.chunks, (unsigned)p.groups), dim3(ln_threads(TPR)), 0, st, p);
+    return hipGetLastError();
+}
+
+template <typename TY, typename TH, bool VEC>
+static hipError_t launch_bwd(const RmsNormParams& p, hipStream_t st) {
+    if (p.D <= 64) return launch_bwd<TY, TH, VEC, 16, 1>(p, st);
+    if (p.D <= 128) return launch_bwd<TY, TH, VEC, 32, 1>(p, st);
+    if (p.D <= 256) return launch_bwd<TY, TH, VEC, 64, 1>(p, st);
+    if (p.D <= 512) return launch_bwd<TY, TH, VEC, 64, 2>(p, st);
+    if (p.D <= 1024) return launch_bwd<TY, TH, VEC, 256, 1>(p, st);
+    if (p.D <= 2048) return launch_bwd<TY, TH, VEC, 256, 2>(p, st);
+    if (p.D <= 4096) return launch_bwd<TY, TH, VEC, 512, 2>(p, st);
+    return launch_bwd<TY, TH, VEC, 512, 4>(p, st);
+}
+
+hipError_t launch_rms_norm_bwd(const RmsNormParams& p, hipStream_t st) {
+    if (p.rows == 0) {
+        const int64_t n = p.groups * p.D;
+        hipLaunchKernelGGL(rms_norm_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, p.dweight, n);
+        return hipGetLastError();
+    }
+    const bool vec = p.D % 4 == 0, y_bf16 = p.x_type == PDA_BF16;
+    hipError_t e;
+    if (p.h_type == PDA_BF16) {
+        if (y_bf16) e = vec ? launch_bwd<__bf16, __bf16, true>(p, st) : launch_bwd<__bf16, __bf16, false>(p, st);
+        else e = vec ? launch_bwd<float, __bf16, true>(p, st) : launch_bwd<float, __bf16, false>(p, st);
+    } else {
+        if (y_bf16) e = vec ? launch_bwd<__bf16, float, true>(p, st) : launch_bwd<__bf16, float, false>(p, st);
+        else e = vec ? launch_bwd<float, float, true>(p, st) : launch_bwd<float, float, false>(p, st);
+    }
+    if (e != hipSuccess || p.chunks == 1 || !p.dweight) return e;
+    hipLaunchKernelGGL(rms_norm_join_kernel, dim3((unsigned)((p.D + 31) / 32), (unsigned)p.groups), dim3(1024), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace pda
