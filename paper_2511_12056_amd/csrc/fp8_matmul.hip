@@ -7,6 +7,7 @@
 #include "attn_device.h"
 #include "attn_internal.h"
 #include "proj_internal.h"
+#include "train_device.h"
 
 namespace pda {
 
@@ -39,12 +40,8 @@ __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsig
                  : "memory", "m0", "vcc");
 }
 
-// Four results of row m, columns n .. n + 3: rounded, or into the part's sums.
-__device__ __forceinline__ void store4(const MatmulParams& p, float* part, int64_t m, int64_t n, f32x4 v) {
-    if (part) {
-        *reinterpret_cast<f32x4*>(part + m * ((p.N + 3) & ~(int64_t)3) + n) = v;       // (rows of the parts are padded to four)
-        return;
-    }
+// Four results of row m, columns n .. n + 3: the bias added, rounded.
+__device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t n, f32x4 v) {
     __bf16* o = p.out + m * p.ldo + n;
     if (p.bias) {
 #pragma unroll
@@ -117,12 +114,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const Matmu
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // operand addresses: granules 2g and 2g + 1 of a row, at their swizzled places
+    // operand addresses: granules g and g + 4 of a row, at their swizzled places
     const int nrow = wn * 64 + (r16 / 4) * 16 + (r16 & 3);      // + 4 j: the row of instruction j, so that a lane's results are 16 consecutive columns
     const int mrow = wm * (TM / WM) + r16;                      // + 16 i
     const unsigned sw_b = ((nrow >> 1) & 1) | ((nrow >> 4) & 3) << 1, sw_a = (mrow >> 1) & 7;
-    const unsigned a_lo = mrow * 128 + (((2 * g) ^ sw_a) * 16), a_hi = mrow * 128 + (((2 * g + 1) ^ sw_a) * 16);
-    const unsigned b_lo = B_AT + nrow * 128 + (((2 * g) ^ sw_b) * 16), b_hi = B_AT + nrow * 128 + (((2 * g + 1) ^ sw_b) * 16);
+    const unsigned a_lo = mrow * 128 + ((g ^ sw_a) * 16), a_hi = a_lo ^ 64;
+    const unsigned b_lo = B_AT + nrow * 128 + ((g ^ sw_b) * 16), b_hi = b_lo ^ 64;
     if (nk > 0) fetch(0);
     for (int t = 0; t < nk; ++t) {
         wait_vmcnt<0>();
@@ -147,7 +144,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const Matmu
         }
     }
     keep(acc);
-    float* to = p.parts > 1 ? p.part + (int64_t)part * p.M * ((p.N + 3) & ~(int64_t)3) : nullptr;
+    if (p.parts > 1) {
+        float* to = p.part + ((int64_t)part * gridDim.x + blockIdx.x) * (TM * TN) + mrow * TN + wn * 64 + 16 * g;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(to + i * 16 * TN + 4 * j) = acc[i][j];
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t m = m0 + mrow + 16 * i;
@@ -155,9 +159,263 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const Matmu
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int64_t n = n0 + wn * 64 + 16 * g + 4 * j;
-                if (n < p.N) store4(p, to, m, n, acc[i][j]);
+                if (n < p.N) store4(p, m, n, acc[i][j]);
             }
     }
+}
+
+// ---- large products -----------------------------------------------------------------------------------------------
+// 256 x 256 results a workgroup of four wavefronts, 128 x 128 each, one workgroup a compute unit and one wavefront a SIMD, with all of its registers: 256
+// accumulators, 128 of operands.  A step is a block of 128: 64 matrix instructions in 64 slots, each with the LDS read or fetch that is
+// due between two of them.  The first 32 take rows 0 to 3 (of 16) with all columns, the others column by column rows 4 to 7, so that every operand register is free
+// some time before its next content is needed: rows 4 to 7 are read at the start of the first half, and the next step's columns and rows 0 to 3 in the second.
+// Two barriers a step: behind the first (slot 11) the block has been read by all, and the one after the next is fetched into its buffer; behind the second
+// (slot 31) the next one has arrived, for which it has had 67 slots at least.
+// A workgroup goes through its items (tiles, or ranges of K of a tile) without a break; blocks are fetched across the border of an item too.
+constexpr int kLargeSa = 0, kLargeSb = 1024, kLargeA = 2048, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeBias = 2 * kLargeStage, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
+constexpr int kLargeGroup = 8;          // tiles of m that share tiles of n in a row
+
+// Place of tile t of tm x tn: large ones in an order in which neighbours share operands, blocks of kLargeGroup tiles of m, tile of n by tile of n; small ones row by row.
+template <int T>
+__device__ __forceinline__ void tile_place(int t, int tm, int tn, int& m, int& n) {
+    if constexpr (T == 256) {
+        const int group = t / (kLargeGroup * tn), rem = t - group * (kLargeGroup * tn);
+        const int left = tm - group * kLargeGroup, gm = left < kLargeGroup ? left : kLargeGroup;
+        n = rem / gm;
+        m = group * kLargeGroup + rem - n * gm;
+    } else {
+        m = t / tn;
+        n = t - m * tn;
+    }
+}
+
+// An accumulator's values where they are wanted: left to itself the compiler copies all 256 out of their registers first, into memory.
+__device__ __forceinline__ f32x4 taken(const f32x4& a) {
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float x;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a[e]));
+        v[e] = x;
+    }
+    return v;
+}
+
+// lds_dma16 and lds_dma4 (above) to lds_base + OFF.
+template <int OFF>
+__device__ __forceinline__ void lds_dma16_to(const void* sbase, unsigned voff, unsigned lds_base) {
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_mov_b64 vcc, %3\n\tglobal_load_lds_dwordx4 %2, vcc" : : "s"(lds_base), "n"(OFF), "v"(voff), "s"(sbase) : "memory", "m0", "vcc", "scc");
+}
+
+struct LargeItem {
+    int64_t m0, n0;
+    int kb0, nk;
+};
+__device__ __forceinline__ LargeItem large_item(const MatmulParams& p, int i) {
+    const int tm = (int)((p.M + 255) / 256), tn = (int)((p.N + 255) / 256), tiles = tm * tn, part = i / tiles;
+    int m, n;
+    tile_place<256>(i - part * tiles, tm, tn, m, n);
+    const int nk_all = (int)(p.K / 128), kb0 = part * p.part_steps, nk = nk_all - kb0 < p.part_steps ? nk_all - kb0 : p.part_steps;
+    return {(int64_t)m * 256, (int64_t)n * 256, kb0, nk};
+}
+
+template <bool E5M2>
+__global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulParams p, int items) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char matmul_smem_[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))matmul_smem_;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w >> 1, wn = w & 1;
+    // this workgroup's items: XCD x (every eighth workgroup) has a consecutive eighth of them
+    const int x = blockIdx.x % 8, per = gridDim.x / 8;
+    const int end = (int)((int64_t)items * (x + 1) / 8);
+    int next = (int)((int64_t)items * x / 8) + blockIdx.x / 8;  // the item that is fetched
+    if (next >= end) return;
+
+    // ---- fetching: a cursor that runs up to two blocks ahead
+    const unsigned char *pa = nullptr, *pb = nullptr, *psa = nullptr, *psb = nullptr;
+    int f_left = 0, f_kb = 0, f_items = 0;                      // blocks left of the item, its block, items begun
+    unsigned f_to = lds0 + w * 1024;                            // stage, this wavefront's place in its chunks
+    const int r0 = w * 8 + lane / 8;                            // row of chunk 0, + 32 i
+    unsigned va[8], vb[8], vsa = 0, vsb = 0;                    // byte offsets of the lane's pieces
+    const auto fetch_begin = [&]() __attribute__((always_inline)) {
+        if (f_left > 0 || next >= end) return;                  // (behind the last item its last block is fetched again, for nobody)
+        const LargeItem it = large_item(p, next);
+        next += per;
+        const int last_m = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256) - 1, last_n = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256) - 1;
+        const unsigned ga = ((lane & 7) ^ ((r0 >> 1) & 7)) * 16, gb = ((lane & 7) ^ (((r0 >> 1) & 1) | ((r0 >> 4) & 1) << 1)) * 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + 32 * i;
+            va[i] = __umul24(r < last_m ? r : last_m, (unsigned)p.K) + ga;
+            vb[i] = __umul24(r < last_n ? r : last_n, (unsigned)p.K) + (i % 2 ? gb ^ 64 : gb);
+        }
+        const int sr = w * 64 + lane, sm = sr < last_m ? sr : last_m, sn = sr < last_n ? sr : last_n;
+        vsa = (unsigned)sm * (unsigned)p.scale_cols;
+        vsb = (unsigned)(sn >> p.b_shift) * (unsigned)p.scale_cols;
+        psa = p.a_scales + it.m0 * p.scale_cols;
+        psb = p.b_scales + (it.n0 >> p.b_shift) * p.scale_cols;
+        pa = p.a + it.m0 * p.K + (int64_t)it.kb0 * 128;
+        pb = p.b + it.n0 * p.K + (int64_t)it.kb0 * 128;
+        f_left = it.nk;
+        f_kb = it.kb0;
+        if (p.bias && p.parts == 1) {                           // 64 values a wavefront; four places, because an item of one block lets the fetch run two items ahead
+            lds_dma4(p.bias + it.n0, (unsigned)sn * 4, lds0 + kLargeBias + (f_items & 3) * 1024 + w * 256);
+        }
+        ++f_items;
+    };
+    // piece q of a block: 0 to 7 rows of a, 8 to 15 of b, 16 and 17 their scales
+    const auto fetch = [&](auto piece) __attribute__((always_inline)) {
+        constexpr int q = decltype(piece)::value;
+        if constexpr (q < 8) {
+            lds_dma16_to<kLargeA + q * 4096>(pa, va[q], f_to);
+        } else if constexpr (q < 16) {
+            lds_dma16_to<kLargeB + (q - 8) * 4096>(pb, vb[q - 8], f_to);
+        } else {
+            lds_dma4((q == 16 ? psa : psb) + (f_kb & ~3), q == 16 ? vsa : vsb, f_to + (q == 16 ? kLargeSa : kLargeSb) - w * 768);
+        }
+    };
+    const auto fetch_end = [&]() __attribute__((always_inline)) {
+        --f_left;
+        const int more = f_left > 0 ? 1 : 0;
+        pa += 128 * more;
+        pb += 128 * more;
+        f_kb += more;
+        f_to = lds0 + w * 1024 + (lds0 + w * 1024 + kLargeStage - f_to);          // the other stage
+    };
+
+    // ---- operands.  Granules g and g + 4 of a row, at their swizzled places (LDS serves 16-byte reads of 16 lanes at a time, from two neighbouring g: with 2g and
+    // 2g + 1 half of its time went into bank conflicts).  nrow + 64 (j / 4) + 4 (j % 4) is the row of b of column block j, so that a lane's results are 16 consecutive
+    // columns in each half (bits 2, 3 and 6, which b's swizzle does not look at)
+    const int r16 = lane & 15, g = lane >> 4;
+    const int mrow = wm * 128 + r16, nrow = wn * 128 + (r16 / 4) * 16 + (r16 & 3);
+    const unsigned ra = kLargeA + mrow * 128 + ((g ^ (r16 >> 1)) * 16), rb = kLargeB + nrow * 128 + ((g ^ (r16 >> 1)) * 16);
+    const unsigned ra2 = kLargeA + ((ra - kLargeA) ^ 64), rb2 = kLargeB + ((rb - kLargeB) ^ 64);
+    i32x8 fa[8], fb[8];
+    int sa[8], sb[8];
+    f32x4 acc[8][8];
+    const unsigned char* s = matmul_smem_;                      // the stage that is read
+    const unsigned char* s_byte = matmul_smem_;                 // + the block's byte of a word of scales
+    const auto read_a = [&](auto i) __attribute__((always_inline)) {
+        constexpr int I = decltype(i)::value;
+        fa[I] = join8(*reinterpret_cast<const i32x4*>(s + ra + I * 2048), *reinterpret_cast<const i32x4*>(s + ra2 + I * 2048));
+        sa[I] = s_byte[kLargeSa + mrow * 4 + I * 64];
+    };
+    const auto read_b = [&](auto j) __attribute__((always_inline)) {
+        constexpr int J = decltype(j)::value, at = (J / 4) * 8192 + (J % 4) * 512;
+        fb[J] = join8(*reinterpret_cast<const i32x4*>(s + rb + at), *reinterpret_cast<const i32x4*>(s + rb2 + at));
+        sb[J] = s_byte[kLargeSb + nrow * 4 + at / 32];
+    };
+    const auto next_stage = [&](int kb) __attribute__((always_inline)) {
+        s = s == matmul_smem_ ? matmul_smem_ + kLargeStage : matmul_smem_;
+        s_byte = s + (kb & 3);
+    };
+
+    static_for<0, 2>([&](auto) __attribute__((always_inline)) {
+        fetch_begin();
+        static_for<0, 18>([&](auto q) __attribute__((always_inline)) { fetch(q); });
+        fetch_end();
+    });
+    int item = (int)((int64_t)items * x / 8) + blockIdx.x / 8, items_read = 0;
+    LargeItem it = large_item(p, item);
+    wait_vmcnt<0>();
+    asm volatile("s_barrier" ::: "memory");
+    s_byte = s + (it.kb0 & 3);
+    static_for<0, 8>([&](auto j) __attribute__((always_inline)) { read_b(j); });
+    static_for<0, 4>([&](auto i) __attribute__((always_inline)) { read_a(i); });
+    bool stored = false;                                        // this wavefront has stored a whole tile's part just now: 32 stores behind the last fetch
+    for (;;) {
+        const int item_n = item + per;
+        const bool more = item_n < end;
+        const LargeItem it_n = large_item(p, more ? item_n : item);
+        const auto run = [&](auto first, int kb_next) __attribute__((always_inline)) {
+            static_for<0, 64>([&](auto slot) __attribute__((always_inline)) {
+                constexpr int k = decltype(slot)::value, k2 = k - 32;
+                constexpr int i = k < 32 ? k / 8 : 4 + k2 % 4, j = k < 32 ? k % 8 : k2 / 4;
+                acc[i][j] = mfma<E5M2>(fb[j], fa[i], decltype(first)::value ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[i][j], sb[j], sa[i]);
+                asm volatile("" : "+a"(acc[i][j]));             // in its slot: nothing else keeps it there
+                if constexpr (k < 8 && k % 2 == 0) read_a(std::integral_constant<int, 4 + k / 2>{});
+                if constexpr (k == 11) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    fetch_begin();
+                }
+                if constexpr (k >= 12 && k < 30) fetch(std::integral_constant<int, k >= 12 && k < 30 ? k - 12 : 0>{});
+                if constexpr (k == 31) {
+                    fetch_end();
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (decltype(first)::value) {
+                        if (stored) wait_vmcnt<18 + 32>();      // the stores of the tile ahead may still be on their way
+                        else wait_vmcnt<18>();
+                        asm volatile("s_barrier" ::: "memory");
+                    } else {
+                        asm volatile("s_waitcnt vmcnt(18)\n\ts_barrier" ::: "memory");
+                    }
+                    next_stage(kb_next);
+                }
+                if constexpr (k2 >= 0 && k2 < 16 && k2 % 4 == 1) read_a(std::integral_constant<int, k2 >= 0 ? k2 / 4 : 0>{});
+                if constexpr (k2 >= 0 && k2 % 4 == 3) read_b(std::integral_constant<int, k2 >= 0 ? k2 / 4 : 0>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        run(std::true_type{}, it.nk > 1 ? it.kb0 + 1 : it_n.kb0);
+        for (int t = 1; t < it.nk; ++t) run(std::false_type{}, t + 1 < it.nk ? it.kb0 + t + 1 : it_n.kb0);
+        // (the accumulators come out of the loop or of the step ahead of it, so no instruction can be moved down here: see keep)
+        asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");       // behind the last matrix instruction, for what reads its result in inline assembly
+        const int l = opaque_lane(), row = wm * 128 + (l & 15), col = wn * 128 + 16 * (l >> 4);      // + 16 i, + 64 (j / 4) + 4 (j % 4)
+        stored = false;
+        if (p.parts > 1) {
+            float* to = p.part + ((int64_t)item << 16) + row * 256 + col;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + i * 4096 + (j / 4) * 64 + (j % 4) * 4) = taken(acc[i][j]);
+        } else {
+            const int rows = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256), cols = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256);
+            __bf16* to = p.out + it.m0 * p.ldo + it.n0;
+            f32x4 bias[8];
+            const float* b = reinterpret_cast<const float*>(matmul_smem_ + kLargeBias + (items_read & 3) * 1024) + col;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bias[j] = p.bias ? *reinterpret_cast<const f32x4*>(b + (j / 4) * 64 + (j % 4) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+            const auto rounded = [&](const f32x4& a, const f32x4& c) __attribute__((always_inline)) {
+                const f32x4 v = taken(a);
+                return u32x2{pack_bf16(v[0] + c[0], v[1] + c[1]), pack_bf16(v[2] + c[2], v[3] + c[3])};
+            };
+            if (cols == 256 && p.vec_out) {
+                stored = rows == 256;
+                const unsigned pitch = (unsigned)p.ldo * 32;    // bytes of 16 rows
+                unsigned at = (unsigned)row * (unsigned)p.ldo * 2 + col * 2;
+                static_for<0, 8>([&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value;
+                    if (row + 16 * i < rows)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2) {
+                            const u32x2 lo = rounded(acc[i][j], bias[j]), hi = rounded(acc[i][j + 1], bias[j + 1]);
+                            *reinterpret_cast<u32x4*>(reinterpret_cast<unsigned char*>(to) + at + (j / 4) * 128 + (j % 4) * 8) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                        }
+                    at += pitch;
+                });
+            } else {                                            // 16 rows at a time through LDS, element by element
+                __bf16* mine = reinterpret_cast<__bf16*>(matmul_smem_ + kLargeEdge + w * 4096);
+                static_for<0, 8>([&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<u32x2*>(mine + (l & 15) * 128 + 16 * (l >> 4) + (j / 4) * 64 + (j % 4) * 4) = rounded(acc[i][j], bias[j]);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    const int left = rows - wm * 128 - 16 * i, r1 = left < 16 ? left : 16;
+#pragma unroll 1
+                    for (int r = 0; r < r1; ++r)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (wn * 128 + h * 64 + l < cols) to[(int64_t)(wm * 128 + 16 * i + r) * p.ldo + wn * 128 + h * 64 + l] = mine[r * 128 + h * 64 + l];
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                });
+            }
+        }
+        ++items_read;
+        if (!more) break;
+        item = item_n;
+        it = it_n;
+    }
+    wait_vmcnt<0>();                                            // no fetch outlives the workgroup's LDS
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------
@@ -201,24 +459,30 @@ __global__ __launch_bounds__(kFewWaves * 64) void fp8_matmul_few_kernel(const Ma
 #pragma unroll
         for (int o = 1; o < kFewWaves; ++o) v += sums[o][i][lane];
         const int64_t m = m0 + 16 * i + r16, n = n0 + 4 * g;
-        if (m < p.M && n < p.N) store4(p, nullptr, m, n, v);
+        if (m < p.M && n < p.N) store4(p, m, n, v);
     }
 }
 
 // ---- sums of the ranges of K --------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulParams p) {
-    const int64_t n4 = (p.N + 3) / 4, m = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (m >= p.M || c >= n4) return;
-    const f32x4* src = reinterpret_cast<const f32x4*>(p.part) + m * n4 + c;
+// Parts hold whole tiles of T x T; four columns a thread.
+template <int T>
+__global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulParams p, int tiles, int tm, int tn) {
+    const int tile = blockIdx.x, r = blockIdx.y * (1024 / T) + threadIdx.x / (T / 4), c = threadIdx.x % (T / 4) * 4;
+    int im, in;
+    tile_place<T>(tile, tm, tn, im, in);
+    const int64_t m = (int64_t)im * T + r, n = (int64_t)in * T + c;
+    if (m >= p.M || n >= p.N) return;
+    const f32x4* src = reinterpret_cast<const f32x4*>(p.part + (int64_t)tile * (T * T) + r * T + c);
     f32x4 v = *src;
-    for (int k = 1; k < p.parts; ++k) v += src[k * p.M * n4];
-    store4(p, nullptr, m, c * 4, v);
+#pragma unroll 4
+    for (int k = 1; k < p.parts; ++k) v += src[(int64_t)k * tiles * (T * T / 4)];
+    store4(p, m, n, v);
 }
 
 // K == 0: the bias
 __global__ __launch_bounds__(256) void fp8_matmul_bias_kernel(const MatmulParams p) {
     const int64_t n4 = (p.N + 3) / 4, m = (int64_t)blockIdx.z * gridDim.y + blockIdx.y, c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (m < p.M && c < n4) store4(p, nullptr, m, c * 4, f32x4{0.f, 0.f, 0.f, 0.f});
+    if (m < p.M && c < n4) store4(p, m, c * 4, f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
 MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t K, int n_cu) {
@@ -230,11 +494,14 @@ MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t K, int n_cu) {
     const int least = large ? 16 : 4;                          // steps of a part
     int64_t parts = n >= room ? 1 : room / n;
     if (parts > nk / least) parts = nk / least > 1 ? nk / least : 1;
-    const int steps = (int)((nk + parts - 1) / parts);
+    const int steps = (int)((nk + parts - 1) / parts + 3) / 4 * 4;       // words of four scales
     return {large ? MatmulPlan::LARGE : MatmulPlan::SMALL, steps > 0 ? (nk + steps - 1) / steps : 1, steps};
 }
 
-int64_t matmul_workspace_bytes(const MatmulPlan& w, int64_t M, int64_t N) { return w.parts > 1 ? w.parts * M * ((N + 3) / 4 * 16) : 0; }
+int64_t matmul_workspace_bytes(const MatmulPlan& w, int64_t M, int64_t N) {
+    const int64_t t = w.form == MatmulPlan::LARGE ? 256 : 128;
+    return w.parts > 1 ? w.parts * ((M + t - 1) / t) * ((N + t - 1) / t) * t * t * 4 : 0;
+}
 
 static dim3 row_grid(const MatmulParams& p) {
     const int64_t y = p.M < 65535 ? p.M : 65535;
@@ -252,8 +519,21 @@ static hipError_t launch_tiles(const MatmulParams& p, hipStream_t st) {
 }
 
 template <bool E5M2>
+static hipError_t launch_large(const MatmulParams& p, hipStream_t st) {
+    static KernelSetup setup;
+    int n_cu = 0;
+    const hipError_t e = setup.ensure(reinterpret_cast<const void*>(fp8_matmul_large_kernel<E5M2>), kLargeSmem, &n_cu);
+    if (e != hipSuccess) return e;
+    const int64_t items = (p.M + 255) / 256 * ((p.N + 255) / 256) * p.parts;
+    if (items > 0x7fffff00) return hipErrorInvalidValue;
+    const int grid = n_cu < 8 ? 8 : n_cu / 8 * 8;
+    hipLaunchKernelGGL(fp8_matmul_large_kernel<E5M2>, dim3((unsigned)grid), dim3(256), kLargeSmem, st, p, (int)items);
+    return hipGetLastError();
+}
+
+template <bool E5M2>
 static hipError_t launch_form(const MatmulParams& p, const MatmulPlan& w, hipStream_t st) {
-    if (w.form == MatmulPlan::LARGE) return launch_tiles<256, 256, 2, 4, E5M2>(p, st);
+    if (w.form == MatmulPlan::LARGE) return launch_large<E5M2>(p, st);
     if (w.form == MatmulPlan::SMALL) return launch_tiles<128, 128, 2, 2, E5M2>(p, st);
     const unsigned x = (unsigned)((p.N + 15) / 16);
     if (p.M <= 16) hipLaunchKernelGGL((fp8_matmul_few_kernel<1, E5M2>), dim3(x), dim3(kFewWaves * 64), 0, st, p);
@@ -265,13 +545,17 @@ static hipError_t launch_form(const MatmulParams& p, const MatmulPlan& w, hipStr
 hipError_t launch_fp8_matmul(MatmulParams p, const MatmulPlan& w, hipStream_t st) {
     p.parts = w.parts;
     p.part_steps = w.part_steps;
+    p.vec_out = p.ldo % 8 == 0 && p.ldo < (int64_t)1 << 22 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;      // 256 rows within 2^32 bytes
     if (p.K == 0) {
         hipLaunchKernelGGL(fp8_matmul_bias_kernel, row_grid(p), dim3(256), 0, st, p);
         return hipGetLastError();
     }
     const hipError_t e = p.e5m2 ? launch_form<true>(p, w, st) : launch_form<false>(p, w, st);
     if (e != hipSuccess || p.parts == 1) return e;
-    hipLaunchKernelGGL(fp8_matmul_join_kernel, row_grid(p), dim3(256), 0, st, p);
+    const int T = w.form == MatmulPlan::LARGE ? 256 : 128, tm = (int)((p.M + T - 1) / T), tn = (int)((p.N + T - 1) / T);
+    const dim3 grid((unsigned)(tm * tn), (unsigned)(T * T / 1024));
+    if (T == 256) hipLaunchKernelGGL(fp8_matmul_join_kernel<256>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
+    else hipLaunchKernelGGL(fp8_matmul_join_kernel<128>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
     return hipGetLastError();
 }
 

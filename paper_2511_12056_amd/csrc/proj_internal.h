@@ -29,13 +29,14 @@ struct MatmulParams {
     const uint8_t* b_scales;
     const float* bias;       // nullable
     __bf16* out;
-    float* part;             // [parts][M][N rounded up to 4] partial sums
+    float* part;             // [parts][tiles][tile] partial sums
     int64_t M, N, K, ldo;
     int64_t scale_cols;      // bytes between rows of scales
     int b_shift;             // 0 or 7: rows of b that share a scale
     int e5m2;                // of a
     int parts;               // ranges of K, each of part_steps blocks of 128 (the last may have fewer)
     int part_steps;
+    int vec_out;             // rows of out lie at multiples of 16 bytes
 };
 // How a product is split over workgroups: the form of its tiles and the ranges of K.
 struct MatmulPlan {
