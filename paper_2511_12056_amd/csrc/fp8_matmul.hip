@@ -168,11 +168,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const Matmu
 // 256 x 256 results a workgroup of four wavefronts, 128 x 128 each, one workgroup a compute unit and one wavefront a SIMD, with all of its registers: 256
 // accumulators, 128 of operands.  A step is a block of 128: 64 matrix instructions in 64 slots, each with the LDS read or fetch that is
 // due between two of them.  The first 32 take rows 0 to 3 (of 16) with all columns, the others column by column rows 4 to 7, so that every operand register is free
-// some time before its next content is needed: rows 4 to 7 are read at the start of the first half, and the next step's columns and rows 0 to 3 in the second.
-// Two barriers a step: behind the first (slot 11) the block has been read by all, and the one after the next is fetched into its buffer; behind the second
-// (slot 31) the next one has arrived, for which it has had 67 slots at least.
+// some time before its next content is needed: rows 4 to 7 are read in the first half, and the next step's columns and rows 0 to 3 in the second.
+// Two barriers a step.  Behind the first (slot 7) all have read the block but its rows 4 to 7, which have arrived: what has been read is fetched for the block
+// after the next.  Behind the second (slot 31) all have read those rows and their scales too, which are fetched, and the rest of the next block has arrived.  A fetch has 54 slots
+// (1 730 cycles) at least, and a wavefront asks for 1 KB every third slot: faster, requests wait in line and matrix instructions behind them.
 // A workgroup goes through its items (tiles, or ranges of K of a tile) without a break; blocks are fetched across the border of an item too.
-constexpr int kLargeSa = 0, kLargeSb = 1024, kLargeA = 2048, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeBias = 2 * kLargeStage, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
+constexpr int kLargeA = 0, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeScales = 2 * kLargeStage, kLargeSa = 0, kLargeSb = 1024, kLargeBias = kLargeScales + 2 * 2048, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
 constexpr int kLargeGroup = 8;          // tiles of m that share tiles of n in a row
 
 // Place of tile t of tm x tn: large ones in an order in which neighbours share operands, blocks of kLargeGroup tiles of m, tile of n by tile of n; small ones row by row.
@@ -207,6 +208,9 @@ __device__ __forceinline__ void lds_dma16_to(const void* sbase, unsigned voff, u
     asm volatile("s_add_u32 m0, %0, %1\n\ts_mov_b64 vcc, %3\n\tglobal_load_lds_dwordx4 %2, vcc" : : "s"(lds_base), "n"(OFF), "v"(voff), "s"(sbase) : "memory", "m0", "vcc", "scc");
 }
 
+// The piece of a block that is fetched in slot k, or -1: every third slot, twelve behind the step's first barrier, four behind the second.
+constexpr int large_piece(int k) { return k >= 8 && k <= 41 && (k - 8) % 3 == 0 ? (k - 8) / 3 : k >= 44 && k <= 53 && (k - 44) % 3 == 0 ? 12 + (k - 44) / 3 : -1; }
+
 struct LargeItem {
     int64_t m0, n0;
     int kb0, nk;
@@ -235,6 +239,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
     int f_left = 0, f_kb = 0, f_items = 0;                      // blocks left of the item, its block, items begun
     unsigned f_to = lds0 + w * 1024;                            // stage, this wavefront's place in its chunks
     const int r0 = w * 8 + lane / 8;                            // row of chunk 0, + 32 i
+    unsigned f_scales = lds0 + kLargeScales + w * 256;
     unsigned va[8], vb[8], vsa = 0, vsb = 0;                    // byte offsets of the lane's pieces
     const auto fetch_begin = [&]() __attribute__((always_inline)) {
         if (f_left > 0 || next >= end) return;                  // (behind the last item its last block is fetched again, for nobody)
@@ -262,16 +267,22 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
         }
         ++f_items;
     };
-    // piece q of a block: 0 to 7 rows of a, 8 to 15 of b, 16 and 17 their scales
+    // piece q of a block: rows of b, 0 to 7; rows 0 to 3 (of 16) of a's wavefronts, 8 to 11; rows 4 to 7, 12 to 15
     const auto fetch = [&](auto piece) __attribute__((always_inline)) {
         constexpr int q = decltype(piece)::value;
         if constexpr (q < 8) {
-            lds_dma16_to<kLargeA + q * 4096>(pa, va[q], f_to);
-        } else if constexpr (q < 16) {
-            lds_dma16_to<kLargeB + (q - 8) * 4096>(pb, vb[q - 8], f_to);
+            lds_dma16_to<kLargeB + q * 4096>(pb, vb[q], f_to);
         } else {
-            lds_dma4((q == 16 ? psa : psb) + (f_kb & ~3), q == 16 ? vsa : vsb, f_to + (q == 16 ? kLargeSa : kLargeSb) - w * 768);
+            constexpr int i = q < 12 ? (q - 8) / 2 * 4 + q % 2 : (q - 12) / 2 * 4 + 2 + q % 2;      // chunk of 32 rows
+            lds_dma16_to<kLargeA + i * 4096>(pa, va[i], f_to);
         }
+    };
+    // Words of four blocks' scales, with the first of them: a word a row may be a line a row, as many as the block itself has.
+    const auto fetch_scales = [&]() __attribute__((always_inline)) {
+        if ((f_kb & 3) != 0) return;
+        lds_dma4(psa + f_kb, vsa, f_scales + kLargeSa);
+        lds_dma4(psb + f_kb, vsb, f_scales + kLargeSb);
+        f_scales = 2 * (lds0 + kLargeScales + w * 256) + 2048 - f_scales;
     };
     const auto fetch_end = [&]() __attribute__((always_inline)) {
         --f_left;
@@ -279,7 +290,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
         pa += 128 * more;
         pb += 128 * more;
         f_kb += more;
-        f_to = lds0 + w * 1024 + (lds0 + w * 1024 + kLargeStage - f_to);          // the other stage
+        f_to = 2 * (lds0 + w * 1024) + kLargeStage - f_to;      // the other stage
     };
 
     // ---- operands.  Granules g and g + 4 of a row, at their swizzled places (LDS serves 16-byte reads of 16 lanes at a time, from two neighbouring g: with 2g and
@@ -293,7 +304,8 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
     int sa[8], sb[8];
     f32x4 acc[8][8];
     const unsigned char* s = matmul_smem_;                      // the stage that is read
-    const unsigned char* s_byte = matmul_smem_;                 // + the block's byte of a word of scales
+    const unsigned char* s_scales = matmul_smem_ + kLargeScales;        // its words of scales, and its byte in them
+    const unsigned char* s_byte = s_scales;
     const auto read_a = [&](auto i) __attribute__((always_inline)) {
         constexpr int I = decltype(i)::value;
         fa[I] = join8(*reinterpret_cast<const i32x4*>(s + ra + I * 2048), *reinterpret_cast<const i32x4*>(s + ra2 + I * 2048));
@@ -306,19 +318,20 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
     };
     const auto next_stage = [&](int kb) __attribute__((always_inline)) {
         s = s == matmul_smem_ ? matmul_smem_ + kLargeStage : matmul_smem_;
-        s_byte = s + (kb & 3);
+        if ((kb & 3) == 0) s_scales = s_scales == matmul_smem_ + kLargeScales ? matmul_smem_ + kLargeScales + 2048 : matmul_smem_ + kLargeScales;
+        s_byte = s_scales + (kb & 3);
     };
 
     static_for<0, 2>([&](auto) __attribute__((always_inline)) {
         fetch_begin();
-        static_for<0, 18>([&](auto q) __attribute__((always_inline)) { fetch(q); });
+        static_for<0, 16>([&](auto q) __attribute__((always_inline)) { fetch(q); });
+        fetch_scales();
         fetch_end();
     });
     int item = (int)((int64_t)items * x / 8) + blockIdx.x / 8, items_read = 0;
     LargeItem it = large_item(p, item);
     wait_vmcnt<0>();
     asm volatile("s_barrier" ::: "memory");
-    s_byte = s + (it.kb0 & 3);
     static_for<0, 8>([&](auto j) __attribute__((always_inline)) { read_b(j); });
     static_for<0, 4>([&](auto i) __attribute__((always_inline)) { read_a(i); });
     bool stored = false;                                        // this wavefront has stored a whole tile's part just now: 32 stores behind the last fetch
@@ -332,25 +345,24 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 constexpr int i = k < 32 ? k / 8 : 4 + k2 % 4, j = k < 32 ? k % 8 : k2 / 4;
                 acc[i][j] = mfma<E5M2>(fb[j], fa[i], decltype(first)::value ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[i][j], sb[j], sa[i]);
                 asm volatile("" : "+a"(acc[i][j]));             // in its slot: nothing else keeps it there
-                if constexpr (k < 8 && k % 2 == 0) read_a(std::integral_constant<int, 4 + k / 2>{});
-                if constexpr (k == 11) {
+                if constexpr (k == 7) {
                     __builtin_amdgcn_sched_barrier(0);
-                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    if (decltype(first)::value && stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(16 + 32) : "memory");     // the stores of the tile ahead may still be on their way
+                    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(16) : "memory");
+                    asm volatile("s_barrier" ::: "memory");
                     fetch_begin();
                 }
-                if constexpr (k >= 12 && k < 30) fetch(std::integral_constant<int, k >= 12 && k < 30 ? k - 12 : 0>{});
+                if constexpr (k >= 8 && k < 16 && k % 2 == 0) read_a(std::integral_constant<int, 4 + (k >= 8 && k < 16 ? (k - 8) / 2 : 0)>{});
+                if constexpr (large_piece(k) >= 0) fetch(std::integral_constant<int, large_piece(k) >= 0 ? large_piece(k) : 0>{});
                 if constexpr (k == 31) {
-                    fetch_end();
                     __builtin_amdgcn_sched_barrier(0);
-                    if constexpr (decltype(first)::value) {
-                        if (stored) wait_vmcnt<18 + 32>();      // the stores of the tile ahead may still be on their way
-                        else wait_vmcnt<18>();
-                        asm volatile("s_barrier" ::: "memory");
-                    } else {
-                        asm volatile("s_waitcnt vmcnt(18)\n\ts_barrier" ::: "memory");
-                    }
+                    if (decltype(first)::value && stored) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(4 + 8 + 32) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(4 + 8) : "memory");
+                    asm volatile("s_barrier" ::: "memory");
                     next_stage(kb_next);
                 }
+                if constexpr (k == 32) fetch_scales();
+                if constexpr (k == 54) fetch_end();
                 if constexpr (k2 >= 0 && k2 < 16 && k2 % 4 == 1) read_a(std::integral_constant<int, k2 >= 0 ? k2 / 4 : 0>{});
                 if constexpr (k2 >= 0 && k2 % 4 == 3) read_b(std::integral_constant<int, k2 >= 0 ? k2 / 4 : 0>{});
                 __builtin_amdgcn_sched_barrier(0);
