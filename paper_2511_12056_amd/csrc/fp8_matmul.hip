@@ -246,12 +246,12 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
         const LargeItem it = large_item(p, next);
         next += per;
         const int last_m = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256) - 1, last_n = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256) - 1;
-        const unsigned ga = ((lane & 7) ^ ((r0 >> 1) & 7)) * 16, gb = ((lane & 7) ^ (((r0 >> 1) & 1) | ((r0 >> 4) & 1) << 1)) * 16;
+        const unsigned ga = ((lane & 7) ^ ((r0 >> 1) & 7)) * 16, gb = ((lane & 7) ^ (((r0 >> 1) & 1) | ((r0 >> 3) & 3) << 1)) * 16;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = r0 + 32 * i;
             va[i] = __umul24(r < last_m ? r : last_m, (unsigned)p.K) + ga;
-            vb[i] = __umul24(r < last_n ? r : last_n, (unsigned)p.K) + (i % 2 ? gb ^ 64 : gb);
+            vb[i] = __umul24(r < last_n ? r : last_n, (unsigned)p.K) + gb;
         }
         const int sr = w * 64 + lane, sm = sr < last_m ? sr : last_m, sn = sr < last_n ? sr : last_n;
         vsa = (unsigned)sm * (unsigned)p.scale_cols;
@@ -294,10 +294,10 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
     };
 
     // ---- operands.  Granules g and g + 4 of a row, at their swizzled places (LDS serves 16-byte reads of 16 lanes at a time, from two neighbouring g: with 2g and
-    // 2g + 1 half of its time went into bank conflicts).  nrow + 64 (j / 4) + 4 (j % 4) is the row of b of column block j, so that a lane's results are 16 consecutive
-    // columns in each half (bits 2, 3 and 6, which b's swizzle does not look at)
+    // 2g + 1 half of its time went into bank conflicts).  nrow + 32 (j / 2) + 4 (j % 2) is the row of b of column block j, so that a lane's results of two blocks are
+    // eight consecutive columns and those of four lanes 64 bytes (bits 2, 5 and 6, which b's swizzle does not look at)
     const int r16 = lane & 15, g = lane >> 4;
-    const int mrow = wm * 128 + r16, nrow = wn * 128 + (r16 / 4) * 16 + (r16 & 3);
+    const int mrow = wm * 128 + r16, nrow = wn * 128 + (r16 / 4) * 8 + (r16 & 3);
     const unsigned ra = kLargeA + mrow * 128 + ((g ^ (r16 >> 1)) * 16), rb = kLargeB + nrow * 128 + ((g ^ (r16 >> 1)) * 16);
     const unsigned ra2 = kLargeA + ((ra - kLargeA) ^ 64), rb2 = kLargeB + ((rb - kLargeB) ^ 64);
     i32x8 fa[8], fb[8];
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
         sa[I] = s_byte[kLargeSa + mrow * 4 + I * 64];
     };
     const auto read_b = [&](auto j) __attribute__((always_inline)) {
-        constexpr int J = decltype(j)::value, at = (J / 4) * 8192 + (J % 4) * 512;
+        constexpr int J = decltype(j)::value, at = (J / 2) * 4096 + (J % 2) * 512;
         fb[J] = join8(*reinterpret_cast<const i32x4*>(s + rb + at), *reinterpret_cast<const i32x4*>(s + rb2 + at));
         sb[J] = s_byte[kLargeSb + nrow * 4 + at / 32];
     };
@@ -372,21 +372,21 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
         for (int t = 1; t < it.nk; ++t) run(std::false_type{}, t + 1 < it.nk ? it.kb0 + t + 1 : it_n.kb0);
         // (the accumulators come out of the loop or of the step ahead of it, so no instruction can be moved down here: see keep)
         asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");       // behind the last matrix instruction, for what reads its result in inline assembly
-        const int l = opaque_lane(), row = wm * 128 + (l & 15), col = wn * 128 + 16 * (l >> 4);      // + 16 i, + 64 (j / 4) + 4 (j % 4)
+        const int l = opaque_lane(), row = wm * 128 + (l & 15), col = wn * 128 + 8 * (l >> 4);       // + 16 i, + 32 (j / 2) + 4 (j % 2)
         stored = false;
         if (p.parts > 1) {
-            float* to = p.part + ((int64_t)item << 16) + row * 256 + col;
+            float* to = p.part + ((int64_t)item << 16) + w * 16384 + l * 4;      // as they lie in the registers: 1 KB a store
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + i * 4096 + (j / 4) * 64 + (j % 4) * 4) = taken(acc[i][j]);
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + (i * 8 + j) * 256) = taken(acc[i][j]);
         } else {
             const int rows = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256), cols = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256);
             __bf16* to = p.out + it.m0 * p.ldo + it.n0;
             f32x4 bias[8];
             const float* b = reinterpret_cast<const float*>(matmul_smem_ + kLargeBias + (items_read & 3) * 1024) + col;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bias[j] = p.bias ? *reinterpret_cast<const f32x4*>(b + (j / 4) * 64 + (j % 4) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 8; ++j) bias[j] = p.bias ? *reinterpret_cast<const f32x4*>(b + (j / 2) * 32 + (j % 2) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
             const auto rounded = [&](const f32x4& a, const f32x4& c) __attribute__((always_inline)) {
                 const f32x4 v = taken(a);
                 return u32x2{pack_bf16(v[0] + c[0], v[1] + c[1]), pack_bf16(v[2] + c[2], v[3] + c[3])};
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
 #pragma unroll
                         for (int j = 0; j < 8; j += 2) {
                             const u32x2 lo = rounded(acc[i][j], bias[j]), hi = rounded(acc[i][j + 1], bias[j + 1]);
-                            *reinterpret_cast<u32x4*>(reinterpret_cast<unsigned char*>(to) + at + (j / 4) * 128 + (j % 4) * 8) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                            *reinterpret_cast<u32x4*>(reinterpret_cast<unsigned char*>(to) + at + j * 32) = u32x4{lo[0], lo[1], hi[0], hi[1]};
                         }
                     at += pitch;
                 });
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 static_for<0, 8>([&](auto ic) __attribute__((always_inline)) {
                     constexpr int i = decltype(ic)::value;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) *reinterpret_cast<u32x2*>(mine + (l & 15) * 128 + 16 * (l >> 4) + (j / 4) * 64 + (j % 4) * 4) = rounded(acc[i][j], bias[j]);
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<u32x2*>(mine + (l & 15) * 128 + 8 * (l >> 4) + (j / 2) * 32 + (j % 2) * 4) = rounded(acc[i][j], bias[j]);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     const int left = rows - wm * 128 - 16 * i, r1 = left < 16 ? left : 16;
 #pragma unroll 1
@@ -476,19 +476,36 @@ __global__ __launch_bounds__(kFewWaves * 64) void fp8_matmul_few_kernel(const Ma
 }
 
 // ---- sums of the ranges of K --------------------------------------------------------------------------------------
-// Parts hold whole tiles of T x T; four columns a thread.
+// Parts hold whole tiles of T x T, small ones by rows, large ones as they lay in the registers; eight columns a thread.
 template <int T>
 __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulParams p, int tiles, int tm, int tn) {
-    const int tile = blockIdx.x, r = blockIdx.y * (1024 / T) + threadIdx.x / (T / 4), c = threadIdx.x % (T / 4) * 4;
-    int im, in;
+    const int tile = blockIdx.x, e = blockIdx.y * 256 + threadIdx.x;
+    int im, in, r, c, at, second;                               // row and column in the tile, place of its first four sums, of the others behind them
     tile_place<T>(tile, tm, tn, im, in);
+    if constexpr (T == 256) {
+        const int lane = e & 63, jj = e >> 6 & 3, i = e >> 8 & 7, w = e >> 11;
+        r = (w >> 1) * 128 + i * 16 + (lane & 15);
+        c = (w & 1) * 128 + jj * 32 + (lane >> 4) * 8;
+        at = ((w * 64 + i * 8 + jj * 2) * 64 + lane) * 4;
+        second = 256;
+    } else {
+        r = e / (T / 8);
+        c = e % (T / 8) * 8;
+        at = r * T + c;
+        second = 4;
+    }
     const int64_t m = (int64_t)im * T + r, n = (int64_t)in * T + c;
     if (m >= p.M || n >= p.N) return;
-    const f32x4* src = reinterpret_cast<const f32x4*>(p.part + (int64_t)tile * (T * T) + r * T + c);
-    f32x4 v = *src;
+    const float* src = p.part + (int64_t)tile * (T * T) + at;
+    f32x4 v0 = *reinterpret_cast<const f32x4*>(src), v1 = *reinterpret_cast<const f32x4*>(src + second);
 #pragma unroll 4
-    for (int k = 1; k < p.parts; ++k) v += src[(int64_t)k * tiles * (T * T / 4)];
-    store4(p, m, n, v);
+    for (int k = 1; k < p.parts; ++k) {
+        src += (int64_t)tiles * (T * T);
+        v0 += *reinterpret_cast<const f32x4*>(src);
+        v1 += *reinterpret_cast<const f32x4*>(src + second);
+    }
+    store4(p, m, n, v0);
+    if (n + 4 < p.N) store4(p, m, n + 4, v1);
 }
 
 // K == 0: the bias
@@ -565,7 +582,7 @@ hipError_t launch_fp8_matmul(MatmulParams p, const MatmulPlan& w, hipStream_t st
     const hipError_t e = p.e5m2 ? launch_form<true>(p, w, st) : launch_form<false>(p, w, st);
     if (e != hipSuccess || p.parts == 1) return e;
     const int T = w.form == MatmulPlan::LARGE ? 256 : 128, tm = (int)((p.M + T - 1) / T), tn = (int)((p.N + T - 1) / T);
-    const dim3 grid((unsigned)(tm * tn), (unsigned)(T * T / 1024));
+    const dim3 grid((unsigned)(tm * tn), (unsigned)(T * T / 2048));
     if (T == 256) hipLaunchKernelGGL(fp8_matmul_join_kernel<256>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
     else hipLaunchKernelGGL(fp8_matmul_join_kernel<128>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
     return hipGetLastError();
