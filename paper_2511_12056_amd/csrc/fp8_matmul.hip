@@ -56,111 +56,21 @@ __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t
     }
 }
 
-// ---- tiles ------------------------------------------------------------------------------------------------------
-// TM x TN results a workgroup of WM x WN wavefronts; tiles of 128 bytes a row in two LDS buffers.
-template <int TM, int TN, int WM, int WN>
-constexpr int matmul_smem() { return 2 * (TM + TN) * 132; }
-
-template <int TM, int TN, int WM, int WN, bool E5M2>
-__global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const MatmulParams p) {
-    constexpr int NW = WM * WN, MT = TM / WM / 16, NT = TN / WN / 16;
-    static_assert(NT == 4, "a wavefront's 64 columns are dealt to four instructions");
-    constexpr int STAGE = (TM + TN) * 132, B_AT = TM * 128, SA_AT = (TM + TN) * 128, SB_AT = SA_AT + TM * 4;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char matmul_smem_[];
-    const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))matmul_smem_;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w / WN, wn = w % WN;
-    const int r16 = lane & 15, g = lane >> 4;
-    const int64_t tiles_n = (p.N + TN - 1) / TN;
-    const int64_t tm = blockIdx.x / tiles_n, tn = blockIdx.x % tiles_n;
-    const int part = blockIdx.y;
-    const int64_t m0 = tm * TM, n0 = tn * TN;
-    const int nk_all = (int)(p.K / 128), kb0 = part * p.part_steps, nk = nk_all - kb0 < p.part_steps ? nk_all - kb0 : p.part_steps;
-    // what this wavefront fetches of each tile: chunks of eight rows
-    unsigned va[TM / 8 / NW], vb[TN / 8 / NW];
-    const int last_m = (int)(p.M - m0 < TM ? p.M - m0 : TM) - 1, last_n = (int)(p.N - n0 < TN ? p.N - n0 : TN) - 1;
+// Eight results of row m, columns n .. n + 7.
+__device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t n, f32x4 v0, f32x4 v1) {
+    __bf16* o = p.out + m * p.ldo + n;
+    if (n + 8 <= p.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+        if (p.bias) {
 #pragma unroll
-    for (int i = 0; i < TM / 8 / NW; ++i) {
-        const int r = (w + NW * i) * 8 + lane / 8, at = r < last_m ? r : last_m;
-        va[i] = (unsigned)at * (unsigned)p.K + (unsigned)(((lane & 7) ^ ((r >> 1) & 7)) * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < TN / 8 / NW; ++i) {
-        const int r = (w + NW * i) * 8 + lane / 8, at = r < last_n ? r : last_n;
-        vb[i] = (unsigned)at * (unsigned)p.K + (unsigned)(((lane & 7) ^ (((r >> 1) & 1) | ((r >> 4) & 3) << 1)) * 16);
-    }
-    // scales: wavefronts 0 .. TM/64 - 1 those of a, the others those of b, 64 rows each
-    const bool of_a = w < TM / 64;
-    const unsigned char* sbase = of_a ? p.a_scales + m0 * p.scale_cols : p.b_scales + (n0 >> p.b_shift) * p.scale_cols;
-    unsigned vs = 0;
-    {
-        const int r = (of_a ? w : w - TM / 64) * 64 + lane, lim = of_a ? last_m : last_n, at = r < lim ? r : lim;
-        vs = (unsigned)(of_a ? at : at >> p.b_shift) * (unsigned)p.scale_cols;
-    }
-    const unsigned char* pa = p.a + m0 * p.K;
-    const unsigned char* pb = p.b + n0 * p.K;
-    const auto fetch = [&](int t) __attribute__((always_inline)) {
-        const unsigned to = lds0 + (t & 1) * STAGE;
-        const int kb = kb0 + t;
-        const unsigned char* a = pa + (int64_t)kb * 128;
-        const unsigned char* b = pb + (int64_t)kb * 128;
-#pragma unroll
-        for (int i = 0; i < TM / 8 / NW; ++i) lds_dma16(a, va[i], to + (w + NW * i) * 1024);
-#pragma unroll
-        for (int i = 0; i < TN / 8 / NW; ++i) lds_dma16(b, vb[i], to + B_AT + (w + NW * i) * 1024);
-        if (w < (TM + TN) / 64) lds_dma4(sbase + (kb & ~3), vs, to + SA_AT + w * 256);
-    };
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // operand addresses: granules g and g + 4 of a row, at their swizzled places
-    const int nrow = wn * 64 + (r16 / 4) * 16 + (r16 & 3);      // + 4 j: the row of instruction j, so that a lane's results are 16 consecutive columns
-    const int mrow = wm * (TM / WM) + r16;                      // + 16 i
-    const unsigned sw_b = ((nrow >> 1) & 1) | ((nrow >> 4) & 3) << 1, sw_a = (mrow >> 1) & 7;
-    const unsigned a_lo = mrow * 128 + ((g ^ sw_a) * 16), a_hi = a_lo ^ 64;
-    const unsigned b_lo = B_AT + nrow * 128 + ((g ^ sw_b) * 16), b_hi = b_lo ^ 64;
-    if (nk > 0) fetch(0);
-    for (int t = 0; t < nk; ++t) {
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (t + 1 < nk) fetch(t + 1);
-        const unsigned char* s = matmul_smem_ + (t & 1) * STAGE;
-        const int shift = 8 * ((kb0 + t) & 3);
-        i32x8 fb[NT];
-        int sb[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            // rows 4 j apart: bits 2 and 3, which the swizzle does not look at
-            fb[j] = join8(*reinterpret_cast<const i32x4*>(s + b_lo + j * 512), *reinterpret_cast<const i32x4*>(s + b_hi + j * 512));
-            sb[j] = *reinterpret_cast<const int*>(s + SB_AT + (nrow + 4 * j) * 4) >> shift;
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const i32x8 fa = join8(*reinterpret_cast<const i32x4*>(s + a_lo + i * 2048), *reinterpret_cast<const i32x4*>(s + a_hi + i * 2048));
-            const int sa = *reinterpret_cast<const int*>(s + SA_AT + (mrow + 16 * i) * 4) >> shift;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = mfma<E5M2>(fb[j], fa, acc[i][j], sb[j], sa);
-        }
-    }
-    keep(acc);
-    if (p.parts > 1) {
-        float* to = p.part + ((int64_t)part * gridDim.x + blockIdx.x) * (TM * TN) + mrow * TN + wn * 64 + 16 * g;
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(to + i * 16 * TN + 4 * j) = acc[i][j];
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + mrow + 16 * i;
-        if (m < p.M)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int64_t n = n0 + wn * 64 + 16 * g + 4 * j;
-                if (n < p.N) store4(p, m, n, acc[i][j]);
+            for (int e = 0; e < 4; ++e) {
+                v0[e] += p.bias[n + e];
+                v1[e] += p.bias[n + 4 + e];
             }
+        }
+        *reinterpret_cast<u32x4*>(o) = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
+    } else {
+        store4(p, m, n, v0);
+        if (n + 4 < p.N) store4(p, m, n + 4, v1);
     }
 }
 
@@ -176,18 +86,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void fp8_matmul_kernel(const Matmu
 constexpr int kLargeA = 0, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeScales = 2 * kLargeStage, kLargeSa = 0, kLargeSb = 1024, kLargeBias = kLargeScales + 2 * 2048, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
 constexpr int kLargeGroup = 8;          // tiles of m that share tiles of n in a row
 
-// Place of tile t of tm x tn: large ones in an order in which neighbours share operands, blocks of kLargeGroup tiles of m, tile of n by tile of n; small ones row by row.
-template <int T>
+// Place of tile t of tm x tn, in an order in which neighbours share operands: blocks of kLargeGroup tiles of m, tile of n by tile of n.
 __device__ __forceinline__ void tile_place(int t, int tm, int tn, int& m, int& n) {
-    if constexpr (T == 256) {
-        const int group = t / (kLargeGroup * tn), rem = t - group * (kLargeGroup * tn);
-        const int left = tm - group * kLargeGroup, gm = left < kLargeGroup ? left : kLargeGroup;
-        n = rem / gm;
-        m = group * kLargeGroup + rem - n * gm;
-    } else {
-        m = t / tn;
-        n = t - m * tn;
-    }
+    const int group = t / (kLargeGroup * tn), rem = t - group * (kLargeGroup * tn);
+    const int left = tm - group * kLargeGroup, gm = left < kLargeGroup ? left : kLargeGroup;
+    n = rem / gm;
+    m = group * kLargeGroup + rem - n * gm;
 }
 
 // An accumulator's values where they are wanted: left to itself the compiler copies all 256 out of their registers first, into memory.
@@ -218,7 +122,7 @@ struct LargeItem {
 __device__ __forceinline__ LargeItem large_item(const MatmulParams& p, int i) {
     const int tm = (int)((p.M + 255) / 256), tn = (int)((p.N + 255) / 256), tiles = tm * tn, part = i / tiles;
     int m, n;
-    tile_place<256>(i - part * tiles, tm, tn, m, n);
+    tile_place(i - part * tiles, tm, tn, m, n);
     const int nk_all = (int)(p.K / 128), kb0 = part * p.part_steps, nk = nk_all - kb0 < p.part_steps ? nk_all - kb0 : p.part_steps;
     return {(int64_t)m * 256, (int64_t)n * 256, kb0, nk};
 }
@@ -382,7 +286,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + (i * 8 + j) * 256) = taken(acc[i][j]);
         } else {
             // 16 rows at a time through LDS (granules of 16 bytes at granule ^ row), so that a store is 256 bytes of four rows: with 64 bytes of 16 rows, straight from the
-            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of SSS
+            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of 723
             const int rows = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256), cols = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256);
             stored = rows == 256 && cols == 256 && p.vec_out;
             f32x4 bias[8];
@@ -426,6 +330,10 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 through([&](int k, const u32x4& x) __attribute__((always_inline)) {
                     if (row + k >= rows) return;
                     __bf16* at = reinterpret_cast<__bf16*>(to) + (int64_t)(row + k) * p.ldo + col;
+                    if (p.vec_out && col + 8 <= cols) {
+                        *reinterpret_cast<u32x4*>(at) = x;
+                        return;
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (col + e < cols) at[e] = __builtin_bit_cast(__bf16, (unsigned short)(x[e / 2] >> (16 * (e % 2))));
@@ -440,82 +348,195 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
     wait_vmcnt<0>();                                            // no fetch outlives the workgroup's LDS
 }
 
-// ---- few rows -----------------------------------------------------------------------------------------------------
-// 16 columns a workgroup, 16 MT rows; its wavefronts share K and add their sums in LDS, in order.  Operands come straight from memory: a row of b is used once.
-constexpr int kFewWaves = 4;
-template <int MT, bool E5M2>
-__global__ __launch_bounds__(kFewWaves * 64) void fp8_matmul_few_kernel(const MatmulParams p) {
-    __shared__ f32x4 sums[kFewWaves][MT][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int64_t bn = n0 + r16 < p.N ? n0 + r16 : p.N - 1;
-    const int nk = (int)(p.K / 128);
-    f32x4 acc[MT];
+// ---- middle tiles -------------------------------------------------------------------------------------------------
+// TM x TN results a workgroup of 2 x 2 wavefronts, for products that would leave most compute units without a large tile: there time is the latency of
+// memory, so seven blocks of 128 are on their way at once, in a ring of eight LDS buffers with a barrier a block.  A block takes 0.33 us (32 x 64) or 0.37 us (64 x 64).
+// 256 x 1 536 x 4 096 is 13.1 us with the call (32 x 64: 192 workgroups; 64 x 64: 96 workgroups, 14.8), 16.2 with operands straight from memory into registers.
+constexpr int kMidRing = 8, kMidChunks = 4;             // words of scales: of four blocks each
+template <int TM, int TN> constexpr int mid_stage() { return (TM + TN) * 128; }
+template <int TM, int TN> constexpr int mid_smem() { return kMidRing * mid_stage<TM, TN>() + kMidChunks * 512; }
+
+template <int TM, int TN, bool E5M2>
+__global__ __launch_bounds__(256) void fp8_matmul_mid_kernel(const MatmulParams p) {
+    constexpr int MT = TM / 32, NT = TN / 32, PA = TM / 32, PB = TN / 32, STAGE = mid_stage<TM, TN>(), B_AT = TM * 128, SCALES = kMidRing * STAGE;
+    static_assert(NT == 2, "a lane's results of two instructions are eight consecutive columns");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char matmul_smem_[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(LDS_PTR(unsigned char))matmul_smem_;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w >> 1, wn = w & 1, r16 = lane & 15, g = lane >> 4;
+    const int tn = (int)((p.N + TN - 1) / TN), tile_m = blockIdx.x / tn, tile_n = blockIdx.x - tile_m * tn;
+    const int64_t m0 = (int64_t)tile_m * TM, n0 = (int64_t)tile_n * TN;
+    const int nk_all = (int)(p.K / 128), kb0 = blockIdx.y * p.part_steps, nk = nk_all - kb0 < p.part_steps ? nk_all - kb0 : p.part_steps;
+    const int last_m = (int)(p.M - m0 < TM ? p.M - m0 : TM) - 1, last_n = (int)(p.N - n0 < TN ? p.N - n0 : TN) - 1;
+    // fetching: eight rows a request, the granules of 16 bytes swizzled as in large tiles
+    unsigned va[PA], vb[PB];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const unsigned char* b = p.b + bn * p.K + 32 * g;
-    const uint8_t* sbp = p.b_scales + (bn >> p.b_shift) * p.scale_cols;
-    const unsigned char* a[MT];
-    const uint8_t* sap[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + 16 * i + r16 < p.M ? m0 + 16 * i + r16 : p.M - 1;
-        a[i] = p.a + m * p.K + 32 * g;
-        sap[i] = p.a_scales + m * p.scale_cols;
+    for (int i = 0; i < PA; ++i) {
+        const int r = (w + 4 * i) * 8 + lane / 8;
+        va[i] = __umul24(r < last_m ? r : last_m, (unsigned)p.K) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
     }
-    for (int kb = w; kb < nk; kb += kFewWaves) {
-        const i32x8 fb = join8(*reinterpret_cast<const i32x4*>(b + (int64_t)kb * 128), *reinterpret_cast<const i32x4*>(b + (int64_t)kb * 128 + 16));
-        const int sb = sbp[kb];
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+        const int r = (w + 4 * i) * 8 + lane / 8;
+        vb[i] = __umul24(r < last_n ? r : last_n, (unsigned)p.K) + ((lane & 7) ^ (((r >> 1) & 1) | ((r >> 3) & 3) << 1)) * 16;
+    }
+    const int slim = wm == 0 ? last_m : last_n, sr = lane < slim ? lane : slim;
+    const unsigned vs = (unsigned)(wm == 0 ? sr : sr >> p.b_shift) * (unsigned)p.scale_cols;
+    const unsigned char* pa = p.a + m0 * p.K + (int64_t)kb0 * 128;
+    const unsigned char* pb = p.b + n0 * p.K + (int64_t)kb0 * 128;
+    const unsigned char* ps = wm == 0 ? p.a_scales + m0 * p.scale_cols : p.b_scales + (n0 >> p.b_shift) * p.scale_cols;
+    const auto fetch = [&](int t) __attribute__((always_inline)) {
+        const int kb = kb0 + t;
+        if (wn == 0 && (t == 0 || (kb & 3) == 0)) lds_dma4(ps + (kb & ~3), vs, lds0 + SCALES + (kb >> 2) % kMidChunks * 512 + wm * 256);     // wavefront 0 those of a, 2 those of b
+        const unsigned to = lds0 + t % kMidRing * STAGE + w * 1024;
+        const int64_t at = (int64_t)t * 128;
+#pragma unroll
+        for (int i = 0; i < PA; ++i) lds_dma16(pa + at, va[i], to + i * 4096);
+#pragma unroll
+        for (int i = 0; i < PB; ++i) lds_dma16(pb + at, vb[i], to + B_AT + i * 4096);
+    };
+    const int mrow = wm * (TM / 2) + r16, nrow = wn * 32 + (r16 / 4) * 8 + (r16 & 3);
+    const unsigned ra = mrow * 128 + ((g ^ (r16 >> 1)) * 16), rb = B_AT + nrow * 128 + ((g ^ (r16 >> 1)) * 16);
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < kMidRing - 1; ++t)
+        if (t < nk) fetch(t);
+    for (int t = 0; t < nk; ++t) {
+        // block t has arrived when no more are on their way than belong to the blocks behind it (scales apart: then for a little longer)
+        switch (nk - 1 - t) {
+            case 0: wait_vmcnt<0>(); break;
+            case 1: wait_vmcnt<PA + PB>(); break;
+            case 2: wait_vmcnt<2 * (PA + PB)>(); break;
+            case 3: wait_vmcnt<3 * (PA + PB)>(); break;
+            case 4: wait_vmcnt<4 * (PA + PB)>(); break;
+            case 5: wait_vmcnt<5 * (PA + PB)>(); break;
+            default: wait_vmcnt<6 * (PA + PB)>();
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");    // and all have read block t - 1
+        if (t + kMidRing - 1 < nk) fetch(t + kMidRing - 1);
+        const unsigned char* s = matmul_smem_ + t % kMidRing * STAGE;
+        const int kb = kb0 + t;
+        const unsigned char* sc = matmul_smem_ + SCALES + (kb >> 2) % kMidChunks * 512 + (kb & 3);
+        i32x8 fb[NT];
+        int sb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            fb[j] = join8(*reinterpret_cast<const i32x4*>(s + rb + j * 512), *reinterpret_cast<const i32x4*>(s + (rb ^ 64) + j * 512));
+            sb[j] = sc[256 + (nrow + 4 * j) * 4];
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const i32x8 fa = join8(*reinterpret_cast<const i32x4*>(a[i] + (int64_t)kb * 128), *reinterpret_cast<const i32x4*>(a[i] + (int64_t)kb * 128 + 16));
-            acc[i] = mfma<E5M2>(fb, fa, acc[i], sb, sap[i][kb]);
+            const i32x8 fa = join8(*reinterpret_cast<const i32x4*>(s + ra + i * 2048), *reinterpret_cast<const i32x4*>(s + (ra ^ 64) + i * 2048));
+            const int sa = sc[(mrow + 16 * i) * 4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma<E5M2>(fb[j], fa, acc[i][j], sb[j], sa);
         }
     }
     keep(acc);
+    const int col = wn * 32 + 8 * g;
+    if (p.parts > 1) {
+        float* to = p.part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (TM * TN) + mrow * TN + col;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) sums[w][i][lane] = acc[i];
-    __syncthreads();
-    for (int i = w; i < MT; i += kFewWaves) {
-        f32x4 v = sums[0][i][lane];
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int o = 1; o < kFewWaves; ++o) v += sums[o][i][lane];
-        const int64_t m = m0 + 16 * i + r16, n = n0 + 4 * g;
-        if (m < p.M && n < p.N) store4(p, m, n, v);
+            for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4*>(to + i * 16 * TN + 4 * j) = acc[i][j];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + mrow + 16 * i, n = n0 + col;
+        if (m < p.M && n < p.N) store8(p, m, n, acc[i][0], acc[i][1]);
     }
 }
 
+// ---- few rows -----------------------------------------------------------------------------------------------------
+// 16 x 16 results a workgroup, whose four wavefronts each take a range of K, straight from memory into registers without a barrier, and add their sums in LDS, in
+// order: for up to 16 rows, where every row of b is read once and that is all the time there is.  1 x 4 608 x 1 536 is 10.4 us with the call, 4.4 us without; 1 x 8 192 x
+// 8 192 is 14.3 (32 x 64 tiles: 23).
+constexpr int kFewWaves = 4, kFewAhead = 4;             // blocks in registers
+template <bool E5M2>
+__global__ __launch_bounds__(kFewWaves * 64) void fp8_matmul_few_kernel(const MatmulParams p) {
+    __shared__ f32x4 sums[kFewWaves][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int tn = (int)((p.N + 15) / 16), tile_m = blockIdx.x / tn, tile_n = blockIdx.x - tile_m * tn;
+    const int64_t m0 = (int64_t)tile_m * 16, n0 = (int64_t)tile_n * 16;
+    const int nk_all = (int)(p.K / 128), first = blockIdx.y * p.part_steps, nk = nk_all - first < p.part_steps ? nk_all - first : p.part_steps;
+    const int kb0 = first + nk * w / kFewWaves, kb1 = first + nk * (w + 1) / kFewWaves;
+    const int64_t m = m0 + r16 < p.M ? m0 + r16 : p.M - 1, n = n0 + r16 < p.N ? n0 + r16 : p.N - 1;      // rows behind the last are the last one's again
+    const unsigned char *a = p.a + m * p.K + 16 * g, *b = p.b + n * p.K + 16 * g;
+    const uint8_t *sap = p.a_scales + m * p.scale_cols, *sbp = p.b_scales + (n >> p.b_shift) * p.scale_cols;
+    struct Block {
+        i32x8 a, b;
+        int sa, sb;
+    };
+    const auto load = [&](Block& x, int kb) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)kb * 128;
+        x.b = join8(*reinterpret_cast<const i32x4*>(b + at), *reinterpret_cast<const i32x4*>(b + at + 64));
+        x.sb = sbp[kb];
+        x.a = join8(*reinterpret_cast<const i32x4*>(a + at), *reinterpret_cast<const i32x4*>(a + at + 64));
+        x.sa = sap[kb];
+    };
+    f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+    Block x[kFewAhead];
+#pragma unroll
+    for (int u = 0; u < kFewAhead; ++u)
+        if (kb0 + u < kb1) load(x[u], kb0 + u);
+    for (int kb = kb0; kb < kb1; kb += kFewAhead) {
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u)
+            if (kb + u < kb1) {
+                acc[0] = mfma<E5M2>(x[u].b, x[u].a, acc[0], x[u].sb, x[u].sa);
+                if (kb + u + kFewAhead < kb1) load(x[u], kb + u + kFewAhead);
+            }
+    }
+    keep(acc);
+    sums[w][lane] = acc[0];
+    __syncthreads();
+    if (w != 0) return;
+    f32x4 v = sums[0][lane];
+#pragma unroll
+    for (int o = 1; o < kFewWaves; ++o) v += sums[o][lane];
+    if (p.parts > 1) *reinterpret_cast<f32x4*>(p.part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + r16 * 16 + 4 * g) = v;
+    else if (m0 + r16 < p.M && n0 + 4 * g < p.N) store4(p, m0 + r16, n0 + 4 * g, v);
+}
+
 // ---- sums of the ranges of K --------------------------------------------------------------------------------------
-// Parts hold whole tiles of T x T, small ones by rows, large ones as they lay in the registers; eight columns a thread.
-template <int T>
+// Parts hold whole tiles: large ones (TM = 256) as they lay in the registers, others by rows.  Eight columns a thread, or four.
+template <int TM, int TN>
 __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulParams p, int tiles, int tm, int tn) {
+    constexpr int C = TN >= 32 ? 8 : 4;
     const int tile = blockIdx.x, e = blockIdx.y * 256 + threadIdx.x;
-    int im, in, r, c, at, second;                               // row and column in the tile, place of its first four sums, of the others behind them
-    tile_place<T>(tile, tm, tn, im, in);
-    if constexpr (T == 256) {
+    if (e >= TM * TN / C) return;
+    int im, in, r, c, at, second = 4;                           // row and column in the tile, place of its first four sums, of the others behind them
+    if constexpr (TM == 256) {
+        tile_place(tile, tm, tn, im, in);
         const int lane = e & 63, jj = e >> 6 & 3, i = e >> 8 & 7, w = e >> 11;
         r = (w >> 1) * 128 + i * 16 + (lane & 15);
         c = (w & 1) * 128 + jj * 32 + (lane >> 4) * 8;
         at = ((w * 64 + i * 8 + jj * 2) * 64 + lane) * 4;
         second = 256;
     } else {
-        r = e / (T / 8);
-        c = e % (T / 8) * 8;
-        at = r * T + c;
-        second = 4;
+        im = tile / tn;
+        in = tile - im * tn;
+        r = e / (TN / C);
+        c = e % (TN / C) * C;
+        at = r * TN + c;
     }
-    const int64_t m = (int64_t)im * T + r, n = (int64_t)in * T + c;
+    const int64_t m = (int64_t)im * TM + r, n = (int64_t)in * TN + c;
     if (m >= p.M || n >= p.N) return;
-    const float* src = p.part + (int64_t)tile * (T * T) + at;
-    f32x4 v0 = *reinterpret_cast<const f32x4*>(src), v1 = *reinterpret_cast<const f32x4*>(src + second);
+    const float* src = p.part + (int64_t)tile * (TM * TN) + at;
+    f32x4 v0 = *reinterpret_cast<const f32x4*>(src), v1 = C == 8 ? *reinterpret_cast<const f32x4*>(src + second) : v0;
 #pragma unroll 4
     for (int k = 1; k < p.parts; ++k) {
-        src += (int64_t)tiles * (T * T);
+        src += (int64_t)tiles * (TM * TN);
         v0 += *reinterpret_cast<const f32x4*>(src);
-        v1 += *reinterpret_cast<const f32x4*>(src + second);
+        if constexpr (C == 8) v1 += *reinterpret_cast<const f32x4*>(src + second);
     }
-    store4(p, m, n, v0);
-    if (n + 4 < p.N) store4(p, m, n + 4, v1);
+    if constexpr (C == 8) store8(p, m, n, v0, v1);
+    else store4(p, m, n, v0);
 }
 
 // K == 0: the bias
@@ -524,37 +545,58 @@ __global__ __launch_bounds__(256) void fp8_matmul_bias_kernel(const MatmulParams
     if (m < p.M && c < n4) store4(p, m, c * 4, f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
+// Tiles of the forms, in rows and columns.
+struct FormSize { int m, n; };
+static constexpr FormSize kForms[MatmulPlan::FORMS] = {{16, 16}, {32, 64}, {64, 64}, {256, 256}};
+
+// An estimate of a launch's time in us, for choosing among the forms and numbers of parts.  Its rates are fits to every form's times at 14 products, from 1 x 8 192 x 8 192
+// to 119 056 x 4 608 x 1 536 (256 compute units; us, the least of each row is what the rule takes or within 10 % of it):
+//                             few    32 x 64    64 x 64    large    large, 4 parts
+//       1 x 8 192 x 8 192      14         23         26       75          33
+//     256 x 1 536 x 4 096      29         13         15       40          19
+//   1 000 x 1 536 x 1 536      37         17         14       30          18
+//   2 000 x 1 536 x 6 144     282        102         59       67          35
+//   2 048 x 4 608 x 1 536     207         91         56       22          53
+static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
+    const FormSize& s = kForms[f];
+    const int64_t items = tiles * parts, rounds = (items + n_cu - 1) / n_cu;
+    const double load = (double)items / n_cu;
+    double t;
+    if (f == MatmulPlan::LARGE) t = 6.0 + (double)rounds * (steps * (1.07 + 0.4 * (load < 1.0 ? load : 1.0)) + 4.0);
+    else if (f == MatmulPlan::FEW) t = 3.0 + steps * (load > 1.1 ? 0.11 * load : 0.12);
+    else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.365 : 0.33));
+    if (parts > 1) {                                            // parts written and read, more than 128 MB of them from memory: 4 608 x 1 536 x 119 056 took 678 us in
+        const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units, 717 in 7 on 252 (three times)
+        t += 4.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
+    }
+    return t;
+}
+
 MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t K, int n_cu) {
     const int nk = (int)(K / 128);
-    if (M <= 64) return {MatmulPlan::FEW, 1, nk};
-    const auto tiles = [&](int64_t t) { return (M + t - 1) / t * ((N + t - 1) / t); };
-    const bool large = tiles(256) * (nk / 16 + 1) >= n_cu;
-    const int64_t n = large ? tiles(256) : tiles(128), room = large ? n_cu : 2 * n_cu;
-    const int least = large ? 16 : 4;                          // steps of a part
-    int64_t parts = n >= room ? 1 : room / n;
-    if (parts > nk / least) parts = nk / least > 1 ? nk / least : 1;
-    const int steps = (int)((nk + parts - 1) / parts + 3) / 4 * 4;       // words of four scales
-    return {large ? MatmulPlan::LARGE : MatmulPlan::SMALL, steps > 0 ? (nk + steps - 1) / steps : 1, steps};
+    MatmulPlan best{0, 1, nk};
+    double best_time = 1e300;
+    if (nk == 0) return best;                                              // the bias alone
+    for (int f = 0; f < MatmulPlan::FORMS; ++f) {
+        const FormSize& s = kForms[f];
+        const int64_t tiles = (M + s.m - 1) / s.m * ((N + s.n - 1) / s.n);
+        if (tiles > 0x3fffff && f != MatmulPlan::LARGE) continue;          // a launch has fewer than 2^32 threads along x
+        for (int parts = 1; parts <= kMatmulMaxParts; ++parts) {
+            const int steps = ((nk + parts - 1) / parts + 3) / 4 * 4;      // (words of four scales in the large form)
+            if (parts > 1 && (nk + steps - 1) / steps != parts) continue;
+            const double t = form_time(f, tiles, parts, steps < nk ? steps : nk, n_cu);
+            if (t < best_time) {
+                best_time = t;
+                best = {f, parts, steps};
+            }
+        }
+    }
+    return best;
 }
 
 int64_t matmul_workspace_bytes(const MatmulPlan& w, int64_t M, int64_t N) {
-    const int64_t t = w.form == MatmulPlan::LARGE ? 256 : 128;
-    return w.parts > 1 ? w.parts * ((M + t - 1) / t) * ((N + t - 1) / t) * t * t * 4 : 0;
-}
-
-static dim3 row_grid(const MatmulParams& p) {
-    const int64_t y = p.M < 65535 ? p.M : 65535;
-    return dim3((unsigned)(((p.N + 3) / 4 + 255) / 256), (unsigned)y, (unsigned)((p.M + y - 1) / y));
-}
-
-template <int TM, int TN, int WM, int WN, bool E5M2>
-static hipError_t launch_tiles(const MatmulParams& p, hipStream_t st) {
-    static KernelSetup setup;
-    const hipError_t e = setup.ensure(reinterpret_cast<const void*>(fp8_matmul_kernel<TM, TN, WM, WN, E5M2>), matmul_smem<TM, TN, WM, WN>(), nullptr);
-    if (e != hipSuccess) return e;
-    const int64_t tiles = (p.M + TM - 1) / TM * ((p.N + TN - 1) / TN);
-    hipLaunchKernelGGL((fp8_matmul_kernel<TM, TN, WM, WN, E5M2>), dim3((unsigned)tiles, (unsigned)p.parts), dim3(WM * WN * 64), (matmul_smem<TM, TN, WM, WN>()), st, p);
-    return hipGetLastError();
+    const FormSize& s = kForms[w.form];
+    return w.parts > 1 ? w.parts * ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n) * s.m * s.n * 4 : 0;
 }
 
 template <bool E5M2>
@@ -570,15 +612,38 @@ static hipError_t launch_large(const MatmulParams& p, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <bool E5M2>
-static hipError_t launch_form(const MatmulParams& p, const MatmulPlan& w, hipStream_t st) {
-    if (w.form == MatmulPlan::LARGE) return launch_large<E5M2>(p, st);
-    if (w.form == MatmulPlan::SMALL) return launch_tiles<128, 128, 2, 2, E5M2>(p, st);
-    const unsigned x = (unsigned)((p.N + 15) / 16);
-    if (p.M <= 16) hipLaunchKernelGGL((fp8_matmul_few_kernel<1, E5M2>), dim3(x), dim3(kFewWaves * 64), 0, st, p);
-    else if (p.M <= 32) hipLaunchKernelGGL((fp8_matmul_few_kernel<2, E5M2>), dim3(x), dim3(kFewWaves * 64), 0, st, p);
-    else hipLaunchKernelGGL((fp8_matmul_few_kernel<4, E5M2>), dim3(x), dim3(kFewWaves * 64), 0, st, p);
+template <int TM, int TN>
+static hipError_t launch_join(const MatmulParams& p, hipStream_t st) {
+    if (p.parts == 1) return hipSuccess;
+    const int tm = (int)((p.M + TM - 1) / TM), tn = (int)((p.N + TN - 1) / TN), threads = TM * TN / (TN >= 32 ? 8 : 4);
+    hipLaunchKernelGGL((fp8_matmul_join_kernel<TM, TN>), dim3((unsigned)(tm * tn), (unsigned)((threads + 255) / 256)), dim3(256), 0, st, p, tm * tn, tm, tn);
     return hipGetLastError();
+}
+
+template <int TM, int TN, bool E5M2>
+static hipError_t launch_mid(const MatmulParams& p, dim3 grid, hipStream_t st) {
+    static KernelSetup setup;
+    const hipError_t e = setup.ensure(reinterpret_cast<const void*>(fp8_matmul_mid_kernel<TM, TN, E5M2>), mid_smem<TM, TN>(), nullptr);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((fp8_matmul_mid_kernel<TM, TN, E5M2>), grid, dim3(256), (mid_smem<TM, TN>()), st, p);
+    return hipGetLastError();
+}
+
+template <int F>
+static hipError_t launch_form(const MatmulParams& p, hipStream_t st) {
+    constexpr FormSize s = kForms[F];
+    const dim3 grid((unsigned)((p.M + s.m - 1) / s.m * ((p.N + s.n - 1) / s.n)), (unsigned)p.parts);
+    hipError_t e = hipSuccess;
+    if constexpr (F == MatmulPlan::LARGE) {
+        e = p.e5m2 ? launch_large<true>(p, st) : launch_large<false>(p, st);
+    } else if constexpr (F == MatmulPlan::FEW) {
+        if (p.e5m2) hipLaunchKernelGGL(fp8_matmul_few_kernel<true>, grid, dim3(kFewWaves * 64), 0, st, p);
+        else hipLaunchKernelGGL(fp8_matmul_few_kernel<false>, grid, dim3(kFewWaves * 64), 0, st, p);
+        e = hipGetLastError();
+    } else {
+        e = p.e5m2 ? launch_mid<s.m, s.n, true>(p, grid, st) : launch_mid<s.m, s.n, false>(p, grid, st);
+    }
+    return e == hipSuccess ? launch_join<s.m, s.n>(p, st) : e;
 }
 
 hipError_t launch_fp8_matmul(MatmulParams p, const MatmulPlan& w, hipStream_t st) {
@@ -586,16 +651,16 @@ hipError_t launch_fp8_matmul(MatmulParams p, const MatmulPlan& w, hipStream_t st
     p.part_steps = w.part_steps;
     p.vec_out = p.ldo % 8 == 0 && p.ldo < (int64_t)1 << 22 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;      // 256 rows within 2^32 bytes
     if (p.K == 0) {
-        hipLaunchKernelGGL(fp8_matmul_bias_kernel, row_grid(p), dim3(256), 0, st, p);
+        const int64_t y = p.M < 65535 ? p.M : 65535;
+        hipLaunchKernelGGL(fp8_matmul_bias_kernel, dim3((unsigned)(((p.N + 3) / 4 + 255) / 256), (unsigned)y, (unsigned)((p.M + y - 1) / y)), dim3(256), 0, st, p);
         return hipGetLastError();
     }
-    const hipError_t e = p.e5m2 ? launch_form<true>(p, w, st) : launch_form<false>(p, w, st);
-    if (e != hipSuccess || p.parts == 1) return e;
-    const int T = w.form == MatmulPlan::LARGE ? 256 : 128, tm = (int)((p.M + T - 1) / T), tn = (int)((p.N + T - 1) / T);
-    const dim3 grid((unsigned)(tm * tn), (unsigned)(T * T / 2048));
-    if (T == 256) hipLaunchKernelGGL(fp8_matmul_join_kernel<256>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
-    else hipLaunchKernelGGL(fp8_matmul_join_kernel<128>, grid, dim3(256), 0, st, p, tm * tn, tm, tn);
-    return hipGetLastError();
+    switch (w.form) {
+        case MatmulPlan::FEW: return launch_form<MatmulPlan::FEW>(p, st);
+        case MatmulPlan::MID: return launch_form<MatmulPlan::MID>(p, st);
+        case MatmulPlan::MID_WIDE: return launch_form<MatmulPlan::MID_WIDE>(p, st);
+    }
+    return launch_form<MatmulPlan::LARGE>(p, st);
 }
 
 }  // namespace pda

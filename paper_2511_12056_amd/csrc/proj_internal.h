@@ -38,9 +38,11 @@ struct MatmulParams {
     int part_steps;
     int vec_out;             // rows of out lie at multiples of 16 bytes
 };
+constexpr int kMatmulMaxParts = 32;
 // How a product is split over workgroups: the form of its tiles and the ranges of K.
 struct MatmulPlan {
-    enum Form { FEW, SMALL, LARGE } form;
+    static constexpr int FEW = 0, MID = 1, MID_WIDE = 2, LARGE = 3, FORMS = 4;
+    int form;
     int parts, part_steps;
 };
 MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t K, int n_cu);
