@@ -104,6 +104,20 @@ def test_quant_of_extreme_values(kind, block):
     _check_quant(x, kind, block, "both")
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("xt", ["bfloat16", "float32"])
+def test_quant_of_every_exponent(kind, block, xt):
+    """Every bf16 value: a row of 128 for each sign and exponent, so that rows have scales of their own and columns one for 128 exponents; then each row beside
+    values of 2^-24 .. 2^8 times as much, which end in every place of the 8-bit type, below its normal numbers too."""
+    import torch
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.uint16).view(torch.bfloat16).view(512, 128)
+    x = torch.cat([bits, bits.float().mul(2.0 ** -9).bfloat16(), bits.roll(7, 0), bits.roll(3, 0)], 1)
+    x[:, 128:256:5] = (bits.float() * 2.0 ** -24).bfloat16()[:, ::5]
+    x[:, 384:] = torch.where(x[:, 384:].isfinite(), x[:, 384:], torch.ones_like(x[:, 384:]))
+    _check_quant(x.to(getattr(torch, xt)), kind, block, "both")
+
+
 def test_square_blocks_agree_in_both_orders():
     import torch
     x = torch.randn(515, 900, device="cuda")
