@@ -6,6 +6,7 @@ streams); the binding passes raw device pointers and sizes across the C ABI.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -648,11 +649,12 @@ def _expect_fp8(q, scales, rows: int, cols: int, block_rows: int, name: str):
     """q [rows, cols padded to 128] and its scales [blocks of rows, blocks of columns padded to 4]."""
     import torch
     _fp8_code(q, name)
-    shape = (rows, _up(cols, 128))
-    if tuple(q.shape) != shape or not q.is_contiguous() or not q.is_cuda:
+    width = -(-cols // 128)
+    shape = (rows, 128 * width)
+    if q.shape != shape or not q.is_contiguous() or not q.is_cuda:
         raise ValueError(f"{name}: expected contiguous cuda {shape}, got {tuple(q.shape)} contiguous={q.is_contiguous()} cuda={q.is_cuda}")
-    shape = (_up(rows, block_rows) // block_rows, _up(_up(cols, 128) // 128, 4))
-    if scales is None or scales.dtype is not torch.float8_e8m0fnu or tuple(scales.shape) != shape or not scales.is_contiguous() or not scales.is_cuda:
+    shape = (rows if block_rows == 1 else -(-rows // block_rows), width + 3 & ~3)
+    if scales is None or scales.dtype is not torch.float8_e8m0fnu or scales.shape != shape or not scales.is_contiguous() or not scales.is_cuda:
         raise ValueError(f"{name}_scales: expected contiguous cuda float8_e8m0fnu {shape}, got " +
                          ("None" if scales is None else f"{scales.dtype} {tuple(scales.shape)} contiguous={scales.is_contiguous()} cuda={scales.is_cuda}"))
 
@@ -703,6 +705,12 @@ def fp8_matmul_workspace(M: int, N: int, K: int):
     return torch.empty(fp8_matmul_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
 
 
+@functools.lru_cache(maxsize=4096)
+def _fp8_matmul_bytes(M: int, N: int, K: int, device: int) -> int:
+    """fp8_matmul_workspace_bytes on the current device, `device`: a call on few rows is bound by host time."""
+    return fp8_matmul_workspace_bytes(M, N, K)
+
+
 def fp8_matmul(a, a_scales, b, b_scales, out, bias=None, workspace=None, stream=None):
     """pda_fp8_matmul: a [M, K] (blocks of one row), b [N, K] (blocks of one row or of 128, as its scales say) -> out [M, N] bf16 = a b^T + bias [N] fp32.
 
@@ -718,13 +726,14 @@ def fp8_matmul(a, a_scales, b, b_scales, out, bias=None, workspace=None, stream=
     _expect_fp8(b, b_scales, N, K, block, "b")
     if b.dtype is not torch.float8_e4m3fn:
         raise ValueError(f"b: expected float8_e4m3fn, got {b.dtype}")
-    if out.dtype is not torch.bfloat16 or tuple(out.shape) != (M, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N):
+    if out.dtype is not torch.bfloat16 or out.shape != (M, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N):
         raise ValueError(f"out: expected cuda bf16 {(M, N)} with compact rows, got {out.dtype} {tuple(out.shape)} stride {out.stride()}")
     if bias is not None:
         _expect(bias, torch.float32, (N,), "bias")
     _on_current_device(stream, a, a_scales, b, b_scales, out, bias, workspace)
     if workspace is None:
-        workspace = _workspace(fp8_matmul_workspace_bytes(M, N, K), None, stream)
+        nbytes = _fp8_matmul_bytes(M, N, K, a.get_device())
+        workspace = _workspace(nbytes, None, stream) if nbytes else None
     else:
         _workspace(0, workspace, stream)
     _check(lib.pda_fp8_matmul(_ptr(a), _fp8_code(a, "a"), _ptr(a_scales), _ptr(b), _ptr(b_scales), block, _ptr(bias), _ptr(out), M, N, K,
