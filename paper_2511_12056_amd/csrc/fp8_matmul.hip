@@ -286,7 +286,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + (i * 8 + j) * 256) = taken(acc[i][j]);
         } else {
             // 16 rows at a time through LDS (granules of 16 bytes at granule ^ row), so that a store is 256 bytes of four rows: with 64 bytes of 16 rows, straight from the
-            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of 723
+            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of 723 (both without the stores' hint)
             const int rows = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256), cols = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256);
             stored = rows == 256 && cols == 256 && p.vec_out;
             f32x4 bias[8];
@@ -323,8 +323,8 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 const unsigned pitch = (unsigned)p.ldo * 8;     // bytes of four rows
                 unsigned at = ((unsigned)row * (unsigned)p.ldo + col) * 2;
                 through([&](int, const u32x4& x) __attribute__((always_inline)) {
-                    *reinterpret_cast<u32x4*>(to + at) = x;
-                    at += pitch;
+                    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to + at));      // operands stay in L2: 698 us instead of 705, and what reads out next
+                    at += pitch;                                                            // takes as long (9 600 x 4 608 x 1 536) or less (119 056 x 4 608 x 1 536)
                 });
             } else {
                 through([&](int k, const u32x4& x) __attribute__((always_inline)) {
