@@ -40,6 +40,9 @@ __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsig
                  : "memory", "m0", "vcc");
 }
 
+typedef u32x2 u32x2_loose __attribute__((aligned(2)));      // rows of any length start at any element
+typedef u32x4 u32x4_loose __attribute__((aligned(2)));
+
 // Four results of row m, columns n .. n + 3: the bias added, rounded.
 __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t n, f32x4 v) {
     __bf16* o = p.out + m * p.ldo + n;
@@ -47,8 +50,8 @@ __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += n + e < p.N ? p.bias[n + e] : 0.f;
     }
-    if (n + 4 <= p.N && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
-        *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (n + 4 <= p.N) {
+        *reinterpret_cast<u32x2_loose*>(o) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -59,7 +62,7 @@ __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t
 // Eight results of row m, columns n .. n + 7.
 __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t n, f32x4 v0, f32x4 v1) {
     __bf16* o = p.out + m * p.ldo + n;
-    if (n + 8 <= p.N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+    if (n + 8 <= p.N) {
         if (p.bias) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -67,7 +70,7 @@ __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t
                 v1[e] += p.bias[n + 4 + e];
             }
         }
-        *reinterpret_cast<u32x4*>(o) = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
+        *reinterpret_cast<u32x4_loose*>(o) = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
     } else {
         store4(p, m, n, v0);
         if (n + 4 < p.N) store4(p, m, n + 4, v1);
@@ -330,8 +333,8 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 through([&](int k, const u32x4& x) __attribute__((always_inline)) {
                     if (row + k >= rows) return;
                     __bf16* at = reinterpret_cast<__bf16*>(to) + (int64_t)(row + k) * p.ldo + col;
-                    if (p.vec_out && col + 8 <= cols) {
-                        *reinterpret_cast<u32x4*>(at) = x;
+                    if (col + 8 <= cols) {
+                        *reinterpret_cast<u32x4_loose*>(at) = x;
                         return;
                     }
 #pragma unroll

@@ -24,6 +24,7 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Held;
 template <> struct Held<__bf16> {
     static constexpr int W = 4;
+    typedef u32x4 Piece __attribute__((aligned(2)));
     static __device__ __forceinline__ unsigned magnitude(unsigned x) { return x & 0x7fff7fffu; }
     static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) {
         return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
@@ -33,24 +34,25 @@ template <> struct Held<__bf16> {
 };
 template <> struct Held<float> {
     static constexpr int W = 8;
+    typedef u32x4 Piece __attribute__((aligned(4)));
     static __device__ __forceinline__ unsigned magnitude(unsigned x) { return x & 0x7fffffffu; }
     static __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
     static __device__ __forceinline__ unsigned finite(unsigned m) { return m < 0x7f800000u ? m : 0u; }
     static __device__ __forceinline__ unsigned one(unsigned m) { return m; }
 };
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int n, unsigned (&x)[Held<T>::W]) {        // n <= 0: none
-    if constexpr (VEC) {                                        // (a row's end lies behind whole pieces)
+// n < 8 at a row's end; n <= 0: none.  Rows of any length start at any element.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int n, unsigned (&x)[Held<T>::W]) {
+    if (n == 8) {
 #pragma unroll
-        for (int i = 0; i < Held<T>::W / 4; ++i)
-            if (n > 4 * i) {
-                const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
-                x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-            }
+        for (int i = 0; i < Held<T>::W / 4; ++i) {
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const typename Held<T>::Piece*>(p) + i);
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 7; ++e)
             if (e < n) {
                 if constexpr (sizeof(T) == 4) x[e] = __float_as_uint(p[e]);
                 else x[e / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[e]) << (16 * (e % 2));
@@ -88,7 +90,7 @@ __device__ __forceinline__ unsigned to_fp8(unsigned a, unsigned b, unsigned c, u
 template <int CTRL>
 __device__ __forceinline__ unsigned word_perm(unsigned x) { return __builtin_amdgcn_update_dpp(0u, x, CTRL, 0xF, 0xF, false); }
 
-template <typename T, bool VEC, bool E5M2>
+template <typename T, bool E5M2>
 __global__ __launch_bounds__(256) void fp8_quant_kernel(const QuantParams p, int64_t tiles_r, int64_t tiles_c) {
     using H = Held<T>;
     constexpr int W = H::W;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(256) void fp8_quant_kernel(const QuantParams p, int
     for (int j = 0; j < 8; ++j) {
 #pragma unroll
         for (int k = 0; k < W; ++k) x[j][k] = 0u;
-        load8<T, VEC>(px + j * p.ldx, j < rows ? n : 0, x[j]);
+        load8<T>(px + j * p.ldx, j < rows ? n : 0, x[j]);
     }
     unsigned rt[8], ct[W];                                      // largest magnitudes of the thread's rows (two columns of bf16 a word) and columns
 #pragma unroll
@@ -240,22 +242,19 @@ __global__ __launch_bounds__(256) void fp8_quant_kernel(const QuantParams p, int
     }
 }
 
-template <typename T, bool VEC>
+template <typename T>
 static hipError_t launch_quant(const QuantParams& p, hipStream_t st) {
     const int64_t tr = (p.rows + 127) / 128, tc = (p.cols + 127) / 128;
     const int64_t blocks = (tr + 3) / 4 * ((tc + 3) / 4), n = (blocks + 7) / 8 * 128;     // whole rounds of eight blocks of 16 tiles
     const int64_t gx = n < 1 << 23 ? n : 1 << 23;                                       // a launch has fewer than 2^32 threads along x
     const dim3 grid((unsigned)gx, (unsigned)((n + gx - 1) / gx));
-    if (p.e5m2) hipLaunchKernelGGL((fp8_quant_kernel<T, VEC, true>), grid, dim3(256), 0, st, p, tr, tc);
-    else hipLaunchKernelGGL((fp8_quant_kernel<T, VEC, false>), grid, dim3(256), 0, st, p, tr, tc);
+    if (p.e5m2) hipLaunchKernelGGL((fp8_quant_kernel<T, true>), grid, dim3(256), 0, st, p, tr, tc);
+    else hipLaunchKernelGGL((fp8_quant_kernel<T, false>), grid, dim3(256), 0, st, p, tr, tc);
     return hipGetLastError();
 }
 
 hipError_t launch_fp8_quant(const QuantParams& p, hipStream_t st) {
-    const int64_t each = p.x_bf16 ? 8 : 4;                      // values of 16 bytes
-    const bool vec = p.cols % each == 0 && p.ldx % each == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0;
-    if (p.x_bf16) return vec ? launch_quant<__bf16, true>(p, st) : launch_quant<__bf16, false>(p, st);
-    return vec ? launch_quant<float, true>(p, st) : launch_quant<float, false>(p, st);
+    return p.x_bf16 ? launch_quant<__bf16>(p, st) : launch_quant<float>(p, st);
 }
 
 }  // namespace pda
