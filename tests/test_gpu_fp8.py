@@ -206,11 +206,7 @@ def test_matmul_with_a_long_sum(M, N, K):
     _check_matmul(M, N, K, "e5m2", 1, False)
 
 
-@pytest.mark.parametrize("M,N,K,kind,block", [(3000, 4608, 1536, "e4m3", 128), (9594, 1152, 1152, "e5m2", 128), (4608, 1536, 9594, "e5m2", 1), (40000, 130, 640, "e4m3", 128),
-                                              (300, 20000, 300, "e4m3", 1), (1, 8192, 8192, "e4m3", 128), (64, 6144, 4096, "e4m3", 128)])
-def test_larger_matmul_against_fp64_on_the_gpu(M, N, K, kind, block):
-    """More tiles than compute units, ragged ends.  Every result within the matrix instruction's bound (summed magnitudes over 2^13, of which eight consecutive products
-    cannot lose more than seven eighths) and a rounding."""
+def _quantised(M, N, K, kind, block):
     import torch
     import paper_2511_12056_amd as pda
     g = torch.Generator(device="cuda").manual_seed(M + N)
@@ -219,18 +215,65 @@ def test_larger_matmul_against_fp64_on_the_gpu(M, N, K, kind, block):
     b, sb = pda.fp8_empty(N, K, block)
     pda.fp8_quant(x, a, sa)
     pda.fp8_quant(w, b, sb, block_rows=block)
-    out = torch.full((M, N), float("nan"), device="cuda", dtype=torch.bfloat16)
-    pda.fp8_matmul(a, sa, b, sb, out)
-    n = a.shape[1] // 128
+    return a, sa, b, sb
+
+
+def _check_on_the_gpu(out, a, sa, b, sb, block, bias=None):
+    """Every result within the matrix instruction's bound (summed magnitudes over 2^13, of which eight consecutive products cannot lose more than seven eighths) and a rounding."""
+    import torch
+    n, N, K = a.shape[1] // 128, b.shape[0], a.shape[1]
     va = a.double() * sa.double()[:, :n].repeat_interleave(128, dim=1)
     vb = b.double() * sb.double()[:, :n].repeat_interleave(128, dim=1).repeat_interleave(block, dim=0)[:N]
     want = torch.mm(va, vb.t().contiguous())
     # seven dropped shares of the largest of eight products: at most seven times their summed magnitude over 2^13
     tol = torch.mm(va.abs(), vb.abs().t().contiguous()) * (7 * 2.0 ** -13 + K * 2.0 ** -24)
+    if bias is not None:
+        want = want + bias.double()
+        tol = tol + 2.0 ** -24 * want.abs()
     tol = tol + 2.0 ** -8 * (want.abs() + tol)
     assert ((out.double() - want).abs() <= tol).all()
     # and on the whole no further off than a rounding to bf16 (evenly spread: 2^-8 / sqrt(3) at most) and the instruction's share together
     assert (out.double() - want).norm() <= want.norm() * 2.0 ** -8
+
+
+@pytest.mark.parametrize("M,N,K,kind,block", [(3000, 4608, 1536, "e4m3", 128), (9594, 1152, 1152, "e5m2", 128), (4608, 1536, 9594, "e5m2", 1), (40000, 130, 640, "e4m3", 128),
+                                              (300, 20000, 300, "e4m3", 1), (1, 8192, 8192, "e4m3", 128), (64, 6144, 4096, "e4m3", 128)])
+def test_larger_matmul_against_fp64_on_the_gpu(M, N, K, kind, block):
+    """More tiles than compute units, ragged ends."""
+    import torch
+    import paper_2511_12056_amd as pda
+    a, sa, b, sb = _quantised(M, N, K, kind, block)
+    out = torch.full((M, N), float("nan"), device="cuda", dtype=torch.bfloat16)
+    pda.fp8_matmul(a, sa, b, sb, out)
+    _check_on_the_gpu(out, a, sa, b, sb, block)
+
+
+# every tile, alone and in parts of K, with few and many blocks of it
+MIDDLE = [(700, 700, 256), (257, 1500, 300), (150, 2050, 640), (1000, 300, 1000), (500, 517, 1152), (70, 3000, 2176), (150, 3000, 8192),
+          (257, 3000, 100), (500, 1030, 256), (1000, 517, 900), (257, 2050, 1024), (500, 1030, 5120), (700, 300, 3008), (33, 700, 8192), (500, 66, 8192),
+          (2500, 3000, 128), (2000, 2050, 640), (2500, 2050, 1100), (1500, 2050, 2176), (1000, 2050, 2944), (2000, 517, 5120), (500, 2050, 8192)]
+
+
+@pytest.mark.parametrize("M,N,K", MIDDLE)
+@pytest.mark.parametrize("kind,block,gap", [("e4m3", 128, 3), ("e5m2", 1, 8)])
+def test_matmul_of_middle_sizes(M, N, K, kind, block, gap):
+    """With a bias, into a view whose rows lie apart, with a NaN that reaches one row and one column, twice to the same bits."""
+    import torch
+    import paper_2511_12056_amd as pda
+    a, sa, b, sb = _quantised(M, N, K, kind, block)
+    bias = torch.randn(N, device="cuda")
+    whole = torch.full((M, N + gap), 7.0, device="cuda", dtype=torch.bfloat16)
+    pda.fp8_matmul(a, sa, b, sb, whole[:, :N], bias=bias)
+    _check_on_the_gpu(whole[:, :N], a, sa, b, sb, block, bias)
+    assert (whole[:, N:] == 7).all()
+    again = torch.empty(M, N, device="cuda", dtype=torch.bfloat16)
+    assert torch.equal(pda.fp8_matmul(a, sa, b, sb, again, bias=bias), whole[:, :N])
+    a.view(torch.uint8)[M - 1, K - 1] = 0x7f
+    b.view(torch.uint8)[N - 2, 5] = 0x7f
+    got = pda.fp8_matmul(a, sa, b, sb, torch.empty_like(again), bias=bias)
+    nan = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    nan[M - 1] = nan[:, N - 2] = True
+    assert torch.equal(got.isnan(), nan) and torch.equal(torch.where(nan, 0, got), torch.where(nan, 0, again))
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])

@@ -76,6 +76,16 @@ def test_matmul_workspace(pda):
     assert f(8, 8, 128, 256, None) == 1 and f(8, 8, 128, -1, C.byref(C.c_int64())) == 1 and f(8, 8, 100, 256, C.byref(C.c_int64())) == 1
 
 
+@pytest.mark.parametrize("n_cu", [1, 64, 256, 304])
+def test_matmul_workspace_of_extreme_sizes(pda, n_cu):
+    """At most 32 parts, of results padded to tiles of 256."""
+    top = 2 ** 31 - 1
+    for M, N, K in ((1, 1, 2 ** 24 - 128), (top, 1, 128), (1, top, 128), (top, 256, 128), (256, 256, 2 ** 24 - 128), (4000, 4000, 65536), (1, 1, 128), (17, 1, 4096), (65536, 65536, 4096)):
+        n = pda.fp8_matmul_workspace_bytes(M, N, K, n_cu=n_cu)
+        assert 0 <= n <= 32 * 4 * (-(-M // 256) * 256) * (-(-N // 256) * 256)
+        assert n == 0 or K > 128
+
+
 def _rms(pda, x=_addr(0), xt=1, res=_addr(1), rt=0, w=_addr(2), h=_addr(3), y=_addr(4), yt=2, ys=_addr(5), rstd=_addr(6), rows=8, groups=1, D=200, eps=1e-6):
     return pda.lib.pda_rms_norm_fwd(x, xt, res, rt, w, h, y, yt, ys, rstd, rows, groups, D, eps, None)
 
