@@ -276,6 +276,34 @@ def test_matmul_of_middle_sizes(M, N, K, kind, block, gap):
     assert torch.equal(got.isnan(), nan) and torch.equal(torch.where(nan, 0, got), torch.where(nan, 0, again))
 
 
+@pytest.mark.parametrize("shapes", [[(500, 2050, 8192), (33, 700, 8192)], [(70, 66, 40000), (500, 517, 1152)], [(2500, 2050, 200), (3, 40, 256)]])
+def test_captured_products_that_share_a_workspace(shapes):
+    """Two products one after the other in a graph, in parts of K with one workspace or none; replayed with other operands, eager work between the replays."""
+    import torch
+    import paper_2511_12056_amd as pda
+    sets = [_quantised(M, N, K, "e4m3", 128) for M, N, K in shapes]
+    others = [_quantised(M, N, K, "e4m3", 128) for M, N, K in shapes]
+    for o in others:
+        o[0].view(torch.uint8)[:] = o[0].view(torch.uint8).flip(0)
+        o[1].view(torch.uint8)[:] = o[1].view(torch.uint8).flip(0)
+    outs = [torch.empty(M, N, device="cuda", dtype=torch.bfloat16) for M, N, _ in shapes]
+    space = torch.empty(max(pda.fp8_matmul_workspace_bytes(*map(int, (M, N, s[0].shape[1]))) for (M, N, _), s in zip(shapes, sets)) or 256, device="cuda", dtype=torch.uint8)
+    eager = [[pda.fp8_matmul(*s, torch.empty_like(o)) for s, o in zip(group, outs)] for group in (sets, others)]
+    held = [[t.clone() for t in s] for s in sets]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for s, o in zip(held, outs):
+            pda.fp8_matmul(*s, o, workspace=space)
+    for turn in (0, 1, 1, 0):
+        for h, s in zip(held, (sets, others)[turn]):
+            for a, b in zip(h, s):
+                a.view(torch.uint8).copy_(b.view(torch.uint8))
+        space.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, e) for o, e in zip(outs, eager[turn]))
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_matmul_without_k_is_the_bias(M):
     import torch
