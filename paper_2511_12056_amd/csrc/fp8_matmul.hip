@@ -289,7 +289,8 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(to + (i * 8 + j) * 256) = taken(acc[i][j]);
         } else {
             // 16 rows at a time through LDS (granules of 16 bytes at granule ^ row), so that a store is 256 bytes of four rows: with 64 bytes of 16 rows, straight from the
-            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of 723 (both without the stores' hint)
+            // registers, 119 056 x 4 608 x 1 536 took 746 us instead of 723 (both without the stores' hint).  Under the
+            // matrix instructions of the last step's second half and the next tile's first, one accumulator a slot, it took 705 instead of 695: the card's power is the same
             const int rows = (int)(p.M - it.m0 < 256 ? p.M - it.m0 : 256), cols = (int)(p.N - it.n0 < 256 ? p.N - it.n0 : 256);
             stored = rows == 256 && cols == 256 && p.vec_out;
             f32x4 bias[8];
