@@ -43,6 +43,18 @@ __device__ __forceinline__ void lds_dma4(const void* sbase, unsigned voff, unsig
 typedef u32x2 u32x2_loose __attribute__((aligned(2)));      // rows of any length start at any element
 typedef u32x4 u32x4_loose __attribute__((aligned(2)));
 
+// The first n (or all) of eight values.
+__device__ __forceinline__ void store_row(__bf16* at, const u32x4& x, int64_t n) {
+    typedef unsigned u32_loose __attribute__((aligned(2)));
+    if (n >= 8) {
+        *reinterpret_cast<u32x4_loose*>(at) = x;
+        return;
+    }
+    if (n & 4) *reinterpret_cast<u32x2_loose*>(at) = u32x2{x[0], x[1]};
+    if (n & 2) *reinterpret_cast<u32_loose*>(at + (n & 4)) = n & 4 ? x[2] : x[0];
+    if (n & 1) at[n & 6] = __builtin_bit_cast(__bf16, (unsigned short)(n & 4 ? n & 2 ? x[3] : x[2] : n & 2 ? x[1] : x[0]));
+}
+
 // Four results of row m, columns n .. n + 3: the bias added, rounded.
 __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t n, f32x4 v) {
     __bf16* o = p.out + m * p.ldo + n;
@@ -61,20 +73,13 @@ __device__ __forceinline__ void store4(const MatmulParams& p, int64_t m, int64_t
 
 // Eight results of row m, columns n .. n + 7.
 __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t n, f32x4 v0, f32x4 v1) {
-    __bf16* o = p.out + m * p.ldo + n;
-    if (n + 8 <= p.N) {
-        if (p.bias) {
+    float bias[8] = {};
+    if (p.bias) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v0[e] += p.bias[n + e];
-                v1[e] += p.bias[n + 4 + e];
-            }
-        }
-        *reinterpret_cast<u32x4_loose*>(o) = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
-    } else {
-        store4(p, m, n, v0);
-        if (n + 4 < p.N) store4(p, m, n + 4, v1);
+        for (int e = 0; e < 8; ++e) bias[e] = n + e < p.N ? p.bias[n + e] : 0.f;
     }
+    store_row(p.out + m * p.ldo + n, u32x4{pack_bf16(v0[0] + bias[0], v0[1] + bias[1]), pack_bf16(v0[2] + bias[2], v0[3] + bias[3]),
+                                           pack_bf16(v1[0] + bias[4], v1[1] + bias[5]), pack_bf16(v1[2] + bias[6], v1[3] + bias[7])}, p.N - n);
 }
 
 // ---- large products -----------------------------------------------------------------------------------------------
@@ -87,14 +92,13 @@ __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t
 // (1 730 cycles) at least, and a wavefront asks for 1 KB every third slot: faster, requests wait in line and matrix instructions behind them.
 // A workgroup goes through its items (tiles, or ranges of K of a tile) without a break; blocks are fetched across the border of an item too.
 constexpr int kLargeA = 0, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeScales = 2 * kLargeStage, kLargeSa = 0, kLargeSb = 1024, kLargeBias = kLargeScales + 2 * 2048, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
-constexpr int kLargeGroup = 8;          // tiles of m that share tiles of n in a row
 
-// Place of tile t of tm x tn, in an order in which neighbours share operands: blocks of kLargeGroup tiles of m, tile of n by tile of n.
-__device__ __forceinline__ void tile_place(int t, int tm, int tn, int& m, int& n) {
-    const int group = t / (kLargeGroup * tn), rem = t - group * (kLargeGroup * tn);
-    const int left = tm - group * kLargeGroup, gm = left < kLargeGroup ? left : kLargeGroup;
-    n = rem / gm;
-    m = group * kLargeGroup + rem - n * gm;
+// Place of tile t of tm x tn, in an order in which neighbours share operands: strips of `strip` tiles of n, tile of m by tile of m.
+__device__ __forceinline__ void tile_place(int t, int tm, int tn, int strip, int& m, int& n) {
+    const int before = t / (strip * tm), rem = t - before * (strip * tm);
+    const int left = tn - before * strip, width = left < strip ? left : strip;
+    m = rem / width;
+    n = before * strip + rem - m * width;
 }
 
 // An accumulator's values where they are wanted: left to itself the compiler copies all 256 out of their registers first, into memory.
@@ -125,7 +129,7 @@ struct LargeItem {
 __device__ __forceinline__ LargeItem large_item(const MatmulParams& p, int i) {
     const int tm = (int)((p.M + 255) / 256), tn = (int)((p.N + 255) / 256), tiles = tm * tn, part = i / tiles;
     int m, n;
-    tile_place(i - part * tiles, tm, tn, m, n);
+    tile_place(i - part * tiles, tm, tn, p.strip, m, n);
     const int nk_all = (int)(p.K / 128), kb0 = part * p.part_steps, nk = nk_all - kb0 < p.part_steps ? nk_all - kb0 : p.part_steps;
     return {(int64_t)m * 256, (int64_t)n * 256, kb0, nk};
 }
@@ -332,15 +336,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
                 });
             } else {
                 through([&](int k, const u32x4& x) __attribute__((always_inline)) {
-                    if (row + k >= rows) return;
-                    __bf16* at = reinterpret_cast<__bf16*>(to) + (int64_t)(row + k) * p.ldo + col;
-                    if (col + 8 <= cols) {
-                        *reinterpret_cast<u32x4_loose*>(at) = x;
-                        return;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (col + e < cols) at[e] = __builtin_bit_cast(__bf16, (unsigned short)(x[e / 2] >> (16 * (e % 2))));
+                    if (row + k < rows && col < cols) store_row(reinterpret_cast<__bf16*>(to) + (int64_t)(row + k) * p.ldo + col, x, cols - col);
                 });
             }
         }
@@ -516,7 +512,7 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(const MatmulParams
     if (e >= TM * TN / C) return;
     int im, in, r, c, at, second = 4;                           // row and column in the tile, place of its first four sums, of the others behind them
     if constexpr (TM == 256) {
-        tile_place(tile, tm, tn, im, in);
+        tile_place(tile, tm, tn, p.strip, im, in);
         const int lane = e & 63, jj = e >> 6 & 3, i = e >> 8 & 7, w = e >> 11;
         r = (w >> 1) * 128 + i * 16 + (lane & 15);
         c = (w & 1) * 128 + jj * 32 + (lane >> 4) * 8;
@@ -571,7 +567,7 @@ static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
     else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.365 : 0.33));
     if (parts > 1) {                                            // parts written and read, more than 128 MB of them from memory: 4 608 x 1 536 x 119 056 took 678 us in
         const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units, 717 in 7 on 252 (three times)
-        t += 4.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
+        t += 5.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
     }
     return t;
 }
@@ -653,6 +649,10 @@ static hipError_t launch_form(const MatmulParams& p, hipStream_t st) {
 hipError_t launch_fp8_matmul(MatmulParams p, const MatmulPlan& w, hipStream_t st) {
     p.parts = w.parts;
     p.part_steps = w.part_steps;
+    // strips of b of which an XCD's L2 (4 MB) keeps 2.5 MB while a runs past, six tiles at least: 32 compute units' tiles side by side are then about a square.
+    // Blocks of eight tiles of m, tile of n by tile of n, took 768 us instead of 725 at 4 608 x 119 056 x 1 536, 664 instead of 653 at 4 608 x 1 536 x 119 056 and as long elsewhere
+    const int tn = (int)((p.N + 255) / 256), width = (int)(2500000 / (256 * 128 * (int64_t)(w.part_steps > 0 ? w.part_steps : 1))), strip = width > 6 ? width : 6, strips = (tn + strip - 1) / strip;
+    p.strip = strips > 0 ? (tn + strips - 1) / strips : 1;
     p.vec_out = p.ldo % 8 == 0 && p.ldo < (int64_t)1 << 22 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;      // 256 rows within 2^32 bytes
     if (p.K == 0) {
         const int64_t y = p.M < 65535 ? p.M : 65535;

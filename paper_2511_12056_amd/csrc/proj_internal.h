@@ -36,6 +36,7 @@ struct MatmulParams {
     int e5m2;                // of a
     int parts;               // ranges of K, each of part_steps blocks of 128 (the last may have fewer)
     int part_steps;
+    int strip;               // large tiles: tiles of n in a row
     int vec_out;             // rows of out lie at multiples of 16 bytes
 };
 constexpr int kMatmulMaxParts = 32;

@@ -251,7 +251,8 @@ def test_larger_matmul_against_fp64_on_the_gpu(M, N, K, kind, block):
 # every tile, alone and in parts of K, with few and many blocks of it
 MIDDLE = [(700, 700, 256), (257, 1500, 300), (150, 2050, 640), (1000, 300, 1000), (500, 517, 1152), (70, 3000, 2176), (150, 3000, 8192),
           (257, 3000, 100), (500, 1030, 256), (1000, 517, 900), (257, 2050, 1024), (500, 1030, 5120), (700, 300, 3008), (33, 700, 8192), (500, 66, 8192),
-          (2500, 3000, 128), (2000, 2050, 640), (2500, 2050, 1100), (1500, 2050, 2176), (1000, 2050, 2944), (2000, 517, 5120), (500, 2050, 8192)]
+          (2500, 3000, 128), (2000, 2050, 640), (2500, 2050, 1100), (1500, 2050, 2176), (1000, 2050, 2944), (2000, 517, 5120), (500, 2050, 8192),
+          (2000, 2049, 200), (2000, 2051, 128), (2000, 2052, 300), (2000, 2053, 128), (2000, 2054, 200), (2000, 2055, 128), (500, 1029, 256), (500, 1031, 256)]
 
 
 @pytest.mark.parametrize("M,N,K", MIDDLE)
