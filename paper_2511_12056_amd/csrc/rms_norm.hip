@@ -23,6 +23,68 @@ __device__ __forceinline__ void store_row(void* p, int type, int64_t at, int D, 
     else RowIO<float, VEC, TPR, NV>::store(static_cast<float*>(p) + at, D, t, x);
 }
 
+// A block's largest value within 32 of its last bits of where the scale doubles (1.75 times a power of two, large enough that the byte is not held at 0).
+__device__ __forceinline__ bool is_close(float top) {
+    const unsigned u = __float_as_uint(top);
+    return (u & 0x7fffffu) - 0x600000u + 32u <= 64u && u >> 23 >= 8;
+}
+
+// A largest value so near to where the scale doubles that fp32 may be on the wrong side: 64 bits decide.  fp32 is off by at most 25 half-steps of 2^-23 (38 of them in the
+// sum: up to 32 additions in a thread and 6 across lanes, halved by the root; then the root, the quotient and two products), 22 of the steps looked at here, near 1.75.
+// One row of 10 000 at 12 blocks a row: its results are written again, from memory and group by group, so that the others need no
+// registers for it (119 056 x 1 536: 347 us with and without; 4 797 x 1 152: 12 instead of 10.6 us when there is such a row, for its own time).
+template <bool VEC, int TPR>
+__device__ __forceinline__ void settle_row(const RmsNormParams& p, int64_t r, int t, float rstd) {
+    const int D = p.D;
+    const int64_t cols = fp8_cols(D), scale_cols = fp8_scale_cols(D), g = p.groups == 1 ? 0 : (unsigned)r / (unsigned)p.group_rows;
+    unsigned char* y = static_cast<unsigned char*>(p.y) + r * cols;
+    constexpr int L = TPR < 64 ? TPR : 64;              // a wavefront by itself: what the row's others have stored lies ahead of the sum's barrier
+    const auto stored = [&](int c, int lane, float (&x)[1][4]) __attribute__((always_inline)) {      // from column c on
+        if (p.res) load_row<VEC, TPR, 1>(p.h, p.h_type, r * D + c, D - c, lane, x);
+        else load_row<VEC, TPR, 1>(p.x, p.x_type, r * D + c, D - c, lane, x);
+    };
+    double square = 0.0;
+#pragma unroll 3
+    for (int c = 0; c < D; c += 4 * L) {
+        float x[1][4];
+        stored(c, t % L, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) square = __builtin_fma((double)x[0][e], (double)x[0][e], square);
+    }
+#pragma unroll
+    for (int o = 1; o < L; o *= 2) square += __shfl_xor(square, o);
+    square += (double)p.eps * D;                        // D over the square of rstd: no root and no quotient
+#pragma unroll 1
+    for (int at = 0; at < cols; at += 4 * TPR) {
+        const int c = at + 4 * t;
+        float x[1][4], w[1][4] = {{1.f, 1.f, 1.f, 1.f}}, top = 0.f;
+        double exact = 0.0;
+        stored(at, t, x);
+        if (p.weight) RowIO<float, VEC, TPR, 1>::load(p.weight + g * D + at, D - at, t, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double product = fabs((double)x[0][e] * w[0][e]);
+            x[0][e] = c + e < D ? x[0][e] * (p.weight ? rstd * w[0][e] : rstd) : 0.f;
+            const float m = finite_magnitude(x[0][e]);
+            top = fmaxf(top, m);
+            if (m > 0.f && product > exact) exact = product;
+        }
+        top = lane_max<32>(top);
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) exact = fmax(exact, __shfl_xor(exact, o));
+        unsigned byte = scale_byte<false>(top);
+        if (is_close(top)) {
+            const float border = __uint_as_float((__float_as_uint(top) & 0x7f800000u) | 0x600000u);
+            byte = scale_byte<false>(border) + (exact * exact * D > (double)border * border * square ? 1u : 0u);
+        }
+        const float f = inverse_scale(byte);
+        if (c < cols) {
+            __builtin_nontemporal_store(pack_fp8<false>(x[0][0] * f, x[0][1] * f, x[0][2] * f, x[0][3] * f), reinterpret_cast<unsigned*>(y + c));
+            if (t % 32 == 0) p.y_scales[r * scale_cols + c / 128] = (uint8_t)byte;
+        }
+    }
+}
+
 template <bool VEC, int TPR, int NV>
 __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const RmsNormParams p) {
     constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
@@ -69,21 +131,23 @@ __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const Rms
     if (p.y_type == PDA_E4M3) {
         if constexpr (TPR >= 32) {
             const int64_t cols = fp8_cols(D), scale_cols = fp8_scale_cols(D);
+            bool close = false;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * TPR + t) * 4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[i][e] = c + e < D ? h[i][e] : 0.f;       // (0 times a NaN or an infinity above)
-                float top = fmaxf(fmaxf(finite_magnitude(h[i][0]), finite_magnitude(h[i][1])), fmaxf(finite_magnitude(h[i][2]), finite_magnitude(h[i][3])));
-                top = lane_max<32>(top);
+                const float top = lane_max<32>(fmaxf(fmaxf(finite_magnitude(h[i][0]), finite_magnitude(h[i][1])), fmaxf(finite_magnitude(h[i][2]), finite_magnitude(h[i][3]))));
                 const unsigned byte = scale_byte<false>(top);
                 const float f = inverse_scale(byte);
+                close = close || is_close(top);
                 if (c < cols) {                                 // (a block of lanes alike)
                     const unsigned q = pack_fp8<false>(h[i][0] * f, h[i][1] * f, h[i][2] * f, h[i][3] * f);
                     __builtin_nontemporal_store(q, reinterpret_cast<unsigned*>(static_cast<unsigned char*>(p.y) + r * cols + c));
                     if (t % 32 == 0) p.y_scales[r * scale_cols + c / 128] = (uint8_t)byte;
                 }
             }
+            if (__any(close)) settle_row<VEC, TPR>(p, r, t, rstd);
         }
     } else {
         store_row<VEC, TPR, NV>(p.y, p.y_type, r * D, D, t, h);

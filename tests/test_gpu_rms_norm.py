@@ -148,6 +148,31 @@ def test_without_weight_or_rstd_and_in_place(yt):
         assert torch.equal(h, ref[0]) and torch.equal(out[1].view(torch.uint8), ref[1].view(torch.uint8))
 
 
+@pytest.mark.parametrize("xt,rt", [("bf16", "fp32"), ("fp32", "none"), ("bf16", "bf16")])
+@pytest.mark.parametrize("rows,D", [(3000, 128), (1500, 203), (900, 1536), (700, 2176), (300, 5000)])
+def test_scales_at_their_borders(rows, D, xt, rt):
+    """A weight a row that puts the largest value of one of its blocks within some 2^-22 of 1.75 times a power of two, where the scale doubles: the bytes of those blocks are what the
+    definition gives in 64 bits, on either side."""
+    import torch
+    x, res, _ = _inputs(rows + D, rows, D, 1, xt, rt)
+    h = (x.float() if res is None else (x.float() + res.float()).to(res.dtype).float()).double()
+    y = h / torch.sqrt(h.square().mean(dim=-1, keepdim=True) + float(np.float32(EPS)))
+    pad = torch.nn.functional.pad(y.abs(), (0, -D % 128)).view(rows, -1, 128).amax(dim=-1)
+    r = torch.arange(rows, device="cuda")
+    block = r % pad.shape[1]
+    step = torch.linspace(-2.0 ** -22, 2.0 ** -22, rows, device="cuda", dtype=torch.float64)
+    w = (1.75 * (1 << r % 20).double() * (1 + step) / pad[r, block]).float()
+    out = _forward(x, res, w[:, None].expand(rows, D).contiguous(), "e4m3")
+    top = pad[r, block] * w.double()
+    got = out[2].view(torch.uint8)[r, block].double()
+    mantissa, e = torch.frexp(top)                          # top = mantissa 2^e, 1/2 <= mantissa < 1: 2^(e - 1 - 8) is enough up to 0.875
+    assert torch.equal(got, (e - 9 + (mantissa > 0.875).int() + 127).double())
+    assert (mantissa > 0.875).any() and (mantissa <= 0.875).any()
+    if res is not None:                                     # and in place
+        again = _forward(x, res, w[:, None].expand(rows, D).contiguous(), "e4m3", h=res)
+        assert torch.equal(again[2].view(torch.uint8)[r, block], out[2].view(torch.uint8)[r, block]) and torch.equal(again[1].view(torch.uint8), out[1].view(torch.uint8))
+
+
 @pytest.mark.parametrize("ht", TYPES)
 def test_backward_in_place(ht):
     import torch
