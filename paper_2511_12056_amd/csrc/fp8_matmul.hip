@@ -350,8 +350,9 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
 
 // ---- middle tiles -------------------------------------------------------------------------------------------------
 // TM x TN results a workgroup of 2 x 2 wavefronts, for products that would leave most compute units without a large tile: there time is the latency of
-// memory, so seven blocks of 128 are on their way at once, in a ring of eight LDS buffers with a barrier a block.  A block takes 0.33 us (32 x 64) or 0.37 us (64 x 64).
-// 256 x 1 536 x 4 096 is 13.1 us with the call (32 x 64: 192 workgroups; 64 x 64: 96 workgroups, 14.8), 16.2 with operands straight from memory into registers.
+// memory, so six blocks of 128 are on their way at once, in a ring of eight LDS buffers with a barrier every two blocks.  A block takes 0.28 us (32 x 64) or 0.35 us (64 x 64).
+// 256 x 1 536 x 4 096 is 11.3 us with the call (32 x 64: 192 workgroups; 64 x 64: 96 workgroups, 14.1), 13.2 with a barrier every block, 16.2 with operands straight
+// from memory into registers.
 constexpr int kMidRing = 8, kMidChunks = 4;             // words of scales: of four blocks each
 template <int TM, int TN> constexpr int mid_stage() { return (TM + TN) * 128; }
 template <int TM, int TN> constexpr int mid_smem() { return kMidRing * mid_stage<TM, TN>() + kMidChunks * 512; }
@@ -402,37 +403,42 @@ __global__ __launch_bounds__(256) void fp8_matmul_mid_kernel(const MatmulParams 
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < kMidRing - 1; ++t)
+    for (int t = 0; t < kMidRing - 2; ++t)
         if (t < nk) fetch(t);
-    for (int t = 0; t < nk; ++t) {
-        // block t has arrived when no more are on their way than belong to the blocks behind it (scales apart: then for a little longer)
-        switch (nk - 1 - t) {
+    for (int t = 0; t < nk; t += 2) {
+        // blocks t and t + 1 have arrived when no more are on their way than belong to the blocks behind them (scales apart: then for a little longer)
+        switch (nk - 2 - t) {
+            case -1:
             case 0: wait_vmcnt<0>(); break;
             case 1: wait_vmcnt<PA + PB>(); break;
             case 2: wait_vmcnt<2 * (PA + PB)>(); break;
             case 3: wait_vmcnt<3 * (PA + PB)>(); break;
-            case 4: wait_vmcnt<4 * (PA + PB)>(); break;
-            case 5: wait_vmcnt<5 * (PA + PB)>(); break;
-            default: wait_vmcnt<6 * (PA + PB)>();
+            default: wait_vmcnt<4 * (PA + PB)>();
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");    // and all have read block t - 1
-        if (t + kMidRing - 1 < nk) fetch(t + kMidRing - 1);
-        const unsigned char* s = matmul_smem_ + t % kMidRing * STAGE;
-        const int kb = kb0 + t;
-        const unsigned char* sc = matmul_smem_ + SCALES + (kb >> 2) % kMidChunks * 512 + (kb & 3);
-        i32x8 fb[NT];
-        int sb[NT];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");    // and all have read blocks t - 2 and t - 1
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            fb[j] = join8(*reinterpret_cast<const i32x4*>(s + rb + j * 512), *reinterpret_cast<const i32x4*>(s + (rb ^ 64) + j * 512));
-            sb[j] = sc[256 + (nrow + 4 * j) * 4];
-        }
+        for (int u = 0; u < 2; ++u)
+            if (t + kMidRing - 2 + u < nk) fetch(t + kMidRing - 2 + u);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const i32x8 fa = join8(*reinterpret_cast<const i32x4*>(s + ra + i * 2048), *reinterpret_cast<const i32x4*>(s + (ra ^ 64) + i * 2048));
-            const int sa = sc[(mrow + 16 * i) * 4];
+        for (int u = 0; u < 2; ++u) {
+            if (u == 1 && t + 1 >= nk) break;
+            const unsigned char* s = matmul_smem_ + (t + u) % kMidRing * STAGE;
+            const int kb = kb0 + t + u;
+            const unsigned char* sc = matmul_smem_ + SCALES + (kb >> 2) % kMidChunks * 512 + (kb & 3);
+            i32x8 fb[NT];
+            int sb[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = mfma<E5M2>(fb[j], fa, acc[i][j], sb[j], sa);
+            for (int j = 0; j < NT; ++j) {
+                fb[j] = join8(*reinterpret_cast<const i32x4*>(s + rb + j * 512), *reinterpret_cast<const i32x4*>(s + (rb ^ 64) + j * 512));
+                sb[j] = sc[256 + (nrow + 4 * j) * 4];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const i32x8 fa = join8(*reinterpret_cast<const i32x4*>(s + ra + i * 2048), *reinterpret_cast<const i32x4*>(s + (ra ^ 64) + i * 2048));
+                const int sa = sc[(mrow + 16 * i) * 4];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma<E5M2>(fb[j], fa, acc[i][j], sb[j], sa);
+            }
         }
     }
     keep(acc);
@@ -553,7 +559,7 @@ static constexpr FormSize kForms[MatmulPlan::FORMS] = {{16, 16}, {32, 64}, {64, 
 // to 119 056 x 4 608 x 1 536 (256 compute units; us, the least of each row is what the rule takes or within 10 % of it):
 //                             few    32 x 64    64 x 64    large    large, 4 parts
 //       1 x 8 192 x 8 192      14         23         26       75          33
-//     256 x 1 536 x 4 096      29         13         15       40          19
+//     256 x 1 536 x 4 096      29         11         14       40          19
 //   1 000 x 1 536 x 1 536      37         17         14       30          18
 //   2 000 x 1 536 x 6 144     282        102         59       67          35
 //   2 048 x 4 608 x 1 536     207         91         56       22          53
@@ -564,7 +570,7 @@ static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
     double t;
     if (f == MatmulPlan::LARGE) t = 6.0 + (double)rounds * (steps * (1.07 + 0.4 * (load < 1.0 ? load : 1.0)) + 4.0);
     else if (f == MatmulPlan::FEW) t = 3.0 + steps * (load > 1.1 ? 0.11 * load : 0.12);
-    else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.365 : 0.33));
+    else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.345 : 0.28));
     if (parts > 1) {                                            // parts written and read, more than 128 MB of them from memory: 4 608 x 1 536 x 119 056 took 678 us in
         const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units, 717 in 7 on 252 (three times)
         t += 5.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
