@@ -35,18 +35,14 @@ __device__ __forceinline__ unsigned pack_fp8(float a, float b, float c, float d)
     return (unsigned)r;
 }
 
-// Maximum over groups of N consecutive lanes (N = 16, 32), in every lane of the group.
-template <int N>
-__device__ __forceinline__ float lane_max(float x) {
+// Maximum over groups of 32 consecutive lanes, in every lane of the group.
+__device__ __forceinline__ float lane_max32(float x) {
     x = fmaxf(x, lane_perm<0xB1>(x));
     x = fmaxf(x, lane_perm<0x4E>(x));
     x = fmaxf(x, lane_perm<0x141>(x));
     x = fmaxf(x, lane_perm<0x140>(x));
-    if constexpr (N >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    }
-    return x;
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 }  // namespace pda

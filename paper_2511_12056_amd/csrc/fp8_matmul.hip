@@ -91,6 +91,8 @@ __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t
 // after the next.  Behind the second (slot 31) all have read those rows and their scales too, which are fetched, and the rest of the next block has arrived.  A fetch has 54 slots
 // (1 730 cycles) at least, and a wavefront asks for 1 KB every third slot: faster, requests wait in line and matrix instructions behind them.
 // A workgroup goes through its items (tiles, or ranges of K of a tile) without a break; blocks are fetched across the border of an item too.
+// 119 056 x 4 608 x 1 536: 680 to 735 us (2.3 to 2.5 PFLOP/s; boxes differ), of which 65 are stores and 70 conversion and LDS; 8 192^3: 2.9 PFLOP/s.  The matrix units are 64 to 71 %
+// busy at 1.9 to 2.0 of 2.4 GHz.
 constexpr int kLargeA = 0, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeScales = 2 * kLargeStage, kLargeSa = 0, kLargeSb = 1024, kLargeBias = kLargeScales + 2 * 2048, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
 
 // Place of tile t of tm x tn, in an order in which neighbours share operands: strips of `strip` tiles of n, tile of m by tile of m.
@@ -460,8 +462,8 @@ __global__ __launch_bounds__(256) void fp8_matmul_mid_kernel(const MatmulParams 
 
 // ---- few rows -----------------------------------------------------------------------------------------------------
 // 16 x 16 results a workgroup, whose four wavefronts each take a range of K, straight from memory into registers without a barrier, and add their sums in LDS, in
-// order: for up to 16 rows, where every row of b is read once and that is all the time there is.  1 x 4 608 x 1 536 is 10.4 us with the call, 4.4 us without; 1 x 8 192 x
-// 8 192 is 14.3 (32 x 64 tiles: 23).
+// order: for up to 16 rows, where every row of b is read once and that is all the time there is.  1 x 4 608 x 1 536 is 10.2 us with the call, 4.9 us without; 1 x 8 192 x
+// 8 192 is 14.3 (32 x 64 tiles: 19.5).
 constexpr int kFewWaves = 4, kFewAhead = 4;             // blocks in registers
 template <bool E5M2>
 __global__ __launch_bounds__(kFewWaves * 64) void fp8_matmul_few_kernel(const MatmulParams p) {
@@ -558,11 +560,11 @@ static constexpr FormSize kForms[MatmulPlan::FORMS] = {{16, 16}, {32, 64}, {64, 
 // An estimate of a launch's time in us, for choosing among the forms and numbers of parts.  Its rates are fits to every form's times at 14 products, from 1 x 8 192 x 8 192
 // to 119 056 x 4 608 x 1 536 (256 compute units; us, the least of each row is what the rule takes or within 10 % of it):
 //                             few    32 x 64    64 x 64    large    large, 4 parts
-//       1 x 8 192 x 8 192      14         23         26       75          33
+//       1 x 8 192 x 8 192      14         20         24       74          33
 //     256 x 1 536 x 4 096      29         11         14       40          19
-//   1 000 x 1 536 x 1 536      37         17         14       30          18
-//   2 000 x 1 536 x 6 144     282        102         59       67          35
-//   2 048 x 4 608 x 1 536     207         91         56       22          53
+//   1 000 x 1 536 x 1 536      37         15         14       21          18
+//   2 000 x 1 536 x 6 144     281         85         56       59          35
+//   2 048 x 4 608 x 1 536     207         80         54       20          56
 static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
     const FormSize& s = kForms[f];
     const int64_t items = tiles * parts, rounds = (items + n_cu - 1) / n_cu;

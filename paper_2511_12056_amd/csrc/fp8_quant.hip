@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void fp8_quant_kernel(const QuantParams p, int
     const int64_t q_cols = fp8_cols(p.cols), qt_cols = fp8_cols(p.rows);
     const int64_t q_sc = fp8_scale_cols(p.cols), qt_sc = fp8_scale_cols(p.rows);
     if (p.square) {
-        const float top = pair_max(lane_max<32>(__uint_as_float(H::one(most))));
+        const float top = pair_max(lane_max32(__uint_as_float(H::one(most))));
         if ((t & 63) == 0) col_tops[w][0] = __float_as_uint(top);
         __syncthreads();
         float all = 0.f;

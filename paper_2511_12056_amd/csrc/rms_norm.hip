@@ -4,6 +4,8 @@
 //
 // Forward, the types of x, the residual and y are branches that all threads take alike (36 combinations of them would otherwise be as many kernels
 // a row length); an access by groups of four keeps a block of 128 columns in 32 consecutive lanes, whose largest magnitude five lane permutations find.
+//
+// 119 056 x 1 536: forward, bf16 x and fp32 stream to 8 bits, 347 us (5.8 TB/s); backward, bf16 dy, fp32 h and dres, 471 us (5.5 TB/s; 6 us of them the second kernel).
 #include <hip/hip_runtime.h>
 #include "attn_internal.h"
 #include "fp8_device.h"
@@ -69,7 +71,7 @@ __device__ __forceinline__ void settle_row(const RmsNormParams& p, int64_t r, in
             top = fmaxf(top, m);
             if (m > 0.f && product > exact) exact = product;
         }
-        top = lane_max<32>(top);
+        top = lane_max32(top);
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) exact = fmax(exact, __shfl_xor(exact, o));
         unsigned byte = scale_byte<false>(top);
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const Rms
                 const int c = (i * TPR + t) * 4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[i][e] = c + e < D ? h[i][e] : 0.f;       // (0 times a NaN or an infinity above)
-                const float top = lane_max<32>(fmaxf(fmaxf(finite_magnitude(h[i][0]), finite_magnitude(h[i][1])), fmaxf(finite_magnitude(h[i][2]), finite_magnitude(h[i][3]))));
+                const float top = lane_max32(fmaxf(fmaxf(finite_magnitude(h[i][0]), finite_magnitude(h[i][1])), fmaxf(finite_magnitude(h[i][2]), finite_magnitude(h[i][3]))));
                 const unsigned byte = scale_byte<false>(top);
                 const float f = inverse_scale(byte);
                 close = close || is_close(top);
