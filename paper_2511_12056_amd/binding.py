@@ -412,13 +412,24 @@ def pack_heads(x, y, unit_rms: bool, premul: float = 1.0, stream=None):
 
 # ---- training: gradients, layer norm (include/pipedit_train.h) ----------------------------------------------
 
-def _type_code(t, name):
+@functools.lru_cache(maxsize=None)
+def _torch():
+    """torch, without an import statement's search in every check: a call on few rows is bound by host time."""
     import torch
-    if t.dtype is torch.float32:
-        return PDA_F32
-    if t.dtype is torch.bfloat16:
-        return PDA_BF16
-    raise ValueError(f"{name}: expected fp32 or bf16, got {t.dtype}")
+    return torch
+
+
+@functools.lru_cache(maxsize=None)
+def _type_codes():
+    torch = _torch()
+    return {torch.float32: PDA_F32, torch.bfloat16: PDA_BF16}, {torch.float8_e4m3fn: PDA_E4M3, torch.float8_e5m2: PDA_E5M2}
+
+
+def _type_code(t, name):
+    code = _type_codes()[0].get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected fp32 or bf16, got {t.dtype}")
+    return code
 
 
 def _elsewhere(t):
@@ -435,7 +446,7 @@ def _stream_of(current: int, stream):
 
 def _on_current_device(stream, *tensors):
     """A kernel runs on the current device and would follow another device's addresses there."""
-    import torch
+    torch = _torch()
     current = torch.cuda.current_device()
     _stream_of(current, stream)
     for t in tensors:
@@ -445,7 +456,7 @@ def _on_current_device(stream, *tensors):
 
 def _workspace(nbytes: int, workspace, stream):
     """The given workspace, checked, or a new one from torch's allocator, on the stream of the call that is to use it."""
-    import torch
+    torch = _torch()
     if workspace is None:
         if nbytes == 0:
             return None
@@ -536,7 +547,7 @@ def attn_bwd_strided(dout, q, k, v, out, lse, dq, dk, dv, scale: float, kv_valid
 def _norm_sizes(stream, x, per_row, params, others):
     """Rows, D and groups of a call, and that all tensors and the stream are of the current device (others: of the shape of x, a workspace).  per_row: fp32 with an entry per row; params: fp32 [D] or [groups, D], which must agree; None: not wanted.
     (One function: a call on few rows is bound by host time.)"""
-    import torch
+    torch = _torch()
     f32, device = torch.float32, x.get_device()
     if device < 0 or x.dim() < 1 or not x.is_contiguous():
         raise ValueError("x: expected a contiguous cuda tensor of at least one axis")
@@ -633,12 +644,10 @@ def pack_heads_bwd(dy, x, dx, unit_rms: bool, premul: float = 1.0, stream=None):
 # ---- projections: RMS norm, 8-bit matrices and their product, rotary positions (include/pipedit_proj.h) -------
 
 def _fp8_code(t, name):
-    import torch
-    if t.dtype is torch.float8_e4m3fn:
-        return PDA_E4M3
-    if t.dtype is torch.float8_e5m2:
-        return PDA_E5M2
-    raise ValueError(f"{name}: expected float8_e4m3fn or float8_e5m2, got {t.dtype}")
+    code = _type_codes()[1].get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected float8_e4m3fn or float8_e5m2, got {t.dtype}")
+    return code
 
 
 def _up(n: int, m: int) -> int:
@@ -646,17 +655,17 @@ def _up(n: int, m: int) -> int:
 
 
 def _expect_fp8(q, scales, rows: int, cols: int, block_rows: int, name: str):
-    """q [rows, cols padded to 128] and its scales [blocks of rows, blocks of columns padded to 4]."""
-    import torch
-    _fp8_code(q, name)
+    """q [rows, cols padded to 128] and its scales [blocks of rows, blocks of columns padded to 4] -> the code of its type."""
+    code = _fp8_code(q, name)
     width = -(-cols // 128)
     shape = (rows, 128 * width)
     if q.shape != shape or not q.is_contiguous() or not q.is_cuda:
         raise ValueError(f"{name}: expected contiguous cuda {shape}, got {tuple(q.shape)} contiguous={q.is_contiguous()} cuda={q.is_cuda}")
     shape = (rows if block_rows == 1 else -(-rows // block_rows), width + 3 & ~3)
-    if scales is None or scales.dtype is not torch.float8_e8m0fnu or scales.shape != shape or not scales.is_contiguous() or not scales.is_cuda:
+    if scales is None or scales.dtype is not _torch().float8_e8m0fnu or scales.shape != shape or not scales.is_contiguous() or not scales.is_cuda:
         raise ValueError(f"{name}_scales: expected contiguous cuda float8_e8m0fnu {shape}, got " +
                          ("None" if scales is None else f"{scales.dtype} {tuple(scales.shape)} contiguous={scales.is_contiguous()} cuda={scales.is_cuda}"))
+    return code
 
 
 def fp8_empty(rows: int, cols: int, block_rows: int = 1, dtype=None):
@@ -679,15 +688,15 @@ def fp8_quant(x, q=None, q_scales=None, qt=None, qt_scales=None, block_rows: int
     if block_rows not in (1, 128):
         raise ValueError(f"block_rows: expected 1 or 128, got {block_rows}")
     if q is not None:
-        _expect_fp8(q, q_scales, rows, cols, block_rows, "q")
+        code = _expect_fp8(q, q_scales, rows, cols, block_rows, "q")
     if qt is not None:
-        _expect_fp8(qt, qt_scales, cols, rows, block_rows, "qt")
+        code = _expect_fp8(qt, qt_scales, cols, rows, block_rows, "qt")
         if q is not None and q.dtype is not qt.dtype:
             raise ValueError("q and qt: expected one type")
     if (q is None and q_scales is not None) or (qt is None and qt_scales is not None):
         raise ValueError("scales without their values")
     _on_current_device(stream, x, q, q_scales, qt, qt_scales)
-    _check(lib.pda_fp8_quant(_ptr(x), _type_code(x, "x"), rows, cols, max(x.stride(0), cols) if rows > 1 else cols, _fp8_code(q if q is not None else qt, "q"), block_rows,
+    _check(lib.pda_fp8_quant(_ptr(x), _type_code(x, "x"), rows, cols, max(x.stride(0), cols) if rows > 1 else cols, code, block_rows,
                              _ptr(q), _ptr(q_scales), _ptr(qt), _ptr(qt_scales), _stream_handle(stream)))
     return q, q_scales, qt, qt_scales
 
@@ -716,15 +725,14 @@ def fp8_matmul(a, a_scales, b, b_scales, out, bias=None, workspace=None, stream=
 
     K is the padded length of the rows.  out may be a view whose rows lie apart.
     """
-    import torch
+    torch = _torch()
     if a.dim() != 2 or b.dim() != 2 or a.shape[1] != b.shape[1] or a.shape[1] % 128:
         raise ValueError(f"a, b: expected [M, K] and [N, K] with rows padded to 128, got {tuple(a.shape)} and {tuple(b.shape)}")
     M, K = a.shape
     N = b.shape[0]
     block = 1 if b_scales is not None and b_scales.dim() == 2 and b_scales.shape[0] == N else 128
-    _expect_fp8(a, a_scales, M, K, 1, "a")
-    _expect_fp8(b, b_scales, N, K, block, "b")
-    if b.dtype is not torch.float8_e4m3fn:
+    code = _expect_fp8(a, a_scales, M, K, 1, "a")
+    if _expect_fp8(b, b_scales, N, K, block, "b") != PDA_E4M3:
         raise ValueError(f"b: expected float8_e4m3fn, got {b.dtype}")
     if out.dtype is not torch.bfloat16 or out.shape != (M, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N):
         raise ValueError(f"out: expected cuda bf16 {(M, N)} with compact rows, got {out.dtype} {tuple(out.shape)} stride {out.stride()}")
@@ -736,7 +744,7 @@ def fp8_matmul(a, a_scales, b, b_scales, out, bias=None, workspace=None, stream=
         workspace = _workspace(nbytes, None, stream) if nbytes else None
     else:
         _workspace(0, workspace, stream)
-    _check(lib.pda_fp8_matmul(_ptr(a), _fp8_code(a, "a"), _ptr(a_scales), _ptr(b), _ptr(b_scales), block, _ptr(bias), _ptr(out), M, N, K,
+    _check(lib.pda_fp8_matmul(_ptr(a), code, _ptr(a_scales), _ptr(b), _ptr(b_scales), block, _ptr(bias), _ptr(out), M, N, K,
                               out.stride(0) if M > 1 else N, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_handle(stream)))
     return out
 
@@ -747,7 +755,7 @@ def rms_norm_fwd(x, weight, y, res=None, h=None, y_scales=None, rstd=None, eps: 
     weight: [D], or [groups, D] with one row for every rows/groups consecutive rows, or None.  y: fp32 or bf16 of the shape of x, or
     float8_e4m3fn [rows, D padded to 128] with y_scales (fp8_empty(rows, D)).  rstd [rows] fp32, for rms_norm_bwd, or None.
     """
-    import torch
+    torch = _torch()
     rows, D, groups = _norm_sizes(stream, x, ((rstd, "rstd"),), ((weight, "weight"),), (res, h, y, y_scales))
     if (res is None) != (h is None):
         raise ValueError("res and h go together")
@@ -824,11 +832,11 @@ class Rope:
             raise ValueError(f"freqs: expected a multiple of 4 of them, at most 64, got {len(freqs)}")
         self.rot, self.layout, self.axes = 2 * len(freqs), layout, len(pairs)
         self._freqs = (C.c_double * max(len(freqs), 1))(*freqs)
-        self._pairs = (C.c_int * PDA_ROPE_MAX_AXES)(*pairs)
+        self._struct = bytes(RopeStruct(self.rot, ROPE_LAYOUTS[layout], self.axes, (C.c_int * PDA_ROPE_MAX_AXES)(*pairs), C.cast(self._freqs, C.POINTER(C.c_double)), None, 0, 0))
 
     def at(self, positions, first: int, B: int, S: int) -> RopeStruct:
         """The description for one call (positions, checked, must outlive it)."""
-        import torch
+        torch = _torch()
         pos_batch = 0
         if positions is not None:
             if first:
@@ -838,7 +846,11 @@ class Rope:
                     shape not in ((S, self.axes), (B, S, self.axes), (1, S, self.axes)):
                 raise ValueError(f"positions: expected contiguous cuda int32 {(S, self.axes)} or {(B, S, self.axes)}, got {positions.dtype} {shape}")
             pos_batch = S * self.axes if len(shape) == 3 and shape[0] == B else 0
-        return RopeStruct(self.rot, ROPE_LAYOUTS[self.layout], self.axes, self._pairs, C.cast(self._freqs, C.POINTER(C.c_double)), _ptr(positions), pos_batch, int(first))
+        r = RopeStruct.from_buffer_copy(self._struct)
+        if positions is not None:
+            r.positions, r.pos_batch = positions.data_ptr(), pos_batch
+        r.first = int(first)
+        return r
 
 
 def _token_strides(t, B, S, H, d, name):
@@ -851,7 +863,7 @@ def _token_strides(t, B, S, H, d, name):
 
 def _head_strides(t, B, H, S, d, name):
     """(batch stride, head stride) of a bf16 [B,H,S,d] view whose heads are compact."""
-    import torch
+    torch = _torch()
     if t.dtype is not torch.bfloat16 or tuple(t.shape) != (B, H, S, d):
         raise ValueError(f"{name}: expected bf16 {(B, H, S, d)}, got {t.dtype} {tuple(t.shape)}")
     st = t.stride()
