@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256, 1) void fp8_matmul_large_kernel(const MatmulPa
 // ---- middle tiles -------------------------------------------------------------------------------------------------
 // TM x TN results a workgroup of 2 x 2 wavefronts, for products that would leave most compute units without a large tile: there time is the latency of
 // memory, so six blocks of 128 are on their way at once, in a ring of eight LDS buffers with a barrier every two blocks.  A block takes 0.28 us (32 x 64) or 0.35 us (64 x 64).
-// 256 x 1 536 x 4 096 is 11.3 us with the call (32 x 64: 192 workgroups; 64 x 64: 96 workgroups, 14.1), 13.2 with a barrier every block, 16.2 with operands straight
+// 256 x 1 536 x 4 096 is 11.1 us with the call (32 x 64: 192 workgroups; 64 x 64: 96 workgroups, 14.1), 13.2 with a barrier every block, 16.2 with operands straight
 // from memory into registers.
 constexpr int kMidRing = 8, kMidChunks = 4;             // words of scales: of four blocks each
 template <int TM, int TN> constexpr int mid_stage() { return (TM + TN) * 128; }
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256) void fp8_matmul_mid_kernel(const MatmulParams 
 
 // ---- few rows -----------------------------------------------------------------------------------------------------
 // 16 x 16 results a workgroup, whose four wavefronts each take a range of K, straight from memory into registers without a barrier, and add their sums in LDS, in
-// order: for up to 16 rows, where every row of b is read once and that is all the time there is.  1 x 4 608 x 1 536 is 10.2 us with the call, 4.9 us without; 1 x 8 192 x
+// order: for up to 16 rows, where every row of b is read once and that is all the time there is.  1 x 4 608 x 1 536 is 9.8 us with the call, 4.9 us without; 1 x 8 192 x
 // 8 192 is 14.3 (32 x 64 tiles: 19.5).
 constexpr int kFewWaves = 4, kFewAhead = 4;             // blocks in registers
 template <bool E5M2>
@@ -574,7 +574,7 @@ static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
     else if (f == MatmulPlan::FEW) t = 3.0 + steps * (load > 1.1 ? 0.11 * load : 0.12);
     else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.345 : 0.28));
     if (parts > 1) {                                            // parts written and read, more than 128 MB of them from memory: 4 608 x 1 536 x 119 056 took 678 us in
-        const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units, 717 in 7 on 252 (three times)
+        const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units (now 666), 717 in 7 on 252 (three times)
         t += 5.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
     }
     return t;
