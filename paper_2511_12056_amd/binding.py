@@ -676,13 +676,16 @@ def fp8_empty(rows: int, cols: int, block_rows: int = 1, dtype=None):
 
 
 def fp8_quant(x, q=None, q_scales=None, qt=None, qt_scales=None, block_rows: int = 1, stream=None):
-    """pda_fp8_quant: x [rows, cols] fp32 or bf16 (rows may lie apart) -> q, q_scales and/or qt, qt_scales (of the transposed matrix), as fp8_empty makes them.
+    """pda_fp8_quant: x [rows, cols] fp32 or bf16 (rows may lie apart, not share elements) -> q, q_scales and/or qt, qt_scales (of the transposed matrix), as fp8_empty makes them.
 
     block_rows: 1 (a scale per row and 128 columns of what is written) or 128 (per 128 x 128, the same in both orders).
     """
     if x.dim() != 2 or not x.is_cuda or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"x: expected a cuda matrix with compact rows, got {tuple(x.shape)} stride {x.stride()}")
     rows, cols = x.shape
+    ldx = x.stride(0) if rows > 1 and cols > 0 else cols
+    if ldx < cols:
+        raise ValueError(f"x: rows that share elements (stride {x.stride()} of {tuple(x.shape)}); a row that is repeated needs .contiguous()")
     if q is None and qt is None:
         raise ValueError("neither q nor qt: nothing to compute")
     if block_rows not in (1, 128):
@@ -696,7 +699,7 @@ def fp8_quant(x, q=None, q_scales=None, qt=None, qt_scales=None, block_rows: int
     if (q is None and q_scales is not None) or (qt is None and qt_scales is not None):
         raise ValueError("scales without their values")
     _on_current_device(stream, x, q, q_scales, qt, qt_scales)
-    _check(lib.pda_fp8_quant(_ptr(x), _type_code(x, "x"), rows, cols, max(x.stride(0), cols) if rows > 1 else cols, code, block_rows,
+    _check(lib.pda_fp8_quant(_ptr(x), _type_code(x, "x"), rows, cols, ldx, code, block_rows,
                              _ptr(q), _ptr(q_scales), _ptr(qt), _ptr(qt_scales), _stream_handle(stream)))
     return q, q_scales, qt, qt_scales
 
