@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void pack_heads_kernel(const float4* __restric
             ss = __uint_as_float(r[0]) + __uint_as_float(r[1]);    // lane ^ 16
         }
         // 1/sqrt by the hardware approximation (1 ulp): far inside the bf16 rounding that follows
-        const float inv = ss > 0.f ? premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV))) : 0.f;
+        const float inv = ss == 0.f ? 0.f : premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV)));      // (NaN goes into the whole vector)
         a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
     } else if (premul != 1.0f) {
         a.x *= premul; a.y *= premul; a.z *= premul; a.w *= premul;
