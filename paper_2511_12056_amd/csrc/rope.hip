@@ -101,8 +101,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
             if constexpr (!BWD) {
                 float f = p.premul;
                 if constexpr (RMS) {
-                    const float ss = lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w);
-                    // the hardware's 1/sqrt (1 ulp): far inside the bf16 rounding that follows
+                    const float ss = sum_of_squares<LPV>(a);
+                    // the hardware's 1/sqrt (1 ulp, of a normal number): far inside the bf16 rounding that follows
                     f = ss == 0.f ? 0.f : p.premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV)));       // (NaN goes into the whole vector)
                 }
                 r = rotate(make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
