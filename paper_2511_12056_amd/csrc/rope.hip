@@ -94,6 +94,9 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
                 if constexpr (BWD) g[u] = load_cols<true>(p.y, yt + (h + u) * p.y_head);
             }
         }
+        bool again = false;
+        // the hardware's 1/sqrt (1 ulp, of a normal number): far inside the bf16 rounding that follows
+        const auto unit = [&](float ss) __attribute__((always_inline)) { return ss == 0.f ? 0.f : p.premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV))); };      // (NaN goes into the whole vector)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float4 a = x[u];
@@ -102,8 +105,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
                 float f = p.premul;
                 if constexpr (RMS) {
                     const float ss = sum_of_squares<LPV>(a);
-                    // the hardware's 1/sqrt (1 ulp, of a normal number): far inside the bf16 rounding that follows
-                    f = ss == 0.f ? 0.f : p.premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV)));       // (NaN goes into the whole vector)
+                    again = again || into_range(ss) != 1.f;
+                    f = unit(ss);
                 }
                 r = rotate(make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
             } else {
@@ -125,6 +128,18 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams p) {
             if (live && h + u < h1) {
                 if constexpr (!BWD) store_cols<true>(p.y, yt + (h + u) * p.y_head, r);
                 else store_cols<XBF16>(p.dx, dt + (h + u) * (4 * LPV), r);
+            }
+        }
+        if constexpr (!BWD && RMS) {                            // written again: in front of the stores the branch would keep the heads' sums apart, 119 056 x 12 x 128: 146 us instead of 145 (144 without it)
+            if (__any(again)) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float by = into_range(sum_of_squares<LPV>(x[u]));
+                    float4 a = make_float4(x[u].x * by, x[u].y * by, x[u].z * by, x[u].w * by);
+                    const float f = unit(sum_of_squares<LPV>(a));
+                    a = rotate(make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
+                    if (by != 1.f && live && h + u < h1) store_cols<true>(p.y, yt + (h + u) * p.y_head, a);
+                }
             }
         }
     }

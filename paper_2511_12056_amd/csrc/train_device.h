@@ -24,18 +24,12 @@ __device__ __forceinline__ float lane_sum(float x) {
     return x;
 }
 
-// Sum of the squares of a d-vector, four columns in each of its LPV lanes, for dividing the vector by their root, whatever power of two it is multiplied by: where the
-// sum is not 0 but so small that single squares have lost bits, or past fp32's range, the vector and its sum are those of 2^60 and 2^-80 times as much, exactly (columns
-// that this takes below the normal numbers are nothing beside the largest).  A branch that whole wavefronts take.
+// Sum of the squares of a d-vector, four columns of it in each of its LPV lanes.
 template <int LPV>
-__device__ __forceinline__ float sum_of_squares(float4& a) {
-    const float ss = lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w);
-    const float by = ss > 0.f && ss < 0x1p-100f ? 0x1p60f : ss == __builtin_huge_valf() ? 0x1p-80f : 1.f;
-    if (!__any(by != 1.f)) return ss;
-    a.x *= by; a.y *= by; a.z *= by; a.w *= by;
-    const float again = lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w);
-    return by != 1.f ? again : ss;
-}
+__device__ __forceinline__ float sum_of_squares(const float4& a) { return lane_sum<LPV>(a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w); }
+// What a vector is to be multiplied by, before its squares are summed again and it is divided by their root, where the sum is not 0 but so small that single squares
+// have lost bits, or past fp32's range; 1 elsewhere.  Exact (columns that this takes below the normal numbers are nothing beside the largest).
+__device__ __forceinline__ float into_range(float ss) { return ss > 0.f && ss < 0x1p-100f ? 0x1p60f : ss == __builtin_huge_valf() ? 0x1p-80f : 1.f; }
 
 // The lane's index, formed anew where it is used: the compiler cannot trace two of them back to each other, so it keeps nothing
 // derived from it in registers in between.
