@@ -32,11 +32,6 @@ static RowGrid row_grid(int64_t rows) {
 }
 __device__ __forceinline__ int64_t grid_row() { return (int64_t)blockIdx.z * gridDim.y + blockIdx.y; }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_f32(float x) {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xF, 0xF, false));
-}
-
 // Algorithm 1 steps 10-13.  grid.y/z = row r; grid.x covers the row's h*n*D/4 float4s in INPUT
 // order of the concatenated tensor (local head j, source GPU i, 4 columns): consecutive
 // workgroups read consecutive memory when the chunks are the slices of one concatenated
@@ -117,18 +112,14 @@ __global__ __launch_bounds__(256) void pack_heads_kernel(const float4* __restric
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     if (live) a = nt_load4(x + ((b * S + s) * H + hh) * LPV + lane);
     if (unit_rms) {
-        // sum of squares over the vector's LPV lanes, in registers (DPP lane permutations and, for
-        // 32 lanes, the 16-lane row swap): every lane ends up with the total
-        float ss = a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w;
-        ss += dpp_f32<0xB1>(ss);          // quad_perm [1,0,3,2]: lane ^ 1
-        ss += dpp_f32<0x4E>(ss);          // quad_perm [2,3,0,1]: lane ^ 2
-        ss += dpp_f32<0x141>(ss);         // row_half_mirror: the other quad of each 8
-        ss += dpp_f32<0x140>(ss);         // row_mirror: the other half of each 16
-        if constexpr (LPV == 32) {
-            auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(ss), __float_as_uint(ss), false, false);
-            ss = __uint_as_float(r[0]) + __uint_as_float(r[1]);    // lane ^ 16
+        float ss = sum_of_squares<LPV>(a);                    // in every lane of the vector
+        const float by = into_range(ss);
+        if (__any(by != 1.f)) {
+            a.x *= by; a.y *= by; a.z *= by; a.w *= by;
+            const float again = sum_of_squares<LPV>(a);
+            ss = by != 1.f ? again : ss;
         }
-        // 1/sqrt by the hardware approximation (1 ulp): far inside the bf16 rounding that follows
+        // 1/sqrt by the hardware approximation (1 ulp, of a normal number): far inside the bf16 rounding that follows
         const float inv = ss == 0.f ? 0.f : premul * __builtin_amdgcn_rsqf(ss * (1.0f / (4 * LPV)));      // (NaN goes into the whole vector)
         a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
     } else if (premul != 1.0f) {
