@@ -553,60 +553,6 @@ __global__ __launch_bounds__(256) void fp8_matmul_bias_kernel(const MatmulParams
     if (m < p.M && c < n4) store4(p, m, c * 4, f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
-// Tiles of the forms, in rows and columns.
-struct FormSize { int m, n; };
-static constexpr FormSize kForms[MatmulPlan::FORMS] = {{16, 16}, {32, 64}, {64, 64}, {256, 256}};
-
-// An estimate of a launch's time in us, for choosing among the forms and numbers of parts.  Its rates are fits to every form's times at 14 products, from 1 x 8 192 x 8 192
-// to 119 056 x 4 608 x 1 536 (256 compute units; us, the least of each row is what the rule takes or within 10 % of it):
-//                             few    32 x 64    64 x 64    large    large, 4 parts
-//       1 x 8 192 x 8 192      14         20         24       74          33
-//     256 x 1 536 x 4 096      29         11         14       40          19
-//   1 000 x 1 536 x 1 536      37         15         14       21          18
-//   2 000 x 1 536 x 6 144     281         85         56       59          35
-//   2 048 x 4 608 x 1 536     207         80         54       20          56
-static double form_time(int f, int64_t tiles, int parts, int steps, int n_cu) {
-    const FormSize& s = kForms[f];
-    const int64_t items = tiles * parts, rounds = (items + n_cu - 1) / n_cu;
-    const double load = (double)items / n_cu;
-    double t;
-    if (f == MatmulPlan::LARGE) t = 6.0 + (double)rounds * (steps * (1.07 + 0.4 * (load < 1.0 ? load : 1.0)) + 4.0);
-    else if (f == MatmulPlan::FEW) t = 3.0 + steps * (load > 1.1 ? 0.11 * load : 0.12);
-    else t = 3.0 + (double)rounds * (1.0 + steps * (s.m == 64 ? 0.345 : 0.28));
-    if (parts > 1) {                                            // parts written and read, more than 128 MB of them from memory: 4 608 x 1 536 x 119 056 took 678 us in
-        const double bytes = (double)items * s.m * s.n * 8;     // 2 parts on 216 compute units (now 666), 717 in 7 on 252 (three times)
-        t += 5.0 + (bytes < 128e6 ? bytes / 10e6 : 12.8 + (bytes - 128e6) / 4e6);
-    }
-    return t;
-}
-
-MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t K, int n_cu) {
-    const int nk = (int)(K / 128);
-    MatmulPlan best{0, 1, nk};
-    double best_time = 1e300;
-    if (nk == 0) return best;                                              // the bias alone
-    for (int f = 0; f < MatmulPlan::FORMS; ++f) {
-        const FormSize& s = kForms[f];
-        const int64_t tiles = (M + s.m - 1) / s.m * ((N + s.n - 1) / s.n);
-        if (tiles > 0x3fffff && f != MatmulPlan::LARGE) continue;          // a launch has fewer than 2^32 threads along x
-        for (int parts = 1; parts <= kMatmulMaxParts; ++parts) {
-            const int steps = ((nk + parts - 1) / parts + 3) / 4 * 4;      // (words of four scales in the large form)
-            if (parts > 1 && (nk + steps - 1) / steps != parts) continue;
-            const double t = form_time(f, tiles, parts, steps < nk ? steps : nk, n_cu);
-            if (t < best_time) {
-                best_time = t;
-                best = {f, parts, steps};
-            }
-        }
-    }
-    return best;
-}
-
-int64_t matmul_workspace_bytes(const MatmulPlan& w, int64_t M, int64_t N) {
-    const FormSize& s = kForms[w.form];
-    return w.parts > 1 ? w.parts * ((M + s.m - 1) / s.m) * ((N + s.n - 1) / s.n) * s.m * s.n * 4 : 0;
-}
-
 template <bool E5M2>
 static hipError_t launch_large(const MatmulParams& p, hipStream_t st) {
     static KernelSetup setup;
