@@ -21,17 +21,10 @@ __device__ __forceinline__ unsigned scale_byte(float top) {
 // 1 over the scale: 2^(127 - byte), a normal number for every byte that scale_byte gives.
 __device__ __forceinline__ float inverse_scale(unsigned byte) { return __uint_as_float((254u - byte) << 23); }
 
-// Four values, none beyond the type's largest but those that are not finite, to four bytes, nearest even.
-template <bool E5M2>
-__device__ __forceinline__ unsigned pack_fp8(float a, float b, float c, float d) {
-    int r = 0;
-    if constexpr (E5M2) {
-        r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, r, false);
-        r = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
-    } else {
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, r, false);
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
-    }
+// Four values, none beyond e4m3's largest but those that are not finite, to four bytes of it, nearest even.
+__device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
     return (unsigned)r;
 }
 

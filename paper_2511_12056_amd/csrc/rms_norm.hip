@@ -81,7 +81,7 @@ __device__ __forceinline__ void settle_row(const RmsNormParams& p, int64_t r, in
         }
         const float f = inverse_scale(byte);
         if (c < cols) {
-            __builtin_nontemporal_store(pack_fp8<false>(x[0][0] * f, x[0][1] * f, x[0][2] * f, x[0][3] * f), reinterpret_cast<unsigned*>(y + c));
+            __builtin_nontemporal_store(pack_e4m3(x[0][0] * f, x[0][1] * f, x[0][2] * f, x[0][3] * f), reinterpret_cast<unsigned*>(y + c));
             if (t % 32 == 0) p.y_scales[r * scale_cols + c / 128] = (uint8_t)byte;
         }
     }
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const Rms
                 const float f = inverse_scale(byte);
                 close = close || is_close(top);
                 if (c < cols) {                                 // (a block of lanes alike)
-                    const unsigned q = pack_fp8<false>(h[i][0] * f, h[i][1] * f, h[i][2] * f, h[i][3] * f);
+                    const unsigned q = pack_e4m3(h[i][0] * f, h[i][1] * f, h[i][2] * f, h[i][3] * f);
                     __builtin_nontemporal_store(q, reinterpret_cast<unsigned*>(static_cast<unsigned char*>(p.y) + r * cols + c));
                     if (t % 32 == 0) p.y_scales[r * scale_cols + c / 128] = (uint8_t)byte;
                 }
