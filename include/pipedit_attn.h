@@ -299,8 +299,10 @@ int pda_headchunk_run_ex(const void* q, const void* k, const void* v, float* out
 /*
  * Pre-attention pack: token-major fp32 projections x [B,S,H,d] (one row of H*d features per
  * token) to the head-major bf16 tensor y [B,H,S,d] that Algorithm 1 slices per head.  With
- * unit_rms != 0 every d-vector is first divided by its own root mean square (fp32 arithmetic;
- * a zero vector stays zero).  Every element is multiplied by premul (finite; 1 for none) before
+ * unit_rms != 0 every d-vector is first divided by its own root mean square (fp32 arithmetic, on the
+ * vector times a power of two where its squares leave that range; a zero vector, and one of elements so
+ * small that their squares in fp32 are all 0, below some 2.6e-23, becomes zeros; a NaN is in all of its
+ * vector, an infinity NaN in its place and 0 elsewhere).  Every element is multiplied by premul (finite; 1 for none) before
  * the one rounding to bf16 (nearest even): a Q packed with premul = scale * log2(e) goes with
  * pda_attn_fwd_base2.  d must be 64 or 128; x and y 16-byte aligned and distinct; B*S*H == 0 is
  * a no-op.

@@ -73,7 +73,8 @@ int pda_fp8_matmul_workspace(int64_t M, int64_t N, int64_t K, int n_cu, int64_t*
  * NULL too and stands for x.  weight [groups, D] fp32, group g holding the rows / groups consecutive rows from g * rows / groups on
  * (pda_layer_norm_fwd), or NULL (1).  y_type PDA_F32 or PDA_BF16: y [rows, D], rounded once.  y_type PDA_E4M3: y and y_scales are
  * the 8-bit matrix, in blocks of one row, of the fp32 values, as pda_fp8_quant makes it; where these are too near to a scale's border, 64 bits decide on its side.  rstd [rows] fp32, for the backward call, may be NULL.
- * h may be res or x itself (if the types agree), otherwise nothing that is written may overlap anything else.  Sums are fp32.
+ * h may be res or x itself (if the types agree), otherwise nothing that is written may overlap anything else.  Sums are fp32 (rstd is 0 where
+ * the squares of a row pass its range).
  * 1 <= D <= PDA_LAYER_NORM_MAX; eps finite and >= 0; tensors 16-byte aligned, y_scales and rstd 4-byte; rows == 0 is a no-op.
  */
 int pda_rms_norm_fwd(const void* x, int x_type, const void* res, int res_type, const float* weight, void* h, void* y, int y_type,

@@ -124,8 +124,8 @@ int pda_layer_norm_bwd_workspace(int64_t rows, int64_t groups, int D, int n_cu, 
  *
  *     dx = premul * r * (dy - xh * mean(dy * xh)),        0 for a zero vector
  *
- * mean(x^2) is taken in fp32, as by the pack: a vector of elements so small that their squares are 0 (below some 1e-23) counts as
- * a zero vector (the squares lose bits below some 1e-19), one whose squares pass fp32's range (some 1e19) has the gradient 0.  A NaN in the vector or its dy makes all of its dx NaN.
+ * mean(x^2) is taken in fp32: a vector of elements so small that their squares are 0 (below some 1e-23) counts as
+ * a zero vector, as in the pack (the squares lose bits below some 1e-19), one whose squares pass fp32's range (some 1e19) has the gradient 0.  A NaN in the vector or its dy makes all of its dx NaN.
  *
  * x is the pack's input and is read with unit_rms only (NULL without).  dx may be x itself.  The rounding of the pack
  * counts as the identity.  d, alignment and sizes as pda_pack_heads, H < 2^24.

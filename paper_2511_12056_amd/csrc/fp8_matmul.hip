@@ -91,7 +91,7 @@ __device__ __forceinline__ void store8(const MatmulParams& p, int64_t m, int64_t
 // after the next.  Behind the second (slot 31) all have read those rows and their scales too, which are fetched, and the rest of the next block has arrived.  A fetch has 54 slots
 // (1 730 cycles) at least, and a wavefront asks for 1 KB every third slot: faster, requests wait in line and matrix instructions behind them.
 // A workgroup goes through its items (tiles, or ranges of K of a tile) without a break; blocks are fetched across the border of an item too.
-// 119 056 x 4 608 x 1 536: 680 to 735 us (2.3 to 2.5 PFLOP/s; boxes differ), of which 65 are stores and 70 conversion and LDS; 8 192^3: 2.9 PFLOP/s.  The matrix units are 64 to 71 %
+// 119 056 x 4 608 x 1 536: 680 to 735 us (2.3 to 2.5 PFLOP/s; cards differ), of which 65 are stores and 70 conversion and LDS; 8 192^3: 2.9 PFLOP/s.  The matrix units are 64 to 71 %
 // busy at 1.9 to 2.0 of 2.4 GHz.
 constexpr int kLargeA = 0, kLargeB = kLargeA + 32768, kLargeStage = kLargeB + 32768, kLargeScales = 2 * kLargeStage, kLargeSa = 0, kLargeSb = 1024, kLargeBias = kLargeScales + 2 * 2048, kLargeEdge = kLargeBias + 4 * 1024, kLargeSmem = kLargeEdge + 4 * 4096;
 

@@ -6,7 +6,7 @@
 // nothing.  A lane's columns turn as x cos + partner * (-sin or sin): the partner lies in the same lane (interleaved) or rot/8 lanes away (half), which
 // takes four lane permutations through LDS.
 //
-// 119 056 x 12 x 128, unit RMS: 145 us (5.05 TB/s), 427 with a head a workgroup.  2 x 4 797 x 12 x 64, the gradient: 15.7 us with a workgroup for half of the heads, 18.7 for all
+// 119 056 x 12 x 128, unit RMS: 146 us (5.0 TB/s), 427 with a head a workgroup.  2 x 4 797 x 12 x 64, the gradient: 15.7 us with a workgroup for half of the heads, 18.7 for all
 // of them, 19.5 for one.
 #include <hip/hip_runtime.h>
 #include "attn_internal.h"
