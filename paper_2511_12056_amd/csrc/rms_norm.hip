@@ -90,7 +90,7 @@ __device__ __forceinline__ void settle_row(const RmsNormParams& p, int64_t r, in
 template <bool VEC, int TPR, int NV>
 __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const RmsNormParams p) {
     constexpr int RPW = ln_threads(TPR) / TPR;                  // rows of a workgroup
-    __shared__ float lds[TPR > 64 ? 2 * (TPR / 64) : 1];
+    __shared__ float lds[TPR > 64 ? 4 * (TPR / 64) : 1];
     const int t = threadIdx.x % TPR, D = p.D;
     const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW + threadIdx.x / TPR;
     if (r >= p.rows) return;                                    // RPW > 1: no barrier follows
@@ -115,7 +115,18 @@ __global__ __launch_bounds__(ln_threads(TPR)) void rms_norm_fwd_kernel(const Rms
 #pragma unroll
         for (int e = 0; e < 4; ++e) ss = __builtin_fmaf(h[i][e], h[i][e], ss);
     row_sum<TPR>(ss, zero, lds);
-    const float rstd = 1.0f / sqrtf(ss / (float)D + p.eps);
+    float rstd = 1.0f / sqrtf(ss / (float)D + p.eps);
+    // Squares so small that they lose bits, and no eps that hides it: those of the row times a power of two.  The threads of a row take this alike.
+    const float by = ss < 0x1p-100f && p.eps < 0x1p-90f ? 0x1p60f : 1.f;
+    if (__any(by != 1.f)) {
+        float again = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) again = __builtin_fmaf(h[i][e] * by, h[i][e] * by, again);
+        row_sum<TPR>(again, zero, lds + 2 * (TPR / 64));
+        if (by != 1.f) rstd = by / sqrtf(again / (float)D + p.eps * by * by);
+    }
     const int64_t g = p.groups == 1 ? 0 : (unsigned)r / (unsigned)p.group_rows;       // rows < 2^31
     if (p.weight) {
         float w[NV][4];
